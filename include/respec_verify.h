@@ -54,7 +54,8 @@ typedef enum {
   RESPEC_ERR_HIP = 7,       /* a HIP call or kernel launch failed                            */
   RESPEC_ERR_WORKSPACE = 8, /* workspace missing or not 256-byte aligned                    */
   RESPEC_ERR_TOKEN = 9,     /* seq_status only: a draft token or source tag is out of range */
-  RESPEC_ERR_SCRATCH = 10   /* respec_verify_step_noalloc: the plan does not fit the static scratch */
+  RESPEC_ERR_SCRATCH = 10,  /* respec_verify_step_noalloc: the plan does not fit the static scratch */
+  RESPEC_ERR_PAGE = 11      /* seq_status of respec_prompt.h only: a page id is out of range   */
 } respec_status;
 
 typedef enum { RESPEC_F32 = 0, RESPEC_BF16 = 1 } respec_dtype;

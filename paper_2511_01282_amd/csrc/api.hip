@@ -65,6 +65,7 @@ const char* respec_status_string(respec_status st) {
     case RESPEC_ERR_WORKSPACE: return "workspace missing or not 256-byte aligned";
     case RESPEC_ERR_TOKEN: return "draft token or source tag out of range";
     case RESPEC_ERR_SCRATCH: return "plan needs more workspace or sequences than the static scratch of the allocation-free step holds";
+    case RESPEC_ERR_PAGE: return "page id out of range";
   }
   return "unknown status";
 }

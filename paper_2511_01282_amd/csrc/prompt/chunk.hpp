@@ -1,0 +1,75 @@
+// Device helpers shared by the kernels that work on chunks of new tokens.
+#pragma once
+
+#include "../common.hpp"
+#include "prompt.hpp"
+
+namespace respec {
+
+constexpr int kStShape = 2, kStCapacity = 6, kStPage = 11;
+
+// Sequence b of a chunk batch; a sequence with unusable lengths has no tokens.
+struct ChunkSeq {
+  int t0, n, L, status;
+};
+__device__ __forceinline__ ChunkSeq chunk_seq(const ChunkBatch& c, int b) {
+  const int t0 = c.new_off[b], t1 = c.new_off[b + 1], L = c.kv_len[b];
+  ChunkSeq s{t0, 0, L, 0};
+  // (as 64-bit: no difference or sum of the device's words wraps)
+  const long long n = (long long)t1 - t0;
+  if (t0 < 0 || n < 0 || t1 > c.total_new || n > c.max_new)
+    s.status = kStShape;
+  else if (L < 0 || L > c.max_kv || (long long)L + n > (long long)c.table_width * c.page.d)
+    s.status = kStCapacity;
+  else
+    s.n = (int)n;
+  return s;
+}
+
+// Byte offset of row r of a sequence within a KV head of the cache.  A page id out of
+// range (reported by report_status) reads page 0 instead.
+__device__ __forceinline__ int64_t row_offset(const ChunkBatch& c, const int32_t* table, uint32_t r) {
+  const uint32_t p = div_by(r, c.page);
+  const int32_t id = table[p];
+  const int64_t page = (uint32_t)id < (uint32_t)c.n_pages ? id : 0;
+  return page * c.page_stride + (int64_t)((uint64_t)(r - p * c.page.d) * c.row_stride);
+}
+
+// The sequence that owns packed token t (n = 0: none), by a whole wave: a lane per sequence.
+__device__ __forceinline__ ChunkSeq seq_of_token(const ChunkBatch& c, int t, int& b) {
+  for (int b0 = 0; b0 < c.batch; b0 += 64) {
+    const int k = b0 + (int)(threadIdx.x & 63);
+    ChunkSeq s{0, 0, 0, 0};
+    if (k < c.batch) s = chunk_seq(c, k);
+    const uint64_t own = __ballot(t >= s.t0 && t - s.t0 < s.n);
+    if (own) {
+      const int l = __builtin_ctzll(own);
+      b = b0 + l;
+      return ChunkSeq{__builtin_amdgcn_readlane(s.t0, l), __builtin_amdgcn_readlane(s.n, l),
+                      __builtin_amdgcn_readlane(s.L, l), 0};
+    }
+  }
+  b = 0;
+  return ChunkSeq{0, 0, 0, 0};
+}
+
+// Status of sequence b, by one workgroup of NT threads: its lengths, then the page ids of
+// rows [lo, L + n), lo = 0 or L.
+template <int NT>
+__device__ __forceinline__ void report_status(const ChunkBatch& c, int b, bool from_zero) {
+  const ChunkSeq s = chunk_seq(c, b);
+  __shared__ int bad;
+  if (threadIdx.x == 0) bad = 0;
+  __syncthreads();
+  if (s.n > 0) {
+    const int32_t* table = c.table + (int64_t)b * c.table_stride;
+    const uint32_t p0 = from_zero ? 0u : div_by((uint32_t)s.L, c.page), p1 = div_by((uint32_t)(s.L + s.n - 1), c.page);
+    bool any = false;
+    for (uint32_t p = p0 + threadIdx.x; p <= p1; p += NT) any |= (uint32_t)table[p] >= (uint32_t)c.n_pages;
+    if (any) bad = 1;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) c.status[b] = s.status ? s.status : (bad ? kStPage : 0);
+}
+
+}  // namespace respec

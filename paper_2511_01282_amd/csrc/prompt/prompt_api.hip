@@ -1,0 +1,247 @@
+// Host side of the prompt side's C ABI: plans, argument validation, launches.
+// See include/respec_prompt.h for the contract.
+#include <limits.h>
+#include <math.h>
+
+#include <algorithm>
+#include <new>
+
+#include "../../../include/respec_prompt.h"
+#include "prompt.hpp"
+
+using namespace respec;
+
+struct respec_chunk_plan {
+  respec_chunk_shape s;
+  int es;            // bytes per element
+  size_t part_rows;  // rows of partials that the workspace holds
+  size_t total;
+};
+
+struct respec_score_plan {
+  respec_score_shape s;
+  int ko;            // width of the key lists: 8 or 16
+  size_t total;
+};
+
+namespace {
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+bool aligned(const void* p, size_t n) { return ((uintptr_t)p % n) == 0; }
+bool known(int32_t dtype) { return dtype == RESPEC_F32 || dtype == RESPEC_BF16; }
+long long cdiv(long long a, long long b) { return (a + b - 1) / b; }
+
+constexpr int kMaxSplits = 64;             // a lane of the merge per split
+constexpr size_t kMaxPartRows = 1u << 18;  // 136 MB at 128 columns
+constexpr int kMaxStride = 1 << 24;
+
+// Checks of a stride in elements: non-negative and whole 16-byte pieces.
+bool stride_ok(int64_t s, int es) { return s >= 0 && s < (1ll << 50) && s * es % 16 == 0; }
+
+respec_status check_batch(const respec_chunk_plan* plan, const respec_chunk_batch& b) {
+  const respec_chunk_shape& s = plan->s;
+  if (b.batch < 0 || b.total_new < 0 || b.max_new_in_batch < 0 || b.max_kv_len_in_batch < 0) return RESPEC_ERR_SHAPE;
+  if (b.batch > s.max_batch || b.total_new > s.max_new || b.max_kv_len_in_batch > s.max_kv_len) return RESPEC_ERR_CAPACITY;
+  if (b.max_new_in_batch > b.total_new) return RESPEC_ERR_SHAPE;
+  if (b.batch == 0) return RESPEC_OK;
+  const respec_paged_cache& c = b.cache;
+  if (!b.new_off || !b.kv_len || !c.k || !c.v || !c.page_table) return RESPEC_ERR_NULL;
+  if (c.n_pages < 1 || c.page_size < 1 || c.table_width < 1) return RESPEC_ERR_SHAPE;
+  if (b.batch > 1 && c.table_stride < c.table_width) return RESPEC_ERR_SHAPE;
+  if (!stride_ok(c.page_stride, plan->es) || !stride_ok(c.head_stride, plan->es) || !stride_ok(c.row_stride, plan->es) ||
+      c.row_stride > kMaxStride)
+    return RESPEC_ERR_SHAPE;
+  if (!aligned(c.k, 16) || !aligned(c.v, 16)) return RESPEC_ERR_SHAPE;
+  return RESPEC_OK;
+}
+
+ChunkBatch device_batch(const respec_chunk_plan* plan, const respec_chunk_batch& b) {
+  const respec_paged_cache& c = b.cache;
+  ChunkBatch d;
+  d.new_off = b.new_off;
+  d.kv_len = b.kv_len;
+  d.table = c.page_table;
+  d.status = b.seq_status;
+  d.k = static_cast<char*>(c.k);
+  d.v = static_cast<char*>(c.v);
+  d.page_stride = c.page_stride * plan->es;
+  d.head_stride = c.head_stride * plan->es;
+  d.table_stride = c.table_stride;
+  d.row_stride = (uint32_t)(c.row_stride * plan->es);
+  d.page = fast_div((uint32_t)c.page_size);
+  d.batch = b.batch;
+  d.total_new = b.total_new;
+  d.max_new = b.max_new_in_batch;
+  d.max_kv = b.max_kv_len_in_batch;
+  d.n_pages = c.n_pages;
+  d.table_width = c.table_width;
+  d.n_kv_heads = plan->s.n_kv_heads;
+  d.group = plan->s.n_q_heads / plan->s.n_kv_heads;
+  return d;
+}
+
+}  // namespace
+
+extern "C" {
+
+respec_status respec_chunk_create(const respec_chunk_shape* shape, respec_chunk_plan** out) {
+  if (!shape || !out) return RESPEC_ERR_NULL;
+  *out = nullptr;
+  const respec_chunk_shape& s = *shape;
+  if (!known(s.dtype)) return RESPEC_ERR_DTYPE;
+  if (s.head_dim != 64 && s.head_dim != 128) return RESPEC_ERR_SHAPE;
+  if (s.n_q_heads < 1 || s.n_q_heads > RESPEC_CHUNK_MAX_HEADS || s.n_kv_heads < 1 || s.n_q_heads % s.n_kv_heads != 0)
+    return RESPEC_ERR_SHAPE;
+  if (s.max_batch < 1 || s.max_batch > RESPEC_CHUNK_MAX_BATCH || s.max_new < 1 || s.max_kv_len < 0) return RESPEC_ERR_SHAPE;
+  if ((long long)s.max_new * s.n_q_heads > INT_MAX || (long long)s.max_new + s.max_kv_len > INT_MAX) return RESPEC_ERR_SHAPE;
+  respec_chunk_plan* p = new (std::nothrow) respec_chunk_plan();
+  if (!p) return RESPEC_ERR_CAPACITY;
+  p->s = s;
+  p->es = s.dtype == RESPEC_BF16 ? 2 : 4;
+  p->part_rows = std::min((size_t)s.max_new * s.n_q_heads * kMaxSplits, kMaxPartRows);
+  p->total = align256(p->part_rows * s.head_dim * 4) + 2 * align256(p->part_rows * 4);
+  *out = p;
+  return RESPEC_OK;
+}
+
+void respec_chunk_destroy(respec_chunk_plan* plan) { delete plan; }
+
+size_t respec_chunk_workspace_bytes(const respec_chunk_plan* plan) { return plan ? plan->total : 0; }
+
+respec_status respec_chunk_append(const respec_chunk_plan* plan, const respec_chunk_append_args* args, void* stream) {
+  if (!plan || !args) return RESPEC_ERR_NULL;
+  const respec_chunk_append_args& x = *args;
+  const respec_status st = check_batch(plan, x.b);
+  if (st != RESPEC_OK) return st;
+  if (x.b.batch == 0) return RESPEC_OK;
+  if (x.b.total_new > 0) {
+    if (!x.k_new || !x.v_new) return RESPEC_ERR_NULL;
+    if (!aligned(x.k_new, 16) || !aligned(x.v_new, 16)) return RESPEC_ERR_SHAPE;
+    for (int64_t s : {x.k_token_stride, x.k_head_stride, x.v_token_stride, x.v_head_stride})
+      if (!stride_ok(s, plan->es)) return RESPEC_ERR_SHAPE;
+  } else if (!x.b.seq_status) {
+    return RESPEC_OK;
+  }
+  AppendArgs a;
+  a.b = device_batch(plan, x.b);
+  a.k_new = static_cast<const char*>(x.k_new);
+  a.v_new = static_cast<const char*>(x.v_new);
+  a.k_tok = x.k_token_stride * plan->es;
+  a.k_head = x.k_head_stride * plan->es;
+  a.v_tok = x.v_token_stride * plan->es;
+  a.v_head = x.v_head_stride * plan->es;
+  const int pieces = 2 * plan->s.n_kv_heads * plan->s.head_dim * plan->es / 16;  // of a token
+  a.per_tok = fast_div((uint32_t)pieces);
+  a.tok_per_wg = std::max(1, std::min(2048 / pieces, kAppendMaxTok));
+  return launch_chunk_append(plan->es, plan->s.head_dim, a, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? RESPEC_OK
+             : RESPEC_ERR_HIP;
+}
+
+respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chunk_attn_args* args, void* workspace,
+                                void* stream) {
+  if (!plan || !args) return RESPEC_ERR_NULL;
+  if (!workspace || !aligned(workspace, 256)) return RESPEC_ERR_WORKSPACE;
+  const respec_chunk_attn_args& x = *args;
+  const respec_status st = check_batch(plan, x.b);
+  if (st != RESPEC_OK) return st;
+  if (!(x.scale >= 0.f) || isinf(x.scale)) return RESPEC_ERR_PARAM;
+  if (x.b.batch == 0) return RESPEC_OK;
+  if (x.b.total_new > 0) {
+    if (!x.q || !x.out) return RESPEC_ERR_NULL;
+    if (!aligned(x.q, 16) || !aligned(x.out, 16)) return RESPEC_ERR_SHAPE;
+    for (int64_t s : {x.q_token_stride, x.q_head_stride, x.out_token_stride, x.out_head_stride})
+      if (!stride_ok(s, plan->es)) return RESPEC_ERR_SHAPE;
+  } else if (!x.b.seq_status) {
+    return RESPEC_OK;
+  }
+  const respec_chunk_shape& s = plan->s;
+  ChunkAttnArgs a;
+  a.b = device_batch(plan, x.b);
+  a.q = static_cast<const char*>(x.q);
+  a.out = static_cast<char*>(x.out);
+  a.q_tok = x.q_token_stride * plan->es;
+  a.q_head = x.q_head_stride * plan->es;
+  a.o_tok = x.out_token_stride * plan->es;
+  a.o_head = x.out_head_stride * plan->es;
+  a.group = fast_div((uint32_t)a.b.group);
+  char* ws = static_cast<char*>(workspace);
+  const size_t o_bytes = align256(plan->part_rows * s.head_dim * 4), m_bytes = align256(plan->part_rows * 4);
+  a.part_o = reinterpret_cast<float*>(ws);
+  a.part_m = reinterpret_cast<float*>(ws + o_bytes);
+  a.part_l = reinterpret_cast<float*>(ws + o_bytes + m_bytes);
+  a.scale_log2 = (float)(1.4426950408889634 * (x.scale > 0.f ? (double)x.scale : 1.0 / sqrt((double)s.head_dim)));
+  a.rows_per_wg = 64;
+  a.n_rowblk = (int)cdiv((long long)a.b.max_new * a.b.group, a.rows_per_wg);
+  const long long items = (long long)a.n_rowblk * s.n_kv_heads * a.b.batch;
+  const long long limit = (long long)a.b.max_kv + a.b.max_new;  // rows that the last token of the longest sequence sees
+  long long n = 1;
+  if (items > 0) {
+    n = std::min({1024 / items, cdiv(limit, 256), (long long)kMaxSplits,
+                  (long long)(plan->part_rows / ((size_t)a.b.total_new * s.n_q_heads))});
+    n = std::max(n, 1ll);
+  }
+  a.split_rows = n == 1 ? INT_MAX : (int)cdiv(cdiv(limit, n), 32) * 32;
+  a.nsplit = n == 1 ? 1 : (int)cdiv(limit, a.split_rows);
+  if (a.nsplit == 1) a.split_rows = INT_MAX;
+  if (items * a.nsplit + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
+  hipStream_t stm = static_cast<hipStream_t>(stream);
+  if (launch_chunk_attn(s.dtype, s.head_dim, a, stm) != hipSuccess) return RESPEC_ERR_HIP;
+  if (a.nsplit > 1 && launch_chunk_merge(s.dtype, s.head_dim, a, stm) != hipSuccess) return RESPEC_ERR_HIP;
+  return RESPEC_OK;
+}
+
+respec_status respec_score_create(const respec_score_shape* shape, respec_score_plan** out) {
+  if (!shape || !out) return RESPEC_ERR_NULL;
+  *out = nullptr;
+  const respec_score_shape& s = *shape;
+  if (!known(s.dtype)) return RESPEC_ERR_DTYPE;
+  if (s.topk_out < 1 || s.topk_out > RESPEC_MAX_TOPK_OUT || s.vocab < s.topk_out || s.vocab >= 1 << 30 || s.max_rows < 1)
+    return RESPEC_ERR_SHAPE;
+  respec_score_plan* p = new (std::nothrow) respec_score_plan();
+  if (!p) return RESPEC_ERR_CAPACITY;
+  p->s = s;
+  p->ko = s.topk_out <= 8 ? 8 : 16;
+  // rows in parts: at most kScoreParts workgroups in all (one row: kScoreMaxKeys / ko)
+  const long long records = std::min({(long long)s.max_rows * (kScoreMaxKeys / p->ko), (long long)kScoreParts});
+  p->total = align256((size_t)records * (kScoreWords + 2 * p->ko) * 4);
+  *out = p;
+  return RESPEC_OK;
+}
+
+void respec_score_destroy(respec_score_plan* plan) { delete plan; }
+
+size_t respec_score_workspace_bytes(const respec_score_plan* plan) { return plan ? plan->total : 0; }
+
+respec_status respec_score(const respec_score_plan* plan, const respec_score_args* args, void* workspace,
+                           void* stream) {
+  if (!plan || !args) return RESPEC_ERR_NULL;
+  if (!workspace || !aligned(workspace, 256)) return RESPEC_ERR_WORKSPACE;
+  const respec_score_shape& s = plan->s;
+  const respec_score_args& x = *args;
+  if (x.rows < 0) return RESPEC_ERR_SHAPE;
+  if (x.rows > s.max_rows) return RESPEC_ERR_CAPACITY;
+  if (x.rows == 0) return RESPEC_OK;
+  if (!x.logits) return RESPEC_ERR_NULL;
+  const int es = s.dtype == RESPEC_BF16 ? 2 : 4;
+  if (!aligned(x.logits, es) || (x.rows > 1 && (x.row_stride < s.vocab || x.row_stride >= 1ll << 50))) return RESPEC_ERR_SHAPE;
+  ScoreArgs a;
+  a.z = x.logits;
+  a.row_stride = x.row_stride;
+  a.token = x.token;
+  a.part = static_cast<float*>(workspace);
+  a.tok_logprob = x.tok_logprob;
+  a.tok_rank = x.tok_rank;
+  a.lse = x.lse;
+  a.entropy = x.entropy;
+  a.topk_id = x.topk_id;
+  a.topk_logprob = x.topk_logprob;
+  a.rows = x.rows;
+  a.vocab = s.vocab;
+  a.topk_out = s.topk_out;
+  a.parts = std::max(1, std::min({kScoreParts / x.rows, kScoreMaxKeys / plan->ko, s.vocab / 2048}));
+  if ((long long)a.rows * a.parts > INT_MAX) return RESPEC_ERR_SHAPE;
+  return launch_score(s.dtype, plan->ko, a, static_cast<hipStream_t>(stream)) == hipSuccess ? RESPEC_OK : RESPEC_ERR_HIP;
+}
+
+}  // extern "C"

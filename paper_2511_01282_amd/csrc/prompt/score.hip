@@ -1,0 +1,311 @@
+// Log probability and rank of a given token, entropy and top alternatives, per row of logits.
+//
+//   m = max z, S = sum e^(z-m), T = sum e^(z-m) (z-m)
+//   lse = m + log S, H = log S - T/S, log p(t) = (z_t - m) - log S
+//   rank(t) = #{u : z_u > z_t} + #{u < t : z_u = z_t}
+//
+// One pass over the row.  A thread keeps the largest logit so far, S and T against it, the count for
+// the rank, and the 16-byte vector that held its largest logit first.  (A reference maximum that is raised
+// only now and then would save rescalings, but not here: T against a reference 16 below the maximum
+// loses 4 bits of the entropy when it is moved.)  The top alternatives need no bookkeeping in the pass: the K-th largest
+// of the threads' maxima, H, is at most the K-th largest logit, so every one of the top K is in a vector
+// of one of the K threads whose maximum reaches H; only those threads' vectors are read again.
+//
+// Keys: (value, id) pairs as 64-bit integers (common.hpp), all distinct, so ties go to the lowest id.
+#include "topk.hpp"
+#include "prompt.hpp"
+
+namespace respec {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kUnroll = 4;         // vectors of a thread per step
+constexpr int kMaxKeys = kScoreMaxKeys;  // keys that reach H and are sorted (more: by repeated passes)
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float exp_f(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+
+// Statistics of a set of logits: the largest one, and S and T against reference ref (-inf: none finite yet).
+struct Stats {
+  float top, ref, S, T;
+  int cnt;
+};
+
+// The same with the sums against a larger maximum.
+__device__ __forceinline__ void rebase(Stats& s, float to) {
+  const bool none = s.ref == kNegInf;
+  const float d = none ? 0.f : s.ref - to, e = none ? 1.f : exp_f(d);
+  s.T = e * (s.T + d * s.S);
+  s.S *= e;
+  s.ref = to;
+}
+
+// Sum over a workgroup's threads; every thread of wave 0 returns it.
+__device__ __forceinline__ Stats all_stats(Stats s, Stats* lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  auto wave_all = [&](Stats& x) {
+    x.top = wave_max(x.top);
+    rebase(x, x.top);
+    x.S = wave_sum(x.S);
+    x.T = wave_sum(x.T);
+    for (int o = 32; o > 0; o >>= 1) x.cnt += __shfl_xor(x.cnt, o, 64);
+  };
+  wave_all(s);
+  if (lane == 0) lds[wave] = s;
+  __syncthreads();
+  s = Stats{kNegInf, kNegInf, 0.f, 0.f, 0};
+  if (lane < kWaves) s = lds[lane];
+  wave_all(s);
+  return s;
+}
+
+// The K largest of up to kMaxKeys keys in LDS: wave 0's lane k returns the k-th (0: fewer keys).
+template <int KO>
+__device__ __forceinline__ uint64_t largest(const uint64_t* keys, int n, uint64_t* lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int at = wave * 64 + lane;
+  uint64_t k = sort_lanes_desc(at < n ? keys[at] : 0ull);
+  if (n <= 64) return k;  // (uniform)
+  if (lane < KO) lds[wave * KO + lane] = k;
+  __syncthreads();
+  return sort_lanes_desc(lane < kWaves * KO ? lds[lane] : 0ull);
+}
+
+// A row's results from its statistics and top keys (wave 0).
+__device__ __forceinline__ void write_row(const ScoreArgs& a, int row, const Stats& s, bool has_tok, bool tok_ok, float zt,
+                                          uint64_t key) {
+  const int lane = threadIdx.x & 63;
+  const float nan = __builtin_nanf("");
+  const bool bad = !(s.S == s.S), none = s.top == kNegInf;
+  const float log_s = logf(s.S);
+  if (lane == 0) {
+    if (a.lse) a.lse[row] = bad ? nan : none ? kNegInf : s.top + log_s;
+    if (a.entropy) a.entropy[row] = bad ? nan : none ? 0.f : log_s - s.T / s.S;
+    if (a.tok_logprob)
+      a.tok_logprob[row] = bad || (has_tok && !tok_ok) ? nan : !has_tok ? 0.f : none ? kNegInf : (zt - s.top) - log_s;
+    if (a.tok_rank) a.tok_rank[row] = bad || !tok_ok ? -1 : s.cnt;
+  }
+  if (lane < a.topk_out) {
+    const int64_t at = (int64_t)row * a.topk_out + lane;
+    if (a.topk_id) a.topk_id[at] = bad ? -1 : key_id(key);
+    if (a.topk_logprob) a.topk_logprob[at] = bad ? nan : none ? kNegInf : (key_value(key) - s.top) - log_s;
+  }
+}
+
+template <typename T>
+struct Vec {
+  static constexpr int N = 16 / Elem<T>::kBytes;
+  float z[N];
+  __device__ __forceinline__ void load(const char* p) {
+    const u32x4 x = ld16(p);
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      if constexpr (N == 4) z[e] = __uint_as_float(x[e]);
+      else z[e] = __uint_as_float(e % 2 ? x[e / 2] & 0xFFFF0000u : x[e / 2] << 16);
+    }
+  }
+};
+
+// The least float above x (x no NaN and not +inf).
+__device__ __forceinline__ float next_above(float x) {
+  const uint32_t u = __float_as_uint(x == 0.f ? 0.f : x);
+  return __uint_as_float(x < 0.f ? u - 1 : u + 1);
+}
+
+template <typename T, int KO>
+__global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
+  constexpr int N = Vec<T>::N, ES = Elem<T>::kBytes;
+  __shared__ Stats l_stats[kWaves];
+  __shared__ uint64_t l_top[kWaves * KO], l_keys[kMaxKeys];
+  __shared__ int l_cand[KO];
+  __shared__ int l_n[2];
+  const int row = (int)(blockIdx.x / (unsigned)a.parts), part = (int)(blockIdx.x % (unsigned)a.parts);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
+  const char* z = reinterpret_cast<const char*>(a.z) + (int64_t)row * a.row_stride * ES;
+  // Vectors of N logits, aligned to 16 bytes: vector j holds logits j N - off .. ; those cut by the
+  // row's ends ("edges", the first and the last) go element by element.
+  const int off = (int)(((uintptr_t)z / ES) % N);
+  const char* base = z - off * ES;
+  const int v_lo = off ? 1 : 0, v_hi = (a.vocab + off) / N, nv = max(0, v_hi - v_lo);
+  const int j0 = v_lo + (int)((int64_t)nv * part / a.parts), j1 = v_lo + (int)((int64_t)nv * (part + 1) / a.parts);
+  const int tok = a.token ? a.token[row] : -1;
+  const bool has_tok = tok != -1, tok_ok = tok >= 0 && tok < a.vocab;
+  const float zt = tok_ok ? Elem<T>::to_f32(z, tok) : 0.f;
+  // a logit counts for the rank if it is at least z_t before the token's vector, and more than z_t from
+  // there on (the vector's own ties are added below)
+  const int jt = tok_ok ? (tok + off) / N : 0;
+  const float thr_lo = tok_ok ? zt : __builtin_huge_valf(), thr_hi = tok_ok ? next_above(zt) : __builtin_huge_valf();
+
+  Stats s{kNegInf, kNegInf, 0.f, 0.f, 0};
+  int jb = j0 + tid < j1 ? j0 + tid : -1;  // vector that held the thread's largest logit first
+  for (int j = j0 + tid; j - tid < j1; j += kThreads * kUnroll) {
+    Vec<T> x[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) x[u].load(base + (int64_t)max(min(j + u * kThreads, j1 - 1), j0) * 16);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int ju = j + u * kThreads;
+      const bool in = ju < j1;
+      float top = x[u].z[0];
+#pragma unroll
+      for (int e = 1; e < N; ++e) top = fmaxf(top, x[u].z[e]);
+      const bool more = in && top > s.top;
+      s.top = more ? top : s.top;
+      jb = more ? ju : jb;
+      const float thr = in ? (ju < jt ? thr_lo : thr_hi) : __builtin_huge_valf();
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        x[u].z[e] = in ? x[u].z[e] : kNegInf;
+        s.cnt += x[u].z[e] >= thr ? 1 : 0;
+      }
+    }
+    if (__any(s.top > s.ref)) {
+      if (s.top > s.ref) rebase(s, s.top);
+    }
+    const float ref = s.ref == kNegInf ? 0.f : s.ref;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float d = x[u].z[e] - ref, p = exp_f(d);  // (a NaN or +inf makes S a NaN)
+        s.S += p;
+        s.T = __builtin_fmaf(p, fmaxf(d, -200.f), s.T);  // (-inf: 0 times a finite number)
+      }
+  }
+  // edges: thread e < N the row's first logits, N <= e < 2 N its last
+  uint64_t edge = 0;
+  if (tid < 2 * N) {
+    const int id = tid < N ? (part == 0 && off && tid < N - off ? tid : -1)
+                           : (part == a.parts - 1 ? v_hi * N - off + tid - N : -1);
+    // (a row of less than one vector: its only logits are the last ones)
+    if (id >= 0 && id < a.vocab && !(tid < N && v_hi < v_lo)) {
+      const float x = Elem<T>::to_f32(z, id);
+      edge = make_key(x, id);
+      if (x > s.top) s.top = x;
+      if (s.top > s.ref) rebase(s, s.top);
+      const float d = x - (s.ref == kNegInf ? 0.f : s.ref), p = exp_f(d);
+      s.S += p;
+      s.T = __builtin_fmaf(p, fmaxf(d, -200.f), s.T);
+      s.cnt += tok_ok && (x > zt || (x == zt && id < tok)) ? 1 : 0;
+    }
+  }
+  // ties of the token's own vector in front of it
+  if (tok_ok && jt >= j0 && jt < j1 && tid < N) {
+    const int id = jt * N - off + tid;
+    s.cnt += id < tok && Elem<T>::to_f32(z, id) == zt ? 1 : 0;
+  }
+
+  // ---- top K of the part ----
+  const bool want_top = a.topk_id || a.topk_logprob;
+  uint64_t key = 0;
+  if (want_top) {
+    uint64_t mine = 0;
+    if (jb >= 0) {
+      Vec<T> x;
+      x.load(base + (int64_t)jb * 16);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const uint64_t k = make_key(x.z[e], jb * N - off + e);
+        mine = x.z[e] == x.z[e] && k > mine ? k : mine;
+      }
+    }
+    const uint64_t sorted = sort_lanes_desc(mine);
+    if (lane < KO) l_top[wave * KO + lane] = sorted;
+    if (tid < 2) l_n[tid] = 0;
+    __syncthreads();
+    const uint64_t H = key_of_lane(sort_lanes_desc(lane < kWaves * KO ? l_top[lane] : 0ull), KO - 1);
+    if (mine != 0 && mine >= H) l_cand[atomicAdd(&l_n[0], 1)] = tid;  // (at most KO: keys are distinct)
+    if (edge != 0 && edge >= H) l_keys[atomicAdd(&l_n[1], 1)] = edge;
+    __syncthreads();
+    const int per = (j1 - j0 + kThreads - 1) / kThreads, total = l_n[0] * per;
+    for (int x = tid; x < total; x += kThreads) {
+      const int j = j0 + l_cand[x / per] + (x % per) * kThreads;
+      if (j >= j1) continue;
+      Vec<T> v;
+      v.load(base + (int64_t)j * 16);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const uint64_t k = make_key(v.z[e], j * N - off + e);
+        if (k >= H && v.z[e] == v.z[e]) {
+          const int at = atomicAdd(&l_n[1], 1);
+          if (at < kMaxKeys) l_keys[at] = k;
+        }
+      }
+    }
+    __syncthreads();
+    const int n = l_n[1];
+    if (n <= kMaxKeys) {
+      key = largest<KO>(l_keys, n, l_top);
+    } else {
+      // more than that reach H (values in an order that favours few threads): the largest key below
+      // the one before, KO times over
+      const int e_lo = part == 0 ? 0 : j0 * N - off, e_hi = part == a.parts - 1 ? a.vocab : j1 * N - off;
+      uint64_t below = ~0ull;
+      for (int r = 0; r < KO; ++r) {
+        uint64_t best = 0;
+        for (int e = e_lo + tid; e < e_hi; e += kThreads) {
+          const float x = Elem<T>::to_f32(z, e);
+          const uint64_t k = make_key(x, e);
+          best = x == x && k < below && k > best ? k : best;
+        }
+        best = key_of_lane(sort_lanes_desc(best), 0);
+        __syncthreads();
+        if (lane == 0) l_top[wave] = best;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) best = l_top[w] > best ? l_top[w] : best;
+        below = best;
+        key = lane == r ? best : key;
+      }
+    }
+  }
+  s = all_stats(s, l_stats);
+  if (wave != 0) return;
+  if (a.parts == 1) {
+    write_row(a, row, s, has_tok, tok_ok, zt, key);
+  } else {
+    float* p = a.part + ((int64_t)row * a.parts + part) * (kScoreWords + 2 * KO);
+    if (lane == 0) *reinterpret_cast<f32x4*>(p) = f32x4{s.top, s.S, s.T, __int_as_float(s.cnt)};
+    if (lane < KO) reinterpret_cast<uint64_t*>(p + kScoreWords)[lane] = key;
+  }
+}
+
+// Rows that were scored in parts (kMaxKeys / KO at most).
+template <typename T, int KO>
+__global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs a) {
+  __shared__ Stats l_stats[kWaves];
+  __shared__ uint64_t l_top[kWaves * KO], l_keys[kMaxKeys];
+  const int row = blockIdx.x, tid = threadIdx.x;
+  const float* p = a.part + (int64_t)row * a.parts * (kScoreWords + 2 * KO);
+  Stats s{kNegInf, kNegInf, 0.f, 0.f, 0};
+  if (tid < a.parts) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(p + tid * (kScoreWords + 2 * KO));
+    s = Stats{x[0], x[0], x[1], x[2], __float_as_int(x[3])};
+  }
+  if (tid < a.parts * KO)
+    l_keys[tid] = reinterpret_cast<const uint64_t*>(p + (tid / KO) * (kScoreWords + 2 * KO) + kScoreWords)[tid % KO];
+  s = all_stats(s, l_stats);  // (its barrier orders the keys, too)
+  const uint64_t key = largest<KO>(l_keys, a.parts * KO, l_top);
+  if (tid >= 64) return;
+  const int tok = a.token ? a.token[row] : -1;
+  const bool tok_ok = tok >= 0 && tok < a.vocab;
+  const float zt = tok_ok ? Elem<T>::to_f32(a.z, (size_t)((int64_t)row * a.row_stride + tok)) : 0.f;
+  write_row(a, row, s, tok != -1, tok_ok, zt, key);
+}
+
+template <typename T, int KO>
+hipError_t go(const ScoreArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((score_kernel<T, KO>), dim3((unsigned)a.rows * a.parts), dim3(kThreads), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.parts == 1) return e;
+  hipLaunchKernelGGL((score_join_kernel<T, KO>), dim3(a.rows), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_score(int dtype, int ko, const ScoreArgs& a, hipStream_t s) {
+  if (dtype == 1) return ko == 8 ? go<bf16_t, 8>(a, s) : go<bf16_t, 16>(a, s);
+  return ko == 8 ? go<float, 8>(a, s) : go<float, 16>(a, s);
+}
+
+}  // namespace respec

@@ -72,4 +72,21 @@ __device__ __forceinline__ void report_status(const ChunkBatch& c, int b, bool f
   if (threadIdx.x == 0) c.status[b] = s.status ? s.status : (bad ? kStPage : 0);
 }
 
+// A workgroup's item: the pairs of sequence and KV head follow one another (a pair's workgroups meet on
+// one XCD where the pairs are a multiple of 8, and read its tiles at about the same time), then the splits,
+// then the row blocks, the longest first.
+struct Item {
+  int split, g, rb, b;
+};
+__device__ __forceinline__ Item item_of(const ChunkBatch& c, const ChunkGeom& ge, int x) {
+  const int pairs = c.n_kv_heads * c.batch, pair = x % pairs, y = x / pairs;
+  return Item{y % ge.nsplit, pair % c.n_kv_heads, ge.n_rowblk - 1 - y / ge.nsplit, pair / c.n_kv_heads};
+}
+
+// Cache rows that the rows of block rb see (at least one).
+__device__ __forceinline__ int block_limit(const ChunkAttnArgs& a, const ChunkGeom& ge, const ChunkSeq& s, int rb) {
+  const int last = min((rb + 1) * ge.rows_per_wg, s.n * a.b.group) - 1;
+  return s.L + (int)div_by((uint32_t)last, a.group) + 1;
+}
+
 }  // namespace respec

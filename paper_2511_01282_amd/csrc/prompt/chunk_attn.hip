@@ -11,31 +11,9 @@
 namespace respec {
 namespace {
 
-// A workgroup's item.
-struct Item {
-  int split, g, rb, b;
-};
-
-__device__ __forceinline__ Item item_of(const ChunkAttnArgs& a, int x) {
-  Item it;
-  it.split = x % a.nsplit;
-  x /= a.nsplit;
-  it.g = x % a.b.n_kv_heads;
-  x /= a.b.n_kv_heads;
-  it.b = x % a.b.batch;
-  it.rb = a.n_rowblk - 1 - x / a.b.batch;  // (the longest first)
-  return it;
-}
-
-// Cache rows that the rows of block rb see (at least one).
-__device__ __forceinline__ int block_limit(const ChunkAttnArgs& a, const ChunkSeq& s, int rb) {
-  const int last = min((rb + 1) * a.rows_per_wg, s.n * a.b.group) - 1;
-  return s.L + (int)div_by((uint32_t)last, a.group) + 1;
-}
-
-template <typename T, int D>
-__global__ __launch_bounds__(256) void chunk_attn_rows_kernel(ChunkAttnArgs a) {
-  constexpr int ES = Elem<T>::kBytes;
+template <int D>
+__global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a, int items) {
+  constexpr int ES = 4;
   constexpr int KC = D * ES / 64;      // 64-byte K-chunks of a head row
   constexpr int DB = D / 16;
   constexpr int TK = 32;
@@ -43,20 +21,20 @@ __global__ __launch_bounds__(256) void chunk_attn_rows_kernel(ChunkAttnArgs a) {
   constexpr int CPR = D * ES / 16;
   __shared__ __align__(16) unsigned char ks[TK * PITCH], vs[TK * PITCH];
 
-  const int items = (int)gridDim.x - (a.b.status ? a.b.batch : 0);
   if ((int)blockIdx.x >= items) {
     report_status<256>(a.b, (int)blockIdx.x - items, true);
     return;
   }
-  const Item it = item_of(a, blockIdx.x);
+  const ChunkGeom& ge = a.wide;
+  const Item it = item_of(a.b, ge, blockIdx.x);
   const ChunkSeq sq = chunk_seq(a.b, it.b);
-  const int rows = sq.n * a.b.group, row0 = it.rb * a.rows_per_wg;
+  const int rows = sq.n * a.b.group, row0 = it.rb * ge.rows_per_wg;
   if (row0 >= rows) return;
-  const int limit = block_limit(a, sq, it.rb);
-  const int lo = it.split * a.split_rows;
+  const int limit = block_limit(a, ge, sq, it.rb);
+  const int lo = it.split * ge.split_rows;
   if (lo >= limit) return;
-  const bool whole = limit <= a.split_rows;   // the block's only split
-  const int hi = a.nsplit == 1 ? limit : min(limit, lo + a.split_rows);
+  const bool whole = limit <= ge.split_rows;   // the block's only split
+  const int hi = ge.nsplit == 1 ? limit : min(limit, lo + ge.split_rows);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c16 = lane & 15, g4 = lane >> 4;
   const int row = row0 + wave * 16 + c16, rowc = min(row, rows - 1);
@@ -90,7 +68,7 @@ __global__ __launch_bounds__(256) void chunk_attn_rows_kernel(ChunkAttnArgs a) {
       s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < KC; ++c)
-        s[u] = mma_k64(T{}, *reinterpret_cast<const u32x4*>(ks + (u * 16 + c16) * PITCH + c * 64 + g4 * 16), qf[c], s[u]);
+        s[u] = mma_k64(0.f, *reinterpret_cast<const u32x4*>(ks + (u * 16 + c16) * PITCH + c * 64 + g4 * 16), qf[c], s[u]);
     }
     const int end = min(vis, hi);
     float mx = kNegInf;
@@ -123,7 +101,7 @@ __global__ __launch_bounds__(256) void chunk_attn_rows_kernel(ChunkAttnArgs a) {
     const bool masked = __any(r0 + TK > end);
     bool odd = false;
     auto value = [&](int key, int d) {
-      float v = Elem<T>::to_f32(vs + key * PITCH, d);
+      float v = Elem<float>::to_f32(vs + key * PITCH, d);
       if (masked && !(fabsf(v) < __builtin_huge_valf())) {
         odd = true;
         v = 0.f;
@@ -132,24 +110,12 @@ __global__ __launch_bounds__(256) void chunk_attn_rows_kernel(ChunkAttnArgs a) {
     };
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
-      if constexpr (ES == 4) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          u32x4 vf;
+      for (int u = 0; u < 2; ++u) {
+        u32x4 vf;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) vf[e] = __float_as_uint(value(u * 16 + g4 * 4 + e, d * 16 + c16));
-          o[d] = mma_k64(T{}, vf, __builtin_bit_cast(u32x4, p[u]), o[d]);
-        }
-      } else {
-        u32x4 vf, pf;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const int u = w / 2, e = 2 * (w % 2);
-          vf[w] = (uint32_t)f32_to_bf16(value(u * 16 + g4 * 4 + e, d * 16 + c16)) |
-                  (uint32_t)f32_to_bf16(value(u * 16 + g4 * 4 + e + 1, d * 16 + c16)) << 16;
-          pf[w] = (uint32_t)f32_to_bf16(p[u][e]) | (uint32_t)f32_to_bf16(p[u][e + 1]) << 16;
-        }
-        o[d] = mma_k64(T{}, vf, pf, o[d]);
+        for (int e = 0; e < 4; ++e) vf[e] = __float_as_uint(value(u * 16 + g4 * 4 + e, d * 16 + c16));
+        o[d] = mma_k64(0.f, vf, __builtin_bit_cast(u32x4, p[u]), o[d]);
       }
     }
     if (__any(odd)) {
@@ -165,7 +131,7 @@ __global__ __launch_bounds__(256) void chunk_attn_rows_kernel(ChunkAttnArgs a) {
             for (int d = 0; d < DB; ++d)
 #pragma unroll
               for (int x = 0; x < 4; ++x) {
-                const float v = Elem<T>::to_f32(vs + key * PITCH, d * 16 + g4 * 4 + x);
+                const float v = Elem<float>::to_f32(vs + key * PITCH, d * 16 + g4 * 4 + x);
                 if (!(fabsf(v) < __builtin_huge_valf())) o[d][x] += pk * v;
               }
           }
@@ -180,7 +146,7 @@ __global__ __launch_bounds__(256) void chunk_attn_rows_kernel(ChunkAttnArgs a) {
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) Elem<T>::store(to, d * 16 + g4 * 4 + e, o[d][e] * inv);
+      for (int e = 0; e < 4; ++e) Elem<float>::store(to, d * 16 + g4 * 4 + e, o[d][e] * inv);
   } else {
     const int64_t hq = (int64_t)a.b.n_kv_heads * a.b.group;
     const int64_t pr = ((int64_t)it.split * a.b.total_new + t) * hq + head;
@@ -201,11 +167,12 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkAttnArgs a) {
   int b;
   const ChunkSeq sq = seq_of_token(a.b, blockIdx.x, b);
   if (sq.n == 0) return;
+  const ChunkGeom& ge = sq.n * a.b.group <= a.few_rows ? a.few : a.wide;
   const int hq = a.b.n_kv_heads * a.b.group, i = (int)blockIdx.x - sq.t0;
   for (int h = blockIdx.y * 4 + wave; h < hq; h += gridDim.y * 4) {
     const int hh = h - (int)div_by((uint32_t)h, a.group) * a.b.group;
-    const int limit = block_limit(a, sq, (i * a.b.group + hh) / a.rows_per_wg);
-    const int ns = (limit + a.split_rows - 1) / a.split_rows;  // (at most 64)
+    const int limit = block_limit(a, ge, sq, (i * a.b.group + hh) / ge.rows_per_wg);
+    const int ns = (limit + ge.split_rows - 1) / ge.split_rows;  // (at most 64)
     if (ns <= 1) continue;
     const int64_t step = (int64_t)a.b.total_new * hq, pr = (int64_t)blockIdx.x * hq + h;
     const float ms = lane < ns ? a.part_m[lane * step + pr] : kNegInf;
@@ -228,11 +195,6 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkAttnArgs a) {
 }
 
 template <typename T, int D>
-hipError_t go(const ChunkAttnArgs& a, unsigned grid, hipStream_t s) {
-  hipLaunchKernelGGL((chunk_attn_rows_kernel<T, D>), dim3(grid), dim3(256), 0, s, a);
-  return hipGetLastError();
-}
-template <typename T, int D>
 hipError_t go_merge(const ChunkAttnArgs& a, hipStream_t s) {
   const int hq = a.b.n_kv_heads * a.b.group;
   hipLaunchKernelGGL((chunk_merge_kernel<T, D>), dim3(a.b.total_new, (hq + 3) / 4), dim3(256), 0, s, a);
@@ -241,11 +203,12 @@ hipError_t go_merge(const ChunkAttnArgs& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_chunk_attn(int dtype, int head_dim, const ChunkAttnArgs& a, hipStream_t s) {
-  const unsigned grid =
-      (unsigned)a.nsplit * a.b.n_kv_heads * a.n_rowblk * a.b.batch + (a.b.status ? (unsigned)a.b.batch : 0u);
-  if (dtype == 1) return head_dim == 128 ? go<bf16_t, 128>(a, grid, s) : go<bf16_t, 64>(a, grid, s);
-  return head_dim == 128 ? go<float, 128>(a, grid, s) : go<float, 64>(a, grid, s);
+hipError_t launch_chunk_attn_f32(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s) {
+  const int items = (int)item_count(a.b, a.wide);
+  const dim3 grid(items + (status ? a.b.batch : 0));
+  if (head_dim == 128) hipLaunchKernelGGL(chunk_attn_f32_kernel<128>, grid, dim3(256), 0, s, a, items);
+  else hipLaunchKernelGGL(chunk_attn_f32_kernel<64>, grid, dim3(256), 0, s, a, items);
+  return hipGetLastError();
 }
 
 hipError_t launch_chunk_merge(int dtype, int head_dim, const ChunkAttnArgs& a, hipStream_t s) {

@@ -1,0 +1,224 @@
+// Causal attention of long chunks over a paged cache, bf16: 256 query rows per workgroup.
+//
+// Four waves own 64 rows each, as two groups of 32, so that a K or V fragment read from LDS serves
+// two matrix products: with 32 rows per wave the fragments of four waves' worth of rows would take the LDS's whole
+// bandwidth (128 bytes per clock) at the matrix cores' rate.  One wave per SIMD, then, with up to 512
+// registers, and it has to keep the matrix core busy by itself: while one group's products run, the
+// other group's softmax does.  Per 32 keys:
+//   phase A:  S_0 = K Q_0^T (next keys), O_0 += V^T P_0 (these)   beside   P_1 of S_1 (these)
+//   phase B:  S_1 = K Q_1^T (next keys), O_1 += V^T P_1 (these)   beside   P_0 of S_0 (next)
+// 16 products of 32 clocks per phase against 16 exponentials of 16 clocks and 32 other instructions of
+// 4.  The fragments of the next 32 keys are read from LDS in the same phases.
+//
+// Tiles of 64 cache rows go round an LDS ring by DMA, each wave bringing 16 of the rows.
+#include <type_traits>
+
+#include "chunk_pages.hpp"
+#include "chunk_tile.hpp"
+
+namespace respec {
+namespace {
+
+constexpr int kTile = 64;
+
+template <int D>
+struct WideShape {
+  static constexpr int S = 4;                      // ring slots
+  static constexpr int kHalf = kTile * D * 2;      // bytes of a K or V tile
+  static constexpr int kSlot = 2 * kHalf;
+  static constexpr int kIds = S * kSlot;
+  static constexpr int kLds = kIds + 4 * kPageIds * 4;
+  static_assert(kLds <= 163840, "LDS of a CU");
+};
+
+// One matrix product, a few vector instructions, one exponential, one LDS read, sixteen times over.
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // DS read
+    __builtin_amdgcn_sched_group_barrier(0x402, 3, 0);  // VALU
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a, int items) {
+  using G = WideShape<D>;
+  using Feed = RowFeed<D, 16>;
+  constexpr int KS = D / 16, DB = D / 32, NR = Feed::NR, S = G::S;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  if ((int)blockIdx.x >= items) {
+    report_status<256>(a.b, (int)blockIdx.x - items, true);
+    return;
+  }
+  const ChunkGeom& ge = a.wide;
+  const Item it = item_of(a.b, ge, blockIdx.x);
+  const ChunkSeq sq = chunk_seq(a.b, it.b);
+  const int rows = sq.n * a.b.group, row0 = it.rb * ge.rows_per_wg;
+  if (row0 >= rows || rows <= a.few_rows) return;
+  const int limit = block_limit(a, ge, sq, it.rb);
+  const int lo = it.split * ge.split_rows;
+  if (lo >= limit) return;
+  const bool whole = limit <= ge.split_rows;  // the block's only split
+  const int hi_row = ge.nsplit == 1 ? limit : min(limit, lo + ge.split_rows);
+  const int nt = (hi_row - lo + kTile - 1) / kTile;
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r32 = lane & 31, hi = lane >> 5;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char*)smem;
+
+  // ---- this wave's rows ----
+  const int wrow = row0 + wave * 64;
+  const bool live = wrow < rows;
+  int64_t tok[2], head[2];
+  int end[2];  // cache rows that this lane's row of each group sees, within the split
+  u32x4 qf[2][KS];
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    const int row = min(wrow + g * 32 + r32, rows - 1), i = (int)div_by((uint32_t)row, a.group);
+    tok[g] = sq.t0 + i;
+    head[g] = (int64_t)it.g * a.b.group + (row - i * a.b.group);
+    end[g] = min(sq.L + i + 1, hi_row);
+    const char* q = a.q + tok[g] * a.q_tok + head[g] * a.q_head;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[g][ks] = ld16(q + (2 * ks + hi) * 16);
+  }
+  // (uniform) tiles that some row of the wave sees, and those from which on some row does not see all
+  const int last = min(wrow + 63, rows - 1);
+  const int my_end = min(sq.L + (int)div_by((uint32_t)last, a.group) + 1, hi_row);
+  const int my_first = min(sq.L + (int)div_by((uint32_t)min(wrow, rows - 1), a.group) + 1, hi_row);
+  const int my_nt = live && my_end > lo ? (my_end - lo + kTile - 1) / kTile : 0;
+  const int unmasked = max(my_first - lo, 0) / kTile;  // tiles that every row sees whole
+
+  // ---- DMA ----
+  Feed feed;
+  feed.init(a.b, it.g, lane);
+  PageIds ids{reinterpret_cast<int32_t*>(smem + G::kIds) + wave * kPageIds, a.b.table + (int64_t)it.b * a.b.table_stride, 0u, 0u,
+              div_by((uint32_t)(hi_row - 1), a.b.page) + 1u};
+  const bool in_page = a.b.page.d % 16 == 0;  // a wave's 16 rows of a tile lie in one page
+  int produced = 0;
+  auto produce = [&]() {
+    const int t0 = lo + produced * kTile + wave * 16, slot = produced % S;
+    const uint32_t dst = lds0 + (uint32_t)(slot * G::kSlot + wave * 16 * D * 2);
+    const uint32_t pa = div_by((uint32_t)min(t0, hi_row - 1), a.b.page);
+    ids.need(pa, div_by((uint32_t)min(t0 + 15, hi_row - 1), a.b.page), lane);
+    if (in_page && t0 + 16 <= hi_row)
+      feed.from_page(a.b, dst, dst + G::kHalf, ids.uniform(pa), (uint32_t)t0 - pa * a.b.page.d);
+    else
+      feed.from_rows(a.b, dst, dst + G::kHalf, ids.ids, ids.p0, t0, hi_row, lane);
+    ++produced;
+  };
+  // Tiles up to t have landed for every wave (t < produced).
+  auto landed = [&](int t) {
+    const int newer = produced - 1 - t;
+    if (newer >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * NR) : "memory");
+    else if (newer == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NR) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  };
+  for (int t = 0; t < min(nt, S - 1); ++t) produce();
+
+  // ---- rows' state; the first tile's scores ----
+  Rows<D> r[2];
+  r[0].init();
+  r[1].init();
+  f32x16 s[2];
+  u32x4 p[2][2], kf[2][KS], vf[2][DB][2];
+  landed(0);
+  if (my_nt > 0) {
+    read_k<D>(smem, lane, kf[1]);
+    read_v<D>(smem + G::kHalf, lane, vf[0]);
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      s[g] = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) s[g] = mma32(kf[1][ks], qf[g][ks], s[g]);
+      mask_scores(s[g], lo, end[g], lane);
+    }
+    read_k<D>(smem + 32 * D * 2, lane, kf[0]);
+    settle(r[0], s[0], a.scale_log2, p[0], weights(s[0], a.scale_log2, r[0].m, p[0]));
+  }
+
+  // 32 keys: substep u of tile j.  kf[u] holds the next substep's K fragments, vf[u] this one's V fragments.
+  auto substep = [&](auto masked_c, auto u_c, int j) {
+    constexpr bool MASKED = decltype(masked_c)::value;
+    constexpr int U = decltype(u_c)::value;
+    const unsigned char* t_cur = smem + (j % S) * G::kSlot;
+    const unsigned char* t_next = smem + ((j + 1) % S) * G::kSlot;
+    const int key0 = lo + j * kTile + 32 * U;
+    bool odd = false;
+    if constexpr (MASKED) odd = take_out_not_finite<D>(vf[U]);
+    // phase A
+    s[0] = f32x16{};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) s[0] = mma32(kf[U][ks], qf[0][ks], s[0]);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2) r[0].o[db] = mma32(vf[U][db][k2], p[0][k2], r[0].o[db]);
+    const float sum1 = weights(s[1], a.scale_log2, r[1].m, p[1]);
+    read_k<D>(t_next + (U ? 32 * D * 2 : 0), lane, kf[1 - U]);
+    interleave();
+    settle(r[1], s[1], a.scale_log2, p[1], sum1);
+    // phase B
+    if constexpr (MASKED) mask_scores(s[0], key0 + 32, end[0], lane);
+    s[1] = f32x16{};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) s[1] = mma32(kf[U][ks], qf[1][ks], s[1]);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2) r[1].o[db] = mma32(vf[U][db][k2], p[1][k2], r[1].o[db]);
+    const float sum0 = weights(s[0], a.scale_log2, r[0].m, p[0]);
+    read_v<D>((U ? t_next : t_cur + 32 * D * 2) + G::kHalf, lane, vf[1 - U]);
+    interleave();
+    if constexpr (MASKED) {
+      mask_scores(s[1], key0 + 32, end[1], lane);
+      if (odd) add_not_finite<D, 2>(r, t_cur + G::kHalf + 32 * U * D * 2, key0, end, lane);
+    }
+    settle(r[0], s[0], a.scale_log2, p[0], sum0);
+  };
+  using No = std::integral_constant<bool, false>;
+  using Yes = std::integral_constant<bool, true>;
+  using I0 = std::integral_constant<int, 0>;
+  using I1 = std::integral_constant<int, 1>;
+
+#pragma unroll 1
+  for (int j = 0; j < nt; ++j) {
+    landed(min(j + 1, nt - 1));  // (and every wave is done with tile j - 1, whose slot is filled again)
+    if (produced < nt) produce();
+    if (j >= my_nt) continue;
+    if (j + 2 <= unmasked) {     // (the next tile's scores are taken, too)
+      substep(No{}, I0{}, j);
+      substep(No{}, I1{}, j);
+    } else {
+      substep(Yes{}, I0{}, j);
+      substep(Yes{}, I1{}, j);
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < 2; ++g)
+    store_rows<D>(r[g], a, whole, it.split, tok[g], head[g], wrow + g * 32 + r32 < rows, lane);
+}
+
+template <int D>
+hipError_t go(bool launch, const ChunkAttnArgs& a, bool status, hipStream_t s) {
+  if (!launch)
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&chunk_attn_wide_kernel<D>),
+                               hipFuncAttributeMaxDynamicSharedMemorySize, WideShape<D>::kLds);
+  const int items = (int)item_count(a.b, a.wide);
+  hipLaunchKernelGGL(chunk_attn_wide_kernel<D>, dim3(items + (status ? a.b.batch : 0)), dim3(256), WideShape<D>::kLds, s, a, items);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_chunk_attn_wide(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s) {
+  return head_dim == 128 ? go<128>(true, a, status, s) : go<64>(true, a, status, s);
+}
+hipError_t set_chunk_attn_wide_lds_limit(int head_dim) {
+  const ChunkAttnArgs none{};
+  return head_dim == 128 ? go<128>(false, none, false, nullptr) : go<64>(false, none, false, nullptr);
+}
+
+}  // namespace respec

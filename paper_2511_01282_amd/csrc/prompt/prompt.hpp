@@ -52,6 +52,14 @@ struct AppendArgs {
   int32_t tok_per_wg;
 };
 
+// How an attention kernel cuts its sequences: a workgroup per (row block, split, KV head, sequence).
+struct ChunkGeom {
+  int32_t rows_per_wg;  // query rows, (token, head-in-group) pairs, of a block
+  int32_t n_rowblk;     // blocks of the longest chunk
+  int32_t nsplit;       // splits of the longest sequence; 1: no partials
+  int32_t split_rows;   // cache rows of a split
+};
+
 struct ChunkAttnArgs {
   ChunkBatch b;
   const char* q;
@@ -62,11 +70,14 @@ struct ChunkAttnArgs {
   float* part_m;      // [nsplit][total_new * Hq] (log2 units)
   float* part_l;
   float scale_log2;   // scale * log2(e)
-  int32_t nsplit;     // 1: out is written by the attention kernel
-  int32_t split_rows; // cache rows of a split
-  int32_t n_rowblk;   // row blocks of the longest chunk
-  int32_t rows_per_wg;
+  // sequences of up to few_rows query rows per KV head are the first geometry's, the others the second's
+  int32_t few_rows;
+  ChunkGeom few, wide;
 };
+inline long long item_count(const ChunkBatch& c, const ChunkGeom& ge) {
+  return (long long)c.n_kv_heads * c.batch * ge.nsplit * ge.n_rowblk;
+}
+constexpr int kFewRows = 32;   // of bf16 chunks; float32 has the second geometry only
 
 struct ScoreArgs {
   const void* z;
@@ -82,7 +93,13 @@ constexpr int kScoreMaxKeys = 256;
 constexpr int kScoreParts = 1024;  // workgroups that a few rows are cut into
 
 hipError_t launch_chunk_append(int es, int head_dim, const AppendArgs& a, hipStream_t s);
-hipError_t launch_chunk_attn(int dtype, int head_dim, const ChunkAttnArgs& a, hipStream_t s);
+// float32; `status`: whether this launch reports the sequences' status
+hipError_t launch_chunk_attn_f32(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s);
+// bf16: sequences of at most / more than kFewRows query rows per KV head
+hipError_t launch_chunk_attn_few(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s);
+hipError_t launch_chunk_attn_wide(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s);
+hipError_t set_chunk_attn_few_lds_limit(int head_dim);
+hipError_t set_chunk_attn_wide_lds_limit(int head_dim);
 hipError_t launch_chunk_merge(int dtype, int head_dim, const ChunkAttnArgs& a, hipStream_t s);
 hipError_t launch_score(int dtype, int ko, const ScoreArgs& a, hipStream_t s);
 

@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 #include <new>
 
 #include "../../../include/respec_prompt.h"
@@ -78,6 +79,36 @@ ChunkBatch device_batch(const respec_chunk_plan* plan, const respec_chunk_batch&
   d.n_kv_heads = plan->s.n_kv_heads;
   d.group = plan->s.n_q_heads / plan->s.n_kv_heads;
   return d;
+}
+
+// Splits of at least `least` cache rows (multiples of `unit`), so many that there are about `wgs` workgroups, if
+// every sequence were the longest.
+ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, int n_rowblk, long long limit, int unit, int least, int wgs, int held) {
+  ChunkGeom g{rows_per_wg, n_rowblk, 1, INT_MAX};
+  const long long items = (long long)n_rowblk * b.n_kv_heads * b.batch;
+  if (items == 0) return g;
+  const long long n = std::min({wgs / items, cdiv(limit, least), (long long)held});
+  if (n <= 1) return g;
+  const long long rows = cdiv(cdiv(limit, n), unit) * unit;
+  if (rows >= limit) return g;
+  g.split_rows = (int)rows;
+  g.nsplit = (int)cdiv(limit, rows);
+  return g;
+}
+
+// Raise the LDS limits of the attention kernels on the current device, once (a call into the runtime that also
+// loads the kernels: the first step pays it).
+bool raise_lds_limits(int head_dim) {
+  constexpr int kMaxDevices = 64;
+  static std::atomic<uint64_t> done[2];  // [head size], a bit per device
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0) return false;
+  std::atomic<uint64_t>& d = done[head_dim == 128];
+  const uint64_t bit = dev < kMaxDevices ? 1ull << dev : 0;  // (past the last: every call raises them)
+  if (d.load(std::memory_order_acquire) & bit) return true;
+  if (set_chunk_attn_few_lds_limit(head_dim) != hipSuccess || set_chunk_attn_wide_lds_limit(head_dim) != hipSuccess) return false;
+  d.fetch_or(bit, std::memory_order_release);
+  return true;
 }
 
 }  // namespace
@@ -171,23 +202,35 @@ respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chun
   a.part_m = reinterpret_cast<float*>(ws + o_bytes);
   a.part_l = reinterpret_cast<float*>(ws + o_bytes + m_bytes);
   a.scale_log2 = (float)(1.4426950408889634 * (x.scale > 0.f ? (double)x.scale : 1.0 / sqrt((double)s.head_dim)));
-  a.rows_per_wg = 64;
-  a.n_rowblk = (int)cdiv((long long)a.b.max_new * a.b.group, a.rows_per_wg);
-  const long long items = (long long)a.n_rowblk * s.n_kv_heads * a.b.batch;
   const long long limit = (long long)a.b.max_kv + a.b.max_new;  // rows that the last token of the longest sequence sees
-  long long n = 1;
-  if (items > 0) {
-    n = std::min({1024 / items, cdiv(limit, 256), (long long)kMaxSplits,
-                  (long long)(plan->part_rows / ((size_t)a.b.total_new * s.n_q_heads))});
-    n = std::max(n, 1ll);
-  }
-  a.split_rows = n == 1 ? INT_MAX : (int)cdiv(cdiv(limit, n), 32) * 32;
-  a.nsplit = n == 1 ? 1 : (int)cdiv(limit, a.split_rows);
-  if (a.nsplit == 1) a.split_rows = INT_MAX;
-  if (items * a.nsplit + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
+  const long long rows = (long long)a.b.max_new * a.b.group;    // query rows per KV head of the longest chunk
+  const int held = x.b.total_new > 0 ? (int)std::min<size_t>(plan->part_rows / ((size_t)x.b.total_new * s.n_q_heads), kMaxSplits) : 1;
   hipStream_t stm = static_cast<hipStream_t>(stream);
-  if (launch_chunk_attn(s.dtype, s.head_dim, a, stm) != hipSuccess) return RESPEC_ERR_HIP;
-  if (a.nsplit > 1 && launch_chunk_merge(s.dtype, s.head_dim, a, stm) != hipSuccess) return RESPEC_ERR_HIP;
+  bool status = a.b.status != nullptr;  // (the first launch reports it)
+  if (s.dtype == RESPEC_F32) {
+    a.few_rows = 0;
+    a.few = ChunkGeom{1, 0, 1, INT_MAX};
+    a.wide = geometry(a.b, 64, (int)cdiv(rows, 64), limit, 32, 256, 1024, held);
+    if (item_count(a.b, a.wide) + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
+    if (launch_chunk_attn_f32(s.head_dim, a, status, stm) != hipSuccess) return RESPEC_ERR_HIP;
+  } else {
+    a.few_rows = kFewRows;
+    a.few = geometry(a.b, kFewRows, 1, limit, 128, 256, 2048, held);
+    a.wide = geometry(a.b, 256, (int)cdiv(rows, 256), limit, 64, 512, 512, held);
+    if (item_count(a.b, a.few) + a.b.batch > INT_MAX || item_count(a.b, a.wide) + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
+    if (!raise_lds_limits(s.head_dim)) return RESPEC_ERR_HIP;
+    const bool any_wide = rows > kFewRows, any_few = !any_wide || a.b.batch > 1;
+    if (any_wide) {
+      if (launch_chunk_attn_wide(s.head_dim, a, status, stm) != hipSuccess) return RESPEC_ERR_HIP;
+      status = false;
+    } else {
+      a.wide = a.few;
+    }
+    if (any_few && launch_chunk_attn_few(s.head_dim, a, status, stm) != hipSuccess) return RESPEC_ERR_HIP;
+  }
+  if (x.b.total_new > 0 && (a.few.nsplit > 1 || a.wide.nsplit > 1) &&
+      launch_chunk_merge(s.dtype, s.head_dim, a, stm) != hipSuccess)
+    return RESPEC_ERR_HIP;
   return RESPEC_OK;
 }
 

@@ -21,6 +21,10 @@ FLAGS = [
     "-I", os.path.join(ROOT, "include"),
 ]
 
+# matrix products accumulate in ordinary registers: the kernel's softmax works on them, and its queries fill the
+# accumulation registers
+FILE_FLAGS = {"chunk_attn_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+
 
 CXX = os.environ.get("CXX", "g++")
 # host-only sources (the drafting side): plain C++, no FP contraction so that the
@@ -44,7 +48,7 @@ def build(verbose: bool = False) -> str:
     for src in sources():
         obj = os.path.join(OBJ, os.path.basename(src) + ".o")
         objs.append(obj)
-        cmd = [HIPCC, *FLAGS, "-c", src, "-o", obj]
+        cmd = [HIPCC, *FLAGS, *FILE_FLAGS.get(os.path.basename(src), []), "-c", src, "-o", obj]
         procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
     for src in host_sources():
         obj = os.path.join(OBJ, os.path.basename(src) + ".o")

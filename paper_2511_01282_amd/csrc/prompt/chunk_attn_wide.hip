@@ -31,16 +31,6 @@ struct WideShape {
   static_assert(kLds <= 163840, "LDS of a CU");
 };
 
-// One matrix product, a few vector instructions, one exponential, one LDS read, sixteen times over.
-__device__ __forceinline__ void interleave() {
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // DS read
-    __builtin_amdgcn_sched_group_barrier(0x402, 3, 0);  // VALU
-  }
-}
-
 template <int D>
 __global__ __launch_bounds__(256, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a, int items) {
   using G = WideShape<D>;
@@ -83,6 +73,11 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[g][ks] = ld16(q + (2 * ks + hi) * 16);
   }
+  // (the queries in accumulation registers, which the products read as they are)
+#pragma unroll
+  for (int g = 0; g < 2; ++g)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) asm("" : "+a"(qf[g][ks]));
   // (uniform) tiles that some row of the wave sees, and those from which on some row does not see all
   const int last = min(wrow + 63, rows - 1);
   const int my_end = min(sq.L + (int)div_by((uint32_t)last, a.group) + 1, hi_row);
@@ -97,7 +92,7 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a
               div_by((uint32_t)(hi_row - 1), a.b.page) + 1u};
   const bool in_page = a.b.page.d % 16 == 0;  // a wave's 16 rows of a tile lie in one page
   int produced = 0;
-  auto produce = [&]() {
+  auto produce = [&]() __attribute__((always_inline)) {
     const int t0 = lo + produced * kTile + wave * 16, slot = produced % S;
     const uint32_t dst = lds0 + (uint32_t)(slot * G::kSlot + wave * 16 * D * 2);
     const uint32_t pa = div_by((uint32_t)min(t0, hi_row - 1), a.b.page);
@@ -109,7 +104,7 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a
     ++produced;
   };
   // Tiles up to t have landed for every wave (t < produced).
-  auto landed = [&](int t) {
+  auto landed = [&](int t) __attribute__((always_inline)) {
     const int newer = produced - 1 - t;
     if (newer >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * NR) : "memory");
     else if (newer == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NR) : "memory");
@@ -123,79 +118,105 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a
   r[0].init();
   r[1].init();
   f32x16 s[2];
-  u32x4 p[2][2], kf[2][KS], vf[2][DB][2];
+  u32x4 p[2][2], kf[KS], vf[DB][2];
   landed(0);
   if (my_nt > 0) {
-    read_k<D>(smem, lane, kf[1]);
-    read_v<D>(smem + G::kHalf, lane, vf[0]);
+    read_k<D>(smem, lane, kf);
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       s[g] = f32x16{};
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s[g] = mma32(kf[1][ks], qf[g][ks], s[g]);
+      for (int ks = 0; ks < KS; ++ks) s[g] = mma32(kf[ks], qf[g][ks], s[g]);
       mask_scores(s[g], lo, end[g], lane);
     }
-    read_k<D>(smem + 32 * D * 2, lane, kf[0]);
+    read_k<D>(smem + 32 * D * 2, lane, kf);
     settle(r[0], s[0], a.scale_log2, p[0], weights(s[0], a.scale_log2, r[0].m, p[0]));
   }
 
-  // 32 keys: substep u of tile j.  kf[u] holds the next substep's K fragments, vf[u] this one's V fragments.
-  auto substep = [&](auto masked_c, auto u_c, int j) {
+  // 32 keys from key0: V rows at v_cur; kf holds the next 32 keys' K fragments, k_next are those after them.
+  auto substep = [&](auto masked_c, const unsigned char* v_cur, const unsigned char* k_next, int key0) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked_c)::value;
-    constexpr int U = decltype(u_c)::value;
-    const unsigned char* t_cur = smem + (j % S) * G::kSlot;
-    const unsigned char* t_next = smem + ((j + 1) % S) * G::kSlot;
-    const int key0 = lo + j * kTile + 32 * U;
-    bool odd = false;
-    if constexpr (MASKED) odd = take_out_not_finite<D>(vf[U]);
     // phase A
     s[0] = f32x16{};
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) s[0] = mma32(kf[U][ks], qf[0][ks], s[0]);
+    for (int ks = 0; ks < KS; ++ks) s[0] = mma32(kf[ks], qf[0][ks], s[0]);
+    read_v<D>(v_cur, lane, vf);
+    bool odd = false;
+    if constexpr (MASKED) odd = take_out_not_finite<D>(vf);
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+    for (int k2 = 0; k2 < 2; ++k2)
 #pragma unroll
-      for (int k2 = 0; k2 < 2; ++k2) r[0].o[db] = mma32(vf[U][db][k2], p[0][k2], r[0].o[db]);
+      for (int db = 0; db < DB; ++db) r[0].o[db] = mma32(vf[db][k2], p[0][k2], r[0].o[db]);
     const float sum1 = weights(s[1], a.scale_log2, r[1].m, p[1]);
-    read_k<D>(t_next + (U ? 32 * D * 2 : 0), lane, kf[1 - U]);
-    interleave();
+    if constexpr (!MASKED) {
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);            // matrix product
+        __builtin_amdgcn_sched_group_barrier(0x100, 4 * DB / KS, 0);  // LDS reads
+        __builtin_amdgcn_sched_group_barrier(0x402, 48 / (KS + 2 * DB), 0);  // vector instructions
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * DB; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, 48 / (KS + 2 * DB), 0);
+      }
+    }
     settle(r[1], s[1], a.scale_log2, p[1], sum1);
     // phase B
     if constexpr (MASKED) mask_scores(s[0], key0 + 32, end[0], lane);
     s[1] = f32x16{};
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) s[1] = mma32(kf[U][ks], qf[1][ks], s[1]);
+    for (int ks = 0; ks < KS; ++ks) s[1] = mma32(kf[ks], qf[1][ks], s[1]);
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+    for (int k2 = 0; k2 < 2; ++k2)
 #pragma unroll
-      for (int k2 = 0; k2 < 2; ++k2) r[1].o[db] = mma32(vf[U][db][k2], p[1][k2], r[1].o[db]);
+      for (int db = 0; db < DB; ++db) r[1].o[db] = mma32(vf[db][k2], p[1][k2], r[1].o[db]);
     const float sum0 = weights(s[0], a.scale_log2, r[0].m, p[0]);
-    read_v<D>((U ? t_next : t_cur + 32 * D * 2) + G::kHalf, lane, vf[1 - U]);
-    interleave();
+    read_k<D>(k_next, lane, kf);
+    if constexpr (!MASKED) {
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, 48 / (KS + 2 * DB), 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * DB; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, KS / (2 * DB), 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, 48 / (KS + 2 * DB), 0);
+      }
+    }
     if constexpr (MASKED) {
       mask_scores(s[1], key0 + 32, end[1], lane);
-      if (odd) add_not_finite<D, 2>(r, t_cur + G::kHalf + 32 * U * D * 2, key0, end, lane);
+      if (odd) add_not_finite<D, 2>(r, v_cur, key0, end, lane);
     }
     settle(r[0], s[0], a.scale_log2, p[0], sum0);
   };
-  using No = std::integral_constant<bool, false>;
-  using Yes = std::integral_constant<bool, true>;
-  using I0 = std::integral_constant<int, 0>;
-  using I1 = std::integral_constant<int, 1>;
-
-#pragma unroll 1
-  for (int j = 0; j < nt; ++j) {
-    landed(min(j + 1, nt - 1));  // (and every wave is done with tile j - 1, whose slot is filled again)
+  auto tile = [&](auto masked_c, int j) __attribute__((always_inline)) {
+    const unsigned char* t_cur = smem + (j % S) * G::kSlot;
+    const unsigned char* t_next = smem + ((j + 1) % S) * G::kSlot;
+    substep(masked_c, t_cur + G::kHalf, t_next, lo + j * kTile);
+    substep(masked_c, t_cur + G::kHalf + 32 * D * 2, t_next + 32 * D * 2, lo + j * kTile + 32);
+  };
+  // Tile j + 1 has landed, and every wave is done with tile j - 1, whose slot is filled again.
+  auto begin = [&](int j) __attribute__((always_inline)) {
+    landed(min(j + 1, nt - 1));
     if (produced < nt) produce();
-    if (j >= my_nt) continue;
-    if (j + 2 <= unmasked) {     // (the next tile's scores are taken, too)
-      substep(No{}, I0{}, j);
-      substep(No{}, I1{}, j);
-    } else {
-      substep(Yes{}, I0{}, j);
-      substep(Yes{}, I1{}, j);
-    }
+  };
+  // (a tile takes the next one's scores, too; every wave passes nt barriers)
+  int j = 0;
+#pragma unroll 1
+  for (; j + 2 <= unmasked && j < my_nt; ++j) {
+    begin(j);
+    tile(std::integral_constant<bool, false>{}, j);
   }
+#pragma unroll 1
+  for (; j < my_nt; ++j) {
+    begin(j);
+    tile(std::integral_constant<bool, true>{}, j);
+  }
+#pragma unroll 1
+  for (; j < nt; ++j) begin(j);
 #pragma unroll
   for (int g = 0; g < 2; ++g)
     store_rows<D>(r[g], a, whole, it.split, tok[g], head[g], wrow + g * 32 + r32 < rows, lane);

@@ -133,59 +133,54 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a
     settle(r[0], s[0], a.scale_log2, p[0], weights(s[0], a.scale_log2, r[0].m, p[0]));
   }
 
+  // A phase: the scores `to` of 32 keys (kf) and O += V^T P of a group, beside the other group's weights `w` of scores
+  // `from`.  Each product is followed by its share of the vector instructions, in this order: the scheduler
+  // would put them together.
+  auto phase = [&](auto masked_c, f32x16& to, const u32x4(&q)[KS], Rows<D>& rows_, const u32x4(&pv)[2], const f32x16& from, float m,
+                   u32x4(&w)[2], auto load) __attribute__((always_inline)) {
+    constexpr int N = KS + 2 * DB;  // products
+    float x[16], sum = 0.f;
+    const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+    auto slice = [&](int n) __attribute__((always_inline)) {  // step n of 18: score n's exponent and exponential, pair n - 2
+      if (n < 16) x[n] = __builtin_fmaf(from[n], a.scale_log2, -m);
+      if (n >= 1 && n < 17) x[n - 1] = __builtin_amdgcn_exp2f(x[n - 1]);
+      if (n >= 3 && n % 2 == 1) {
+        const bf16x2 h = __builtin_convertvector(f32x2{x[n - 3], x[n - 2]}, bf16x2);
+        const int pair = (n - 3) / 2;
+        sum = __builtin_amdgcn_fdot2_f32_bf16(h, ones, sum, false);
+        w[pair / 4][pair % 4] = __builtin_bit_cast(uint32_t, h);
+      }
+    };
+    int done = 0;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if (n < KS) {
+        to = mma32(kf[n], q[n], n == 0 ? f32x16{} : to);
+      } else {
+        const int k2 = (n - KS) / DB, db = (n - KS) % DB;
+        rows_.o[db] = mma32(vf[db][k2], pv[k2], rows_.o[db]);
+      }
+      load(n);
+#pragma unroll
+      for (; done < (n + 1) * 18 / N; ++done) slice(done);
+      if constexpr (!decltype(masked_c)::value) __builtin_amdgcn_sched_barrier(0);
+    }
+    return sum;
+  };
   // 32 keys from key0: V rows at v_cur; kf holds the next 32 keys' K fragments, k_next are those after them.
   auto substep = [&](auto masked_c, const unsigned char* v_cur, const unsigned char* k_next, int key0) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked_c)::value;
     // phase A
-    s[0] = f32x16{};
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) s[0] = mma32(kf[ks], qf[0][ks], s[0]);
     read_v<D>(v_cur, lane, vf);
     bool odd = false;
     if constexpr (MASKED) odd = take_out_not_finite<D>(vf);
-#pragma unroll
-    for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-      for (int db = 0; db < DB; ++db) r[0].o[db] = mma32(vf[db][k2], p[0][k2], r[0].o[db]);
-    const float sum1 = weights(s[1], a.scale_log2, r[1].m, p[1]);
-    if constexpr (!MASKED) {
-#pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);            // matrix product
-        __builtin_amdgcn_sched_group_barrier(0x100, 4 * DB / KS, 0);  // LDS reads
-        __builtin_amdgcn_sched_group_barrier(0x402, 48 / (KS + 2 * DB), 0);  // vector instructions
-      }
-#pragma unroll
-      for (int i = 0; i < 2 * DB; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x402, 48 / (KS + 2 * DB), 0);
-      }
-    }
+    const float sum1 = phase(masked_c, s[0], qf[0], r[0], p[0], s[1], r[1].m, p[1], [&](int) {});
     settle(r[1], s[1], a.scale_log2, p[1], sum1);
     // phase B
     if constexpr (MASKED) mask_scores(s[0], key0 + 32, end[0], lane);
-    s[1] = f32x16{};
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) s[1] = mma32(kf[ks], qf[1][ks], s[1]);
-#pragma unroll
-    for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-      for (int db = 0; db < DB; ++db) r[1].o[db] = mma32(vf[db][k2], p[1][k2], r[1].o[db]);
-    const float sum0 = weights(s[0], a.scale_log2, r[0].m, p[0]);
-    read_k<D>(k_next, lane, kf);
-    if constexpr (!MASKED) {
-#pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x402, 48 / (KS + 2 * DB), 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 2 * DB; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, KS / (2 * DB), 0);
-        __builtin_amdgcn_sched_group_barrier(0x402, 48 / (KS + 2 * DB), 0);
-      }
-    }
+    const float sum0 = phase(masked_c, s[1], qf[1], r[1], p[1], s[0], r[0].m, p[0], [&](int x) {
+      if (x >= KS && x - KS < KS) kf[x - KS] = read_k1<D>(k_next, lane, x - KS);
+    });
     if constexpr (MASKED) {
       mask_scores(s[1], key0 + 32, end[1], lane);
       if (odd) add_not_finite<D, 2>(r, v_cur, key0, end, lane);

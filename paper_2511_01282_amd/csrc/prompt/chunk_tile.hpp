@@ -131,12 +131,14 @@ struct RowFeed {
 
 // K fragments of 32 keys (A operand: lane l holds key l & 31).
 template <int D>
-__device__ __forceinline__ void read_k(const unsigned char* tile, int lane, u32x4 (&kf)[D / 16]) {
+__device__ __forceinline__ u32x4 read_k1(const unsigned char* tile, int lane, int ks) {
   const int r32 = lane & 31, hi = lane >> 5;
-  const unsigned char* kr = tile + r32 * D * 2;
+  return *reinterpret_cast<const u32x4*>(tile + r32 * D * 2 + (((2 * ks + hi) ^ k_chunk<D>(r32)) << 4));
+}
+template <int D>
+__device__ __forceinline__ void read_k(const unsigned char* tile, int lane, u32x4 (&kf)[D / 16]) {
 #pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks)
-    kf[ks] = *reinterpret_cast<const u32x4*>(kr + (((2 * ks + hi) ^ k_chunk<D>(r32)) << 4));
+  for (int ks = 0; ks < D / 16; ++ks) kf[ks] = read_k1<D>(tile, lane, ks);
 }
 
 // V^T fragments of 32 keys (A operand: lane l holds column 32 db + (l & 31), keys 16 k2 + {0..3, 8..11} + 4 (l / 32)),

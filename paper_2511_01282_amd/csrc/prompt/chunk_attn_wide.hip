@@ -171,15 +171,19 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a
   auto substep = [&](auto masked_c, const unsigned char* v_cur, const unsigned char* k_next, int key0) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked_c)::value;
     // phase A
-    read_v<D>(v_cur, lane, vf);
     bool odd = false;
-    if constexpr (MASKED) odd = take_out_not_finite<D>(vf);
-    const float sum1 = phase(masked_c, s[0], qf[0], r[0], p[0], s[1], r[1].m, p[1], [&](int) {});
+    if constexpr (MASKED) {
+      read_v<D>(v_cur, lane, vf);
+      odd = take_out_not_finite<D>(vf);
+    }
+    const float sum1 = phase(masked_c, s[0], qf[0], r[0], p[0], s[1], r[1].m, p[1], [&](int n) __attribute__((always_inline)) {
+      if (!MASKED && n < 2 * DB) vf[n % DB][n / DB] = read_v1<D>(v_cur, lane, n % DB, n / DB);
+    });
     settle(r[1], s[1], a.scale_log2, p[1], sum1);
     // phase B
     if constexpr (MASKED) mask_scores(s[0], key0 + 32, end[0], lane);
-    const float sum0 = phase(masked_c, s[1], qf[1], r[1], p[1], s[0], r[0].m, p[0], [&](int x) {
-      if (x >= KS && x - KS < KS) kf[x - KS] = read_k1<D>(k_next, lane, x - KS);
+    const float sum0 = phase(masked_c, s[1], qf[1], r[1], p[1], s[0], r[0].m, p[0], [&](int n) __attribute__((always_inline)) {
+      if (n >= KS) kf[n - KS] = read_k1<D>(k_next, lane, n - KS);
     });
     if constexpr (MASKED) {
       mask_scores(s[1], key0 + 32, end[1], lane);

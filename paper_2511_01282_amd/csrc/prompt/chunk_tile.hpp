@@ -145,24 +145,22 @@ __device__ __forceinline__ void read_k(const unsigned char* tile, int lane, u32x
 // by transposing reads: lane j of a 16-lane group addresses row + j / 4, columns 4 (j % 4) .. and receives column j
 // of the four rows.
 template <int D>
-__device__ __forceinline__ void read_v(const unsigned char* tile, int lane, u32x4 (&vf)[D / 32][2]) {
+__device__ __forceinline__ u32x4 read_v1(const unsigned char* tile, int lane, int db, int k2) {
   typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
   const int lr = lane & 15, dh = (lane >> 4) & 1, hi = lane >> 5;
   const int r = 4 * hi + lr / 4;  // (rows + 8 and + 16 share the permutation)
-  const unsigned char* vr = tile + r * D * 2;
+  const int col = 32 * db + 16 * dh + 4 * (lr % 4);
+  const unsigned char* p = tile + r * D * 2 + ((col >> 3) ^ v_chunk<D>(r)) * 16 + (col & 7) * 2 + 16 * k2 * D * 2;
+  const u32x2 h0 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p));
+  const u32x2 h1 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + 8 * D * 2)));
+  return u32x4{h0.x, h0.y, h1.x, h1.y};
+}
+template <int D>
+__device__ __forceinline__ void read_v(const unsigned char* tile, int lane, u32x4 (&vf)[D / 32][2]) {
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db) {
-    const int col = 32 * db + 16 * dh + 4 * (lr % 4);
-    const unsigned char* p = vr + ((col >> 3) ^ v_chunk<D>(r)) * 16 + (col & 7) * 2;
+  for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int k2 = 0; k2 < 2; ++k2) {
-      const u32x2 h0 =
-          __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + (16 * k2) * D * 2)));
-      const u32x2 h1 =
-          __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + (16 * k2 + 8) * D * 2)));
-      vf[db][k2] = u32x4{h0.x, h0.y, h1.x, h1.y};
-    }
-  }
+    for (int k2 = 0; k2 < 2; ++k2) vf[db][k2] = read_v1<D>(tile, lane, db, k2);
 }
 
 // 32 query rows of a wave (lane l: row l & 31; both halves of the wave hold half of its keys and columns).

@@ -92,16 +92,31 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a
               div_by((uint32_t)(hi_row - 1), a.b.page) + 1u};
   const bool in_page = a.b.page.d % 16 == 0;  // a wave's 16 rows of a tile lie in one page
   int produced = 0;
-  auto produce = [&]() __attribute__((always_inline)) {
-    const int t0 = lo + produced * kTile + wave * 16, slot = produced % S;
-    const uint32_t dst = lds0 + (uint32_t)(slot * G::kSlot + wave * 16 * D * 2);
-    const uint32_t pa = div_by((uint32_t)min(t0, hi_row - 1), a.b.page);
-    ids.need(pa, div_by((uint32_t)min(t0 + 15, hi_row - 1), a.b.page), lane);
-    if (in_page && t0 + 16 <= hi_row)
-      feed.from_page(a.b, dst, dst + G::kHalf, ids.uniform(pa), (uint32_t)t0 - pa * a.b.page.d);
-    else
-      feed.from_rows(a.b, dst, dst + G::kHalf, ids.ids, ids.p0, t0, hi_row, lane);
+  // The next tile's requests: `fast`, and from where to where, if the wave's rows lie whole in one page; requested
+  // as a tile's products go on.  Other tiles are requested at once.
+  bool fast = false;
+  uint64_t next_k = 0, next_v = 0;
+  uint32_t next_dst = 0;
+  int next_id = 0;  // page of the wave's first row of the next tile, read ahead where the window holds it
+  auto prepare = [&]() __attribute__((always_inline)) {
+    const int t0 = lo + produced * kTile + wave * 16;
+    next_dst = lds0 + (uint32_t)((produced % S) * G::kSlot + wave * 16 * D * 2);
     ++produced;
+    const uint32_t pa = div_by((uint32_t)min(t0, hi_row - 1), a.b.page);
+    fast = in_page && t0 + 16 <= hi_row && pa < ids.p1;
+    if (fast) {
+      const int64_t off = feed.page_offset(a.b, __builtin_amdgcn_readfirstlane(next_id), (uint32_t)t0 - pa * a.b.page.d);
+      next_k = (uint64_t)(feed.k + off);
+      next_v = (uint64_t)(feed.v + off);
+    } else {
+      ids.need(pa, div_by((uint32_t)min(t0 + 15, hi_row - 1), a.b.page), lane);
+      feed.from_rows(a.b, next_dst, next_dst + G::kHalf, ids.ids, ids.p0, t0, hi_row, lane);
+    }
+    const uint32_t pn = div_by((uint32_t)min(t0 + kTile, hi_row - 1), a.b.page);
+    if (pn < ids.p1) next_id = ids.ids[pn - ids.p0];
+  };
+  auto request = [&](bool v) __attribute__((always_inline)) {
+    if (fast) dma_rows<NR>(v ? next_dst + G::kHalf : next_dst, v ? next_v : next_k, v ? feed.v_off : feed.k_off);
   };
   // Tiles up to t have landed for every wave (t < produced).
   auto landed = [&](int t) __attribute__((always_inline)) {
@@ -109,9 +124,14 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a
     if (newer >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * NR) : "memory");
     else if (newer == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NR) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    // (what a wave has read of the slots it is done with it has used in products, so nothing of them is under way)
+    asm volatile("s_barrier" ::: "memory");
   };
-  for (int t = 0; t < min(nt, S - 1); ++t) produce();
+  for (int t = 0; t < min(nt, S - 1); ++t) {
+    prepare();
+    request(false);
+    request(true);
+  }
 
   // ---- rows' state; the first tile's scores ----
   Rows<D> r[2];
@@ -162,14 +182,15 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a
       }
       load(n);
 #pragma unroll
-      for (; done < (n + 1) * 18 / N; ++done) slice(done);
+      for (; done < min(18, ((n + 1) * 18 + N - 3) / (N - 2)); ++done) slice(done);
       if constexpr (!decltype(masked_c)::value) __builtin_amdgcn_sched_barrier(0);
     }
     return sum;
   };
   // 32 keys from key0: V rows at v_cur; kf holds the next 32 keys' K fragments, k_next are those after them.
-  auto substep = [&](auto masked_c, const unsigned char* v_cur, const unsigned char* k_next, int key0) __attribute__((always_inline)) {
+  auto substep = [&](auto masked_c, auto u_c, const unsigned char* v_cur, const unsigned char* k_next, int key0) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked_c)::value;
+    constexpr int U = decltype(u_c)::value;
     // phase A
     bool odd = false;
     if constexpr (MASKED) {
@@ -178,6 +199,7 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a
     }
     const float sum1 = phase(masked_c, s[0], qf[0], r[0], p[0], s[1], r[1].m, p[1], [&](int n) __attribute__((always_inline)) {
       if (!MASKED && n < 2 * DB) vf[n % DB][n / DB] = read_v1<D>(v_cur, lane, n % DB, n / DB);
+      if (U == 0 && (n == 1 || n == KS)) request(n > 1);
     });
     settle(r[1], s[1], a.scale_log2, p[1], sum1);
     // phase B
@@ -194,13 +216,14 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a
   auto tile = [&](auto masked_c, int j) __attribute__((always_inline)) {
     const unsigned char* t_cur = smem + (j % S) * G::kSlot;
     const unsigned char* t_next = smem + ((j + 1) % S) * G::kSlot;
-    substep(masked_c, t_cur + G::kHalf, t_next, lo + j * kTile);
-    substep(masked_c, t_cur + G::kHalf + 32 * D * 2, t_next + 32 * D * 2, lo + j * kTile + 32);
+    substep(masked_c, std::integral_constant<int, 0>{}, t_cur + G::kHalf, t_next, lo + j * kTile);
+    substep(masked_c, std::integral_constant<int, 1>{}, t_cur + G::kHalf + 32 * D * 2, t_next + 32 * D * 2, lo + j * kTile + 32);
   };
   // Tile j + 1 has landed, and every wave is done with tile j - 1, whose slot is filled again.
   auto begin = [&](int j) __attribute__((always_inline)) {
     landed(min(j + 1, nt - 1));
-    if (produced < nt) produce();
+    fast = false;
+    if (produced < nt) prepare();
   };
   // (a tile takes the next one's scores, too; every wave passes nt barriers)
   int j = 0;
@@ -215,7 +238,11 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a
     tile(std::integral_constant<bool, true>{}, j);
   }
 #pragma unroll 1
-  for (; j < nt; ++j) begin(j);
+  for (; j < nt; ++j) {
+    begin(j);
+    request(false);
+    request(true);
+  }
 #pragma unroll
   for (int g = 0; g < 2; ++g)
     store_rows<D>(r[g], a, whole, it.split, tok[g], head[g], wrow + g * 32 + r32 < rows, lane);

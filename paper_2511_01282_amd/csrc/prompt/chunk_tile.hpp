@@ -106,10 +106,14 @@ struct RowFeed {
       v_off[q] = row + (uint32_t)((pos ^ v_chunk<D>(r)) * 16);
     }
   }
-  // All R rows in page `id` (uniform), the first at row `at` of it.
-  __device__ __forceinline__ void from_page(const ChunkBatch& c, uint32_t k_dst, uint32_t v_dst, int id, uint32_t at) const {
+  // Offset from k and v of R rows in page `id` (uniform), the first at row `at` of it, for dma_rows with k_off and v_off.
+  __device__ __forceinline__ int64_t page_offset(const ChunkBatch& c, int id, uint32_t at) const {
     const int64_t page = (uint32_t)id < (uint32_t)c.n_pages ? id : 0;
-    const int64_t off = page * c.page_stride + (int64_t)((uint64_t)at * c.row_stride) - 1024 * (NR - 1);
+    return page * c.page_stride + (int64_t)((uint64_t)at * c.row_stride) - 1024 * (NR - 1);
+  }
+  // Such rows.
+  __device__ __forceinline__ void from_page(const ChunkBatch& c, uint32_t k_dst, uint32_t v_dst, int id, uint32_t at) const {
+    const int64_t off = page_offset(c, id, at);
     dma_rows<NR>(k_dst, (uint64_t)(k + off), k_off);
     dma_rows<NR>(v_dst, (uint64_t)(v + off), v_off);
   }

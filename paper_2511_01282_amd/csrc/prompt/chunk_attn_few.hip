@@ -18,6 +18,7 @@ struct FewShape {
   static constexpr int kHalf = kTile * D * 2;      // bytes of a K or V tile
   static constexpr int kSlot = 2 * kHalf;
   static constexpr int kWave = S * kSlot;
+  static constexpr int kPageIds = 1024;            // page ids of a wave's window
   static constexpr int kIds = 4 * kWave;
   static constexpr int kMl = kIds + 4 * kPageIds * 4;
   static constexpr int kLds = kMl + 4 * 64 * 8;
@@ -61,7 +62,7 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_few_kernel(ChunkAttnArgs a,
 
   Feed feed;
   feed.init(a.b, it.g, lane);
-  PageIds ids{reinterpret_cast<int32_t*>(smem + G::kIds) + wave * kPageIds, a.b.table + (int64_t)it.b * a.b.table_stride, 0u, 0u,
+  PageIds<G::kPageIds> ids{reinterpret_cast<int32_t*>(smem + G::kIds) + wave * G::kPageIds, a.b.table + (int64_t)it.b * a.b.table_stride, 0u, 0u,
               div_by((uint32_t)(hi_row - 1), a.b.page) + 1u};
   const bool in_page = a.b.page.d % 16 == 0;  // 16 rows from a multiple of 16 lie in one page
   int produced = 0;

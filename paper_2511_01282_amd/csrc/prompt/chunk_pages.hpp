@@ -5,19 +5,18 @@
 
 namespace respec {
 
-constexpr int kPageIds = 1024;  // ids per wave
-
+template <int N>  // ids that it holds
 struct PageIds {
   int32_t* ids;          // LDS, the wave's own
   const int32_t* table;  // the sequence's row of the page table
   uint32_t p0, p1;       // ids[0] is page p0's; ids of pages p0 .. p1 - 1 are there
   uint32_t end;          // pages of the sequence's rows that this workgroup reads end here
 
-  // Make the ids of pages a .. b (b - a < kPageIds, a no less than before) available.
+  // Make the ids of pages a .. b (b - a < N, a no less than before) available.
   __device__ __forceinline__ void need(uint32_t a, uint32_t b, int lane) {
     if (b < p1) return;
     p0 = a;
-    p1 = min(a + (uint32_t)kPageIds, end);
+    p1 = min(a + (uint32_t)N, end);
     wave_lds_sync();
     for (uint32_t p = p0 + lane; p < p1; p += 64) ids[p - p0] = table[p];
     wave_lds_sync();

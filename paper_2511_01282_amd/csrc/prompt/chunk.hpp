@@ -72,15 +72,54 @@ __device__ __forceinline__ void report_status(const ChunkBatch& c, int b, bool f
   if (threadIdx.x == 0) c.status[b] = s.status ? s.status : (bad ? kStPage : 0);
 }
 
-// A workgroup's item: the pairs of sequence and KV head follow one another (a pair's workgroups meet on
-// one XCD where the pairs are a multiple of 8, and read its tiles at about the same time), then the splits,
-// then the row blocks, the longest first.
+// A workgroup's item.  Item x is of KV head x % Hkv (a head's workgroups meet on one XCD where the heads are a
+// multiple of 8, and read its tiles at about the same time) and entry x / Hkv of the list of (sequence, split, row
+// block), a block's rows descending: the longest first.  A sequence of `rows` query rows from `least` to `most`
+// has its row blocks times its splits of entries; the grid holds as many as any lengths within the call's bounds
+// need, and those past the list's end find nothing (n = 0).
 struct Item {
   int split, g, rb, b;
+  ChunkSeq seq;
 };
-__device__ __forceinline__ Item item_of(const ChunkBatch& c, const ChunkGeom& ge, int x) {
-  const int pairs = c.n_kv_heads * c.batch, pair = x % pairs, y = x / pairs;
-  return Item{y % ge.nsplit, pair % c.n_kv_heads, ge.n_rowblk - 1 - y / ge.nsplit, pair / c.n_kv_heads};
+__device__ __forceinline__ Item find_item(const ChunkBatch& c, const ChunkGeom& ge, int least, int most, int x) {
+  const int lane = (int)(threadIdx.x & 63);
+  Item it{0, x % c.n_kv_heads, 0, 0, ChunkSeq{0, 0, 0, 0}};
+  int y = x / c.n_kv_heads;
+  for (int b0 = 0; b0 < c.batch; b0 += 64) {
+    ChunkSeq s{0, 0, 0, 0};
+    int blocks = 0, splits = 1;
+    if (b0 + lane < c.batch) {
+      s = chunk_seq(c, b0 + lane);
+      const int rows = s.n * c.group;
+      if (rows >= least && rows <= most) {
+        blocks = (rows - 1) / ge.rows_per_wg + 1;
+        splits = (s.L + s.n - 1) / ge.split_rows + 1;
+      }
+    }
+    // (a lane's entries: at most n_rowblk * nsplit; 64 lanes' fit 32 bits, as the grid does)
+    int incl = blocks * splits;
+    if (c.batch > 1) {
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int z = __shfl_up(incl, o, 64);
+        incl += lane >= o ? z : 0;
+      }
+    }
+    const uint64_t past = __ballot(y < incl);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      blocks = __builtin_amdgcn_readlane(blocks, l);
+      y -= __builtin_amdgcn_readlane(incl, l) - blocks * __builtin_amdgcn_readlane(splits, l);
+      it.b = b0 + l;
+      it.split = y / blocks;
+      it.rb = blocks - 1 - (y - it.split * blocks);
+      it.seq = ChunkSeq{__builtin_amdgcn_readlane(s.t0, l), __builtin_amdgcn_readlane(s.n, l),
+                        __builtin_amdgcn_readlane(s.L, l), 0};
+      return it;
+    }
+    y -= __builtin_amdgcn_readlane(incl, 63);
+  }
+  return it;
 }
 
 // Cache rows that the rows of block rb see (at least one).

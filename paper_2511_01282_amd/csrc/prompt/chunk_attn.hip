@@ -12,7 +12,7 @@ namespace respec {
 namespace {
 
 template <int D>
-__global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a, int items) {
+__global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
   constexpr int ES = 4;
   constexpr int KC = D * ES / 64;      // 64-byte K-chunks of a head row
   constexpr int DB = D / 16;
@@ -21,20 +21,20 @@ __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a, in
   constexpr int CPR = D * ES / 16;
   __shared__ __align__(16) unsigned char ks[TK * PITCH], vs[TK * PITCH];
 
-  if ((int)blockIdx.x >= items) {
-    report_status<256>(a.b, (int)blockIdx.x - items, true);
+  if ((int)blockIdx.x >= a.wide.items) {
+    report_status<256>(a.b, (int)blockIdx.x - a.wide.items, true);
     return;
   }
   const ChunkGeom& ge = a.wide;
-  const Item it = item_of(a.b, ge, blockIdx.x);
-  const ChunkSeq sq = chunk_seq(a.b, it.b);
+  const Item it = find_item(a.b, ge, 1, INT32_MAX, blockIdx.x);
+  const ChunkSeq& sq = it.seq;
+  if (sq.n == 0) return;
   const int rows = sq.n * a.b.group, row0 = it.rb * ge.rows_per_wg;
-  if (row0 >= rows) return;
   const int limit = block_limit(a, ge, sq, it.rb);
   const int lo = it.split * ge.split_rows;
   if (lo >= limit) return;
   const bool whole = limit <= ge.split_rows;   // the block's only split
-  const int hi = ge.nsplit == 1 ? limit : min(limit, lo + ge.split_rows);
+  const int hi = whole ? limit : min(limit, lo + ge.split_rows);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c16 = lane & 15, g4 = lane >> 4;
   const int row = row0 + wave * 16 + c16, rowc = min(row, rows - 1);
@@ -159,55 +159,86 @@ __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a, in
   }
 }
 
-// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over a row's splits, M = max_s m_s.  A
-// workgroup takes the heads of one token, a wave per head; blocks with one split are written already.
-template <typename T, int D>
+// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over a row's splits, M = max_s m_s.  A row (token
+// and head) is joined by WPR waves, each a part of its splits, eight at a time; rows of one split are
+// written already.
+template <typename T, int D, int WPR>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkAttnArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int E = D / 64, RPW = 4 / WPR;  // columns per lane, rows per workgroup
+  __shared__ float part[4][D];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % WPR;
   int b;
   const ChunkSeq sq = seq_of_token(a.b, blockIdx.x, b);
-  if (sq.n == 0) return;
+  const int hq = a.b.n_kv_heads * a.b.group, h = (int)blockIdx.y * RPW + wave / WPR;
   const ChunkGeom& ge = sq.n * a.b.group <= a.few_rows ? a.few : a.wide;
-  const int hq = a.b.n_kv_heads * a.b.group, i = (int)blockIdx.x - sq.t0;
-  for (int h = blockIdx.y * 4 + wave; h < hq; h += gridDim.y * 4) {
-    const int hh = h - (int)div_by((uint32_t)h, a.group) * a.b.group;
+  int ns = 0;
+  if (sq.n > 0 && h < hq) {
+    const int hh = h - (int)div_by((uint32_t)h, a.group) * a.b.group, i = (int)blockIdx.x - sq.t0;
     const int limit = block_limit(a, ge, sq, (i * a.b.group + hh) / ge.rows_per_wg);
-    const int ns = (limit + ge.split_rows - 1) / ge.split_rows;  // (at most 64)
-    if (ns <= 1) continue;
-    const int64_t step = (int64_t)a.b.total_new * hq, pr = (int64_t)blockIdx.x * hq + h;
-    const float ms = lane < ns ? a.part_m[lane * step + pr] : kNegInf;
-    const float M = wave_max(ms);
-    float w = ms == kNegInf ? 0.f : exp2f(ms - M);
-    const float lt = wave_sum(lane < ns ? w * a.part_l[lane * step + pr] : 0.f);
-    w /= lt;
-    float acc[D / 64];
-#pragma unroll
-    for (int e = 0; e < D / 64; ++e) acc[e] = 0.f;
-    for (int s = 0; s < ns; ++s) {
-      const float ws = __shfl(w, s, 64);
-#pragma unroll
-      for (int e = 0; e < D / 64; ++e) acc[e] += ws * a.part_o[(s * step + pr) * D + lane * (D / 64) + e];
-    }
-    char* to = a.out + (int64_t)blockIdx.x * a.o_tok + (int64_t)h * a.o_head;
-#pragma unroll
-    for (int e = 0; e < D / 64; ++e) Elem<T>::store(to, lane * (D / 64) + e, acc[e]);
+    ns = (limit - 1) / ge.split_rows + 1;  // (at most 64)
   }
+  if (WPR == 1 && ns <= 1) return;
+  float acc[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.f;
+  if (ns > 1) {
+    const int64_t step = (int64_t)a.b.total_new * hq, pr = (int64_t)blockIdx.x * hq + h;
+    const float ms = lane < ns ? a.part_m[lane * step + pr] : kNegInf, ls = lane < ns ? a.part_l[lane * step + pr] : 0.f;
+    const float M = wave_max(ms);
+    float wt = ms == kNegInf ? 0.f : exp2f(ms - M);
+    const float lt = wave_sum(wt * ls);
+    wt /= lt;
+    const float* o = a.part_o + pr * D + lane * E;
+    for (int s0 = w * 8; s0 < ns; s0 += WPR * 8) {
+      float x[8][E];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float* q = o + min(s0 + u, ns - 1) * step * D;
+        if constexpr (E == 2) *reinterpret_cast<float2*>(x[u]) = *reinterpret_cast<const float2*>(q);
+        else x[u][0] = *q;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float ws = __shfl(wt, min(s0 + u, 63), 64);
+        if (s0 + u < ns) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[e] += ws * x[u][e];
+        }
+      }
+    }
+  }
+  if constexpr (WPR > 1) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) part[wave][lane * E + e] = acc[e];
+    __syncthreads();
+    if (w != 0 || ns <= 1) return;
+#pragma unroll
+    for (int x = 1; x < WPR; ++x)
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += part[wave + x][lane * E + e];
+  }
+  char* to = a.out + (int64_t)blockIdx.x * a.o_tok + (int64_t)h * a.o_head;
+#pragma unroll
+  for (int e = 0; e < E; ++e) Elem<T>::store(to, lane * E + e, acc[e]);
 }
 
 template <typename T, int D>
 hipError_t go_merge(const ChunkAttnArgs& a, hipStream_t s) {
   const int hq = a.b.n_kv_heads * a.b.group;
-  hipLaunchKernelGGL((chunk_merge_kernel<T, D>), dim3(a.b.total_new, (hq + 3) / 4), dim3(256), 0, s, a);
+  // many splits: a row's are read by four waves at once
+  if (max(a.few.nsplit, a.wide.nsplit) > 16)
+    hipLaunchKernelGGL((chunk_merge_kernel<T, D, 4>), dim3(a.b.total_new, hq), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((chunk_merge_kernel<T, D, 1>), dim3(a.b.total_new, (hq + 3) / 4), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_chunk_attn_f32(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s) {
-  const int items = (int)item_count(a.b, a.wide);
-  const dim3 grid(items + (status ? a.b.batch : 0));
-  if (head_dim == 128) hipLaunchKernelGGL(chunk_attn_f32_kernel<128>, grid, dim3(256), 0, s, a, items);
-  else hipLaunchKernelGGL(chunk_attn_f32_kernel<64>, grid, dim3(256), 0, s, a, items);
+  const dim3 grid(a.wide.items + (status ? a.b.batch : 0));
+  if (head_dim == 128) hipLaunchKernelGGL(chunk_attn_f32_kernel<128>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(chunk_attn_f32_kernel<64>, grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

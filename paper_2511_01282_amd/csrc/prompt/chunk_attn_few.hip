@@ -27,25 +27,25 @@ struct FewShape {
 };
 
 template <int D>
-__global__ __launch_bounds__(256, 1) void chunk_attn_few_kernel(ChunkAttnArgs a, int items) {
+__global__ __launch_bounds__(256, 1) void chunk_attn_few_kernel(ChunkAttnArgs a) {
   using G = FewShape<D>;
   using Feed = RowFeed<D, kTile / 2>;
   constexpr int KS = D / 16, DB = D / 32, NR = Feed::NR, S = G::S;
   extern __shared__ __align__(1024) unsigned char smem[];
-  if ((int)blockIdx.x >= items) {
-    report_status<256>(a.b, (int)blockIdx.x - items, true);
+  if ((int)blockIdx.x >= a.few.items) {
+    report_status<256>(a.b, (int)blockIdx.x - a.few.items, true);
     return;
   }
   const ChunkGeom& ge = a.few;
-  const Item it = item_of(a.b, ge, blockIdx.x);
-  const ChunkSeq sq = chunk_seq(a.b, it.b);
+  const Item it = find_item(a.b, ge, 1, a.few_rows, blockIdx.x);
+  const ChunkSeq& sq = it.seq;
+  if (sq.n == 0) return;
   const int rows = sq.n * a.b.group;
-  if (rows == 0 || rows > a.few_rows) return;
   const int limit = block_limit(a, ge, sq, 0);
   const int lo = it.split * ge.split_rows;
   if (lo >= limit) return;
   const bool whole = limit <= ge.split_rows;
-  const int hi_row = ge.nsplit == 1 ? limit : min(limit, lo + ge.split_rows);
+  const int hi_row = whole ? limit : min(limit, lo + ge.split_rows);
   const int nt = (hi_row - lo + kTile - 1) / kTile;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -176,8 +176,7 @@ hipError_t go(bool launch, const ChunkAttnArgs& a, bool status, hipStream_t s) {
   if (!launch)
     return hipFuncSetAttribute(reinterpret_cast<const void*>(&chunk_attn_few_kernel<D>),
                                hipFuncAttributeMaxDynamicSharedMemorySize, FewShape<D>::kLds);
-  const int items = (int)item_count(a.b, a.few);
-  hipLaunchKernelGGL(chunk_attn_few_kernel<D>, dim3(items + (status ? a.b.batch : 0)), dim3(256), FewShape<D>::kLds, s, a, items);
+  hipLaunchKernelGGL(chunk_attn_few_kernel<D>, dim3(a.few.items + (status ? a.b.batch : 0)), dim3(256), FewShape<D>::kLds, s, a);
   return hipGetLastError();
 }
 

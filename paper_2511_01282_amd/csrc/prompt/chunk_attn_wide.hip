@@ -25,25 +25,25 @@ struct WideShape {
 };
 
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a, int items) {
+__global__ __launch_bounds__(64 * kWaves, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a) {
   using G = WideShape<D>;
   using Feed = RowFeed<D, 16>;
   constexpr int KS = D / 16, DB = D / 32, S = G::S;
   extern __shared__ __align__(1024) unsigned char smem[];
-  if ((int)blockIdx.x >= items) {
-    report_status<64 * kWaves>(a.b, (int)blockIdx.x - items, true);
+  if ((int)blockIdx.x >= a.wide.items) {
+    report_status<64 * kWaves>(a.b, (int)blockIdx.x - a.wide.items, true);
     return;
   }
   const ChunkGeom& ge = a.wide;
-  const Item it = item_of(a.b, ge, blockIdx.x);
-  const ChunkSeq sq = chunk_seq(a.b, it.b);
+  const Item it = find_item(a.b, ge, a.few_rows + 1, INT32_MAX, blockIdx.x);
+  const ChunkSeq& sq = it.seq;
+  if (sq.n == 0) return;
   const int rows = sq.n * a.b.group, row0 = it.rb * ge.rows_per_wg;
-  if (row0 >= rows || rows <= a.few_rows) return;
   const int limit = block_limit(a, ge, sq, it.rb);
   const int lo = it.split * ge.split_rows;
   if (lo >= limit) return;
   const bool whole = limit <= ge.split_rows;  // the block's only split
-  const int hi_row = ge.nsplit == 1 ? limit : min(limit, lo + ge.split_rows);
+  const int hi_row = whole ? limit : min(limit, lo + ge.split_rows);
   const int np = (hi_row - lo + kTile * kPass - 1) / (kTile * kPass);  // passes
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -167,9 +167,7 @@ hipError_t go(bool launch, const ChunkAttnArgs& a, bool status, hipStream_t s) {
   if (!launch)
     return hipFuncSetAttribute(reinterpret_cast<const void*>(&chunk_attn_wide_kernel<D>),
                                hipFuncAttributeMaxDynamicSharedMemorySize, WideShape<D>::kLds);
-  const int items = (int)item_count(a.b, a.wide);
-  hipLaunchKernelGGL(chunk_attn_wide_kernel<D>, dim3(items + (status ? a.b.batch : 0)), dim3(64 * kWaves), WideShape<D>::kLds, s, a,
-                     items);
+  hipLaunchKernelGGL(chunk_attn_wide_kernel<D>, dim3(a.wide.items + (status ? a.b.batch : 0)), dim3(64 * kWaves), WideShape<D>::kLds, s, a);
   return hipGetLastError();
 }
 

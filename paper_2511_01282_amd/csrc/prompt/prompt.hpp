@@ -55,9 +55,9 @@ struct AppendArgs {
 // How an attention kernel cuts its sequences: a workgroup per (row block, split, KV head, sequence).
 struct ChunkGeom {
   int32_t rows_per_wg;  // query rows, (token, head-in-group) pairs, of a block
-  int32_t n_rowblk;     // blocks of the longest chunk
   int32_t nsplit;       // splits of the longest sequence; 1: no partials
   int32_t split_rows;   // cache rows of a split
+  int32_t items;        // grid: (row block, split, sequence, KV head), see find_item
 };
 
 struct ChunkAttnArgs {
@@ -74,9 +74,6 @@ struct ChunkAttnArgs {
   int32_t few_rows;
   ChunkGeom few, wide;
 };
-inline long long item_count(const ChunkBatch& c, const ChunkGeom& ge) {
-  return (long long)c.n_kv_heads * c.batch * ge.nsplit * ge.n_rowblk;
-}
 constexpr int kFewRows = 32;   // of bf16 chunks; float32 has the second geometry only
 
 struct ScoreArgs {

@@ -32,6 +32,7 @@ bool aligned(const void* p, size_t n) { return ((uintptr_t)p % n) == 0; }
 bool known(int32_t dtype) { return dtype == RESPEC_F32 || dtype == RESPEC_BF16; }
 long long cdiv(long long a, long long b) { return (a + b - 1) / b; }
 
+constexpr int kCus = 256;                  // compute units
 constexpr int kMaxSplits = 64;             // a lane of the merge per split
 constexpr size_t kMaxPartRows = 1u << 18;  // 136 MB at 128 columns
 constexpr int kMaxStride = 1 << 24;
@@ -81,18 +82,36 @@ ChunkBatch device_batch(const respec_chunk_plan* plan, const respec_chunk_batch&
   return d;
 }
 
-// Splits of at least `least` cache rows (multiples of `unit`), so many that there are about `wgs` workgroups, if
-// every sequence were the longest.
-ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, int n_rowblk, long long limit, int unit, int least, int wgs, int held) {
-  ChunkGeom g{rows_per_wg, n_rowblk, 1, INT_MAX};
-  const long long items = (long long)n_rowblk * b.n_kv_heads * b.batch;
-  if (items == 0) return g;
-  const long long n = std::min({wgs / items, cdiv(limit, least), (long long)held});
-  if (n <= 1) return g;
-  const long long rows = cdiv(cdiv(limit, n), unit) * unit;
-  if (rows >= limit) return g;
-  g.split_rows = (int)rows;
-  g.nsplit = (int)cdiv(limit, rows);
+// How long an attention kernel takes over one cache row of a block, and to start a workgroup (us).
+struct Pace {
+  double row, start;
+};
+
+// Splits of the sequences: the number n (at most `held`, each of `least` cache rows or more, in multiples of `unit`)
+// with the least estimated time  rounds * (rows / n * row + start) + merge,  rounds = items * n / CUs.  One
+// sequence's lengths are known, and its workgroups run in whole rounds; of a batch the host knows the longest
+// alone, so about a third of the work that longest sequences would be is assumed, and half a round of tail.
+ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long long limit, int unit, int least, int per_cu, Pace pace,
+                   int row_bytes, long long held) {
+  ChunkGeom g{rows_per_wg, 1, INT_MAX, 0};
+  const long long items = blocks * b.n_kv_heads;
+  double best = 0;
+  long long most = std::min({cdiv(limit, least), (long long)kMaxSplits, held, items > 0 ? (long long)INT_MAX / items : 1});
+  for (long long n = 1, rows_before = 0; n <= std::max(most, 1ll); ++n) {
+    const long long rows = cdiv(cdiv(limit, n), unit) * unit;
+    if (rows == rows_before) continue;
+    rows_before = rows;
+    const double wgs = (double)items * cdiv(limit, std::max(rows, 1ll)) / (kCus * per_cu);
+    const double rounds = b.batch == 1 ? ceil(wgs) : std::max(1.0, wgs * 0.3) + 0.5;
+    const double merge = n == 1 ? 0 : 4 + 1e-6 * n * b.total_new * b.n_kv_heads * b.group * row_bytes * 2 / 4.5;
+    const double t = rounds * (rows * pace.row + pace.start) + merge;
+    if (n == 1 || t < best) {
+      best = t;
+      g.split_rows = n == 1 || rows >= limit ? INT_MAX : (int)rows;
+    }
+  }
+  g.nsplit = g.split_rows == INT_MAX ? 1 : (int)cdiv(limit, g.split_rows);
+  g.items = (int)std::min(items * g.nsplit, (long long)INT_MAX);
   return g;
 }
 
@@ -203,21 +222,25 @@ respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chun
   a.part_l = reinterpret_cast<float*>(ws + o_bytes + m_bytes);
   a.scale_log2 = (float)(1.4426950408889634 * (x.scale > 0.f ? (double)x.scale : 1.0 / sqrt((double)s.head_dim)));
   const long long limit = (long long)a.b.max_kv + a.b.max_new;  // rows that the last token of the longest sequence sees
-  const long long rows = (long long)a.b.max_new * a.b.group;    // query rows per KV head of the longest chunk
-  const int held = x.b.total_new > 0 ? (int)std::min<size_t>(plan->part_rows / ((size_t)x.b.total_new * s.n_q_heads), kMaxSplits) : 1;
+  const long long all_rows = (long long)a.b.total_new * a.b.group, rows = (long long)a.b.max_new * a.b.group;  // per KV head
+  const long long seqs = std::min(a.b.batch, a.b.total_new);    // sequences that can have tokens
+  const long long held = x.b.total_new > 0 ? (long long)(plan->part_rows / ((size_t)x.b.total_new * s.n_q_heads)) : 1;
+  // row blocks of all sequences: each sequence's last one may be short
+  auto blocks = [&](int per_wg) { return std::min(cdiv(all_rows, per_wg) + (seqs > 1 ? seqs - 1 : 0), seqs * cdiv(rows, per_wg)); };
+  const int rb = (s.head_dim + 2) * 4;
   hipStream_t stm = static_cast<hipStream_t>(stream);
   bool status = a.b.status != nullptr;  // (the first launch reports it)
   if (s.dtype == RESPEC_F32) {
     a.few_rows = 0;
-    a.few = ChunkGeom{1, 0, 1, INT_MAX};
-    a.wide = geometry(a.b, 64, (int)cdiv(rows, 64), limit, 32, 256, 1024, held);
-    if (item_count(a.b, a.wide) + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
+    a.few = ChunkGeom{1, 1, INT_MAX, 0};
+    a.wide = geometry(a.b, 64, blocks(64), limit, 32, 32, 4, s.head_dim == 128 ? Pace{0.2, 5} : Pace{0.1, 5}, rb, held);
+    if ((long long)a.wide.items + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
     if (launch_chunk_attn_f32(s.head_dim, a, status, stm) != hipSuccess) return RESPEC_ERR_HIP;
   } else {
     a.few_rows = kFewRows;
-    a.few = geometry(a.b, kFewRows, 1, limit, 128, 256, 2048, held);
-    a.wide = geometry(a.b, 256, (int)cdiv(rows, 256), limit, 64, 512, 512, held);
-    if (item_count(a.b, a.few) + a.b.batch > INT_MAX || item_count(a.b, a.wide) + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
+    a.few = geometry(a.b, kFewRows, seqs, limit, 128, 128, 1, s.head_dim == 128 ? Pace{0.03, 6} : Pace{0.015, 6}, rb, held);
+    a.wide = geometry(a.b, 256, blocks(256), limit, 128, 256, 1, s.head_dim == 128 ? Pace{0.014, 6} : Pace{0.008, 6}, rb, held);
+    if ((long long)a.few.items + a.b.batch > INT_MAX || (long long)a.wide.items + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
     if (!raise_lds_limits(s.head_dim)) return RESPEC_ERR_HIP;
     const bool any_wide = rows > kFewRows, any_few = !any_wide || a.b.batch > 1;
     if (any_wide) {

@@ -21,9 +21,9 @@ FLAGS = [
     "-I", os.path.join(ROOT, "include"),
 ]
 
-# matrix products accumulate in ordinary registers: the kernel's softmax works on them, and its queries fill the
-# accumulation registers
-FILE_FLAGS = {"chunk_attn_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+# matrix products accumulate in ordinary registers, on which the softmax works (accumulation registers would be moved to
+# and fro)
+FILE_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for f in ("chunk_attn_wide.hip", "chunk_attn_few.hip")}
 
 
 CXX = os.environ.get("CXX", "g++")

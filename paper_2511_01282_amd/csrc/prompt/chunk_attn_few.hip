@@ -1,7 +1,7 @@
 // Causal attention of a few query rows over a paged cache, bf16: decoding steps and short chunks.
 //
-// Up to 32 query rows (tokens times the heads of a group) of a sequence and KV head: the cache is read
-// once and memory bounds it.  A workgroup takes a split of the cache rows; its four waves own all the query rows
+// Up to 32 or 64 query rows (tokens times the heads of a group) of a sequence and KV head: the cache is
+// read once and memory bounds it.  A workgroup takes a split of the cache rows; its four waves own all the query rows
 // and every fourth tile of 32 cache rows each, with a ring of their own in LDS that they fill by DMA, so
 // nothing but a wave's own requests is ever waited for.  At the end the waves' (m, l, O) are joined through LDS.
 #include "chunk_pages.hpp"
@@ -26,7 +26,7 @@ struct FewShape {
   static_assert(kLds <= 163840, "LDS of a CU");
 };
 
-template <int D>
+template <int D, int GR>  // groups of 32 query rows
 __global__ __launch_bounds__(256, 1) void chunk_attn_few_kernel(ChunkAttnArgs a) {
   using G = FewShape<D>;
   using Feed = RowFeed<D, kTile / 2>;
@@ -55,13 +55,19 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_few_kernel(ChunkAttnArgs a)
   const unsigned char* ring = smem + wave * G::kWave;
   const int my_nt = nt > wave ? (nt - wave + 3) / 4 : 0;
 
-  const int row = min(r32, rows - 1), i = (int)div_by((uint32_t)row, a.group);
-  const int64_t tok = sq.t0 + i, head = (int64_t)it.g * a.b.group + (row - i * a.b.group);
-  const int end[1] = {min(sq.L + i + 1, hi_row)};
+  int64_t tok[GR], head[GR];
+  int end[GR];
+#pragma unroll
+  for (int g = 0; g < GR; ++g) {
+    const int row = min(g * 32 + r32, rows - 1), i = (int)div_by((uint32_t)row, a.group);
+    tok[g] = sq.t0 + i;
+    head[g] = (int64_t)it.g * a.b.group + (row - i * a.b.group);
+    end[g] = min(sq.L + i + 1, hi_row);
+  }
   const int unmasked = min(sq.L + 1, hi_row);  // rows that every query row sees
 
   Feed feed;
-  feed.init(a.b, it.g, lane);
+  feed.init(a.b, it.g, 0, lane);
   PageIds<G::kPageIds> ids{reinterpret_cast<int32_t*>(smem + G::kIds) + wave * G::kPageIds, a.b.table + (int64_t)it.b * a.b.table_stride, 0u, 0u,
               div_by((uint32_t)(hi_row - 1), a.b.page) + 1u};
   const bool in_page = a.b.page.d % 16 == 0;  // 16 rows from a multiple of 16 lie in one page
@@ -82,14 +88,21 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_few_kernel(ChunkAttnArgs a)
   };
   for (int t = 0; t < min(my_nt, S); ++t) produce();
 
-  u32x4 qf[KS];
-  {
-    const char* q = a.q + tok * a.q_tok + head * a.q_head;
+  u32x4 qf[GR][KS];
+  Rows<D> r[GR];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = ld16(q + (2 * ks + hi) * 16);
+  for (int g = 0; g < GR; ++g) {
+    const char* q = a.q + tok[g] * a.q_tok + head[g] * a.q_head;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[g][ks] = ld16(q + (2 * ks + hi) * 16);
+    r[g].init();
   }
-  Rows<D> r[1];
-  r[0].init();
+  if constexpr (GR > 1) {  // (the queries in accumulation registers, which the products read as they are)
+#pragma unroll
+    for (int g = 0; g < GR; ++g)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) asm("" : "+a"(qf[g][ks]));
+  }
 #pragma unroll 1
   for (int j = 0; j < my_nt; ++j) {
     switch (produced - 1 - j) {  // tiles requested after this one, 4 NR requests each
@@ -100,24 +113,33 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_few_kernel(ChunkAttnArgs a)
     }
     const unsigned char* t = ring + (j % S) * G::kSlot;
     const int key0 = lo + (j * 4 + wave) * kTile;
-    u32x4 kf[KS], vf[DB][2], p[2];
+    u32x4 kf[KS], vf[DB][2], p[GR][2];
     read_k<D>(t, lane, kf);
     read_v<D>(t + G::kHalf, lane, vf);
-    f32x16 s = f32x16{};
+    f32x16 s[GR];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) s = mma32(kf[ks], qf[ks], s);
+    for (int g = 0; g < GR; ++g) {
+      s[g] = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) s[g] = mma32(kf[ks], qf[g][ks], s[g]);
+    }
     if (key0 + kTile <= unmasked) {
-      settle(r[0], s, a.scale_log2, p, weights(s, a.scale_log2, r[0].m, p));
+#pragma unroll
+      for (int g = 0; g < GR; ++g) settle(r[g], s[g], a.scale_log2, p[g], weights(s[g], a.scale_log2, r[g].m, p[g]));
     } else {
-      mask_scores(s, key0, end[0], lane);
-      const bool odd = take_out_not_finite<D>(vf);
-      settle(r[0], s, a.scale_log2, p, weights(s, a.scale_log2, r[0].m, p));
-      if (odd) add_not_finite<D, 1>(r, t + G::kHalf, key0, end, lane);
+#pragma unroll
+      for (int g = 0; g < GR; ++g) {
+        mask_scores(s[g], key0, end[g], lane);
+        settle(r[g], s[g], a.scale_log2, p[g], weights(s[g], a.scale_log2, r[g].m, p[g]));
+      }
+      if (take_out_not_finite<D>(vf)) add_not_finite<D, GR>(r, t + G::kHalf, key0, end, lane);
     }
 #pragma unroll
     for (int k2 = 0; k2 < 2; ++k2)
 #pragma unroll
-      for (int db = 0; db < DB; ++db) r[0].o[db] = mma32(vf[db][k2], p[k2], r[0].o[db]);
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < GR; ++g) r[g].o[db] = mma32(vf[db][k2], p[g][k2], r[g].o[db]);
     // this wave's reads of the slot are done before it is filled again
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (produced < my_nt) produce();
@@ -125,69 +147,75 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_few_kernel(ChunkAttnArgs a)
 
   // ---- O = sum_w 2^(m_w - M) O_w, l likewise: every wave writes its own, and joins a quarter of the columns ----
   float2* ml = reinterpret_cast<float2*>(smem + G::kMl);
-  {
+#pragma unroll
+  for (int g = 0; g < GR; ++g) {
+    if (g > 0) __syncthreads();
     f32x4* to = reinterpret_cast<f32x4*>(smem + wave * G::kWave) + lane;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        to[(db * 4 + q) * 64] = f32x4{r[0].o[db][4 * q], r[0].o[db][4 * q + 1], r[0].o[db][4 * q + 2], r[0].o[db][4 * q + 3]};
-    ml[wave * 64 + lane] = make_float2(r[0].m, r[0].l);
-  }
-  __syncthreads();
-  float M = kNoRef, w[4], l = 0.f;
+        to[(db * 4 + q) * 64] = f32x4{r[g].o[db][4 * q], r[g].o[db][4 * q + 1], r[g].o[db][4 * q + 2], r[g].o[db][4 * q + 3]};
+    ml[wave * 64 + lane] = make_float2(r[g].m, r[g].l);
+    __syncthreads();
+    float M = kNoRef, w[4], l = 0.f;
 #pragma unroll
-  for (int x = 0; x < 4; ++x) M = fmaxf(M, ml[x * 64 + lane].x);
+    for (int x = 0; x < 4; ++x) M = fmaxf(M, ml[x * 64 + lane].x);
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    w[x] = __builtin_amdgcn_exp2f(ml[x * 64 + lane].x - M);
-    l += w[x] * ml[x * 64 + lane].y;
-  }
-  l += xchg<5>(l);
-  const bool mine = r32 < rows;
-  const int64_t pr = ((int64_t)it.split * a.b.total_new + tok) * ((int64_t)a.b.n_kv_heads * a.b.group) + head;
-  const float inv = 1.f / l;
-#pragma unroll
-  for (int c = 0; c < DB; ++c) {  // (4 DB blocks of 8 columns, DB per wave)
-    const int blk = wave * DB + c;
-    f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int x = 0; x < 4; ++x) v += (reinterpret_cast<const f32x4*>(smem + x * G::kWave) + lane)[blk * 64] * w[x];
-    const int col = 32 * (blk / 4) + 8 * (blk % 4) + 4 * hi;
-    if (!mine) continue;
-    if (whole) {
-      u32x2 y;
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * e] * inv, v[2 * e + 1] * inv}, bf16x2));
-      *reinterpret_cast<u32x2*>(a.out + tok * a.o_tok + head * a.o_head + col * 2) = y;
-    } else {
-      *reinterpret_cast<f32x4*>(a.part_o + pr * D + col) = v;
+    for (int x = 0; x < 4; ++x) {
+      w[x] = __builtin_amdgcn_exp2f(ml[x * 64 + lane].x - M);
+      l += w[x] * ml[x * 64 + lane].y;
     }
-  }
-  if (!whole && mine && wave == 0 && hi == 0) {
-    a.part_m[pr] = M;
-    a.part_l[pr] = l;
+    l += xchg<5>(l);
+    const bool mine = g * 32 + r32 < rows;
+    const int64_t pr = ((int64_t)it.split * a.b.total_new + tok[g]) * ((int64_t)a.b.n_kv_heads * a.b.group) + head[g];
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int c = 0; c < DB; ++c) {  // (4 DB blocks of 8 columns, DB per wave)
+      const int blk = wave * DB + c;
+      f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < 4; ++x) v += (reinterpret_cast<const f32x4*>(smem + x * G::kWave) + lane)[blk * 64] * w[x];
+      const int col = 32 * (blk / 4) + 8 * (blk % 4) + 4 * hi;
+      if (!mine) continue;
+      if (whole) {
+        u32x2 y;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * e] * inv, v[2 * e + 1] * inv}, bf16x2));
+        *reinterpret_cast<u32x2*>(a.out + tok[g] * a.o_tok + head[g] * a.o_head + col * 2) = y;
+      } else {
+        *reinterpret_cast<f32x4*>(a.part_o + pr * D + col) = v;
+      }
+    }
+    if (!whole && mine && wave == 0 && hi == 0) {
+      a.part_m[pr] = M;
+      a.part_l[pr] = l;
+    }
   }
 }
 
-template <int D>
+template <int D, int GR>
 hipError_t go(bool launch, const ChunkAttnArgs& a, bool status, hipStream_t s) {
   if (!launch)
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(&chunk_attn_few_kernel<D>),
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&chunk_attn_few_kernel<D, GR>),
                                hipFuncAttributeMaxDynamicSharedMemorySize, FewShape<D>::kLds);
-  hipLaunchKernelGGL(chunk_attn_few_kernel<D>, dim3(a.few.items + (status ? a.b.batch : 0)), dim3(256), FewShape<D>::kLds, s, a);
+  hipLaunchKernelGGL((chunk_attn_few_kernel<D, GR>), dim3(a.few.items + (status ? a.b.batch : 0)), dim3(256), FewShape<D>::kLds, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_chunk_attn_few(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s) {
-  return head_dim == 128 ? go<128>(true, a, status, s) : go<64>(true, a, status, s);
+  if (a.few.rows_per_wg == 32) return head_dim == 128 ? go<128, 1>(true, a, status, s) : go<64, 1>(true, a, status, s);
+  if (a.few.rows_per_wg == 64) return head_dim == 128 ? go<128, 2>(true, a, status, s) : go<64, 2>(true, a, status, s);
+  return hipErrorInvalidValue;
 }
 hipError_t set_chunk_attn_few_lds_limit(int head_dim) {
   const ChunkAttnArgs none{};
-  return head_dim == 128 ? go<128>(false, none, false, nullptr) : go<64>(false, none, false, nullptr);
+  const hipError_t e = head_dim == 128 ? go<128, 1>(false, none, false, nullptr) : go<64, 1>(false, none, false, nullptr);
+  if (e != hipSuccess) return e;
+  return head_dim == 128 ? go<128, 2>(false, none, false, nullptr) : go<64, 2>(false, none, false, nullptr);
 }
 
 }  // namespace respec

@@ -10,12 +10,15 @@
 namespace respec {
 namespace {
 
-constexpr int kTile = 32, kPass = 4;  // cache rows of a tile, tiles of a pass
+constexpr int kTile = 32;  // cache rows of a tile
 constexpr int kWaves = 8;
 
 template <int D>
 struct WideShape {
-  static constexpr int S = 2 * kPass + 1;          // ring slots: a pass and the tile after it, and the next ones under way
+  static constexpr int kPass = 4;              // tiles between two barriers
+  static constexpr int kAhead = D == 128 ? 1 : 3;  // passes under way
+  static constexpr int S = kPass * (kAhead + 1) + 1;   // ring slots: a pass and the tile after it, and those under way
+  static constexpr int kRows = kPass * kTile / kWaves;  // cache rows of a pass that a wave brings
   static constexpr int kHalf = kTile * D * 2;      // bytes of a K or V tile
   static constexpr int kSlot = 2 * kHalf;
   static constexpr int kPageIds = 384;             // page ids of a wave's window
@@ -27,8 +30,8 @@ struct WideShape {
 template <int D>
 __global__ __launch_bounds__(64 * kWaves, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a) {
   using G = WideShape<D>;
-  using Feed = RowFeed<D, 16>;
-  constexpr int KS = D / 16, DB = D / 32, S = G::S;
+  using Feed = RowFeed<D, G::kRows>;
+  constexpr int KS = D / 16, DB = D / 32, S = G::S, kPass = G::kPass, kRows = G::kRows, NR = Feed::NR;
   extern __shared__ __align__(1024) unsigned char smem[];
   if ((int)blockIdx.x >= a.wide.items) {
     report_status<64 * kWaves>(a.b, (int)blockIdx.x - a.wide.items, true);
@@ -67,37 +70,46 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_attn_wide_kernel(ChunkAt
   const int my_tiles = wrow < rows && my_end > lo ? (my_end - lo + kTile - 1) / kTile : 0;
   const int unmasked = max(my_first - lo, 0) / kTile;
 
-  // ---- DMA: unit u is tiles 4 u + 1 .. 4 u + 4 (unit -1: tile 0), 16 rows of each by every wave ----
+  // ---- DMA: unit u is tiles kPass u + 1 .. kPass u + kPass (unit -1: tile 0), kRows rows of each by every wave ----
   Feed feed;
-  feed.init(a.b, it.g, lane);
+  feed.init(a.b, it.g, wave * kRows % kTile, lane);
   PageIds<G::kPageIds> ids{reinterpret_cast<int32_t*>(smem + G::kIds) + wave * G::kPageIds,
                            a.b.table + (int64_t)it.b * a.b.table_stride, 0u, 0u, div_by((uint32_t)(hi_row - 1), a.b.page) + 1u};
-  const bool in_page = a.b.page.d % 16 == 0;  // a wave's 16 rows lie in one page
+  const bool in_page = a.b.page.d % kRows == 0;  // a wave's rows of a unit lie in one page
+  const int w_tile = wave * kRows / kTile, w_row = wave * kRows % kTile;  // ... within the unit, and the tile
+  // units that this wave requests something of end here (it asks for rows of the last tile, no further ones)
+  const int n_units = ((hi_row - lo + kTile - 1) / kTile - 1 - w_tile + kPass - 1) / kPass;
   int unit = -1;
   auto request = [&]() __attribute__((always_inline)) {
-    const int t = kPass * unit + 1 + (wave >> 1), t0 = lo + t * kTile + (wave & 1) * 16;
-    ++unit;
-    if (t < 0 || t0 >= hi_row + 16) return;  // (the half tile behind the last row is read by the products, too)
-    const uint32_t dst = lds0 + (uint32_t)((t % S) * G::kSlot + (wave & 1) * 16 * D * 2);
+    const int u = unit++, t = kPass * u + 1 + w_tile, t0 = lo + t * kTile + w_row;
+    if (t < 0 || u >= n_units) return;
+    const uint32_t dst = lds0 + (uint32_t)((t % S) * G::kSlot + w_row * D * 2);
     const uint32_t pa = div_by((uint32_t)min(t0, hi_row - 1), a.b.page);
-    ids.need(pa, div_by((uint32_t)min(t0 + 15, hi_row - 1), a.b.page), lane);
-    if (in_page && t0 + 16 <= hi_row)
+    ids.need(pa, div_by((uint32_t)min(t0 + kRows - 1, hi_row - 1), a.b.page), lane);
+    if (in_page && t0 + kRows <= hi_row)
       feed.from_page(a.b, dst, dst + G::kHalf, ids.uniform(pa), (uint32_t)t0 - pa * a.b.page.d);
     else
       feed.from_rows(a.b, dst, dst + G::kHalf, ids.ids, ids.p0, t0, hi_row, lane);
   };
-  // Everything requested has landed for every wave.  (What a wave has read of the slots it is done with it has
-  // used in products, so nothing of them is under way.)
-  auto landed = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory"); };
-  request();
-  request();
+  // Unit u has landed for every wave: of this one's requests only those of later units are under way.  (What a wave
+  // has read of the slots it is done with it has used in products, so nothing of them is under way.)
+  auto landed = [&](int u) __attribute__((always_inline)) {
+    const int newer = min(n_units, u + G::kAhead) - 1 - u;
+    if (newer >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * NR) : "memory");
+    else if (newer == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NR) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_barrier" ::: "memory");
+  };
+  static_assert(G::kAhead <= 3, "landed() tells two newer units apart");
+#pragma unroll
+  for (int u = -1; u < G::kAhead; ++u) request();
 
   Rows<D> r[1];
   r[0].init();
   f32x16 s[2];
   u32x4 p[2], kf[KS], vf[DB][2];
   auto slot = [&](int t) __attribute__((always_inline)) { return smem + (t % S) * G::kSlot; };
-  landed();
+  landed(0);
   if (my_tiles > 0) {
     read_k<D>(slot(0), lane, kf);
     s[0] = f32x16{};
@@ -133,29 +145,31 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_attn_wide_kernel(ChunkAt
   using I1 = std::integral_constant<int, 1>;
   auto pass = [&](auto masked_c, int j) __attribute__((always_inline)) {
     const int t = kPass * j;
-    tile(masked_c, I0{}, t);
-    tile(masked_c, I1{}, t + 1);
-    tile(masked_c, I0{}, t + 2);
-    tile(masked_c, I1{}, t + 3);
+#pragma unroll
+    for (int u = 0; u < kPass; u += 2) {
+      tile(masked_c, I0{}, t + u);
+      tile(masked_c, I1{}, t + u + 1);
+    }
   };
   // (every wave passes np barriers; a tile takes the next one's scores, too)
   int j = 0;
 #pragma unroll 1
   for (; kPass * j + kPass + 1 <= unmasked; ++j) {
-    if (j > 0) landed();
+    if (j > 0) landed(j);
     request();
     pass(std::integral_constant<bool, false>{}, j);
   }
 #pragma unroll 1
   for (; j < np; ++j) {
-    if (j > 0) landed();
+    if (j > 0) landed(j);
     request();
-    const int t = kPass * j;
-    using Yes = std::integral_constant<bool, true>;
-    if (t < my_tiles) tile(Yes{}, I0{}, t);
-    if (t + 1 < my_tiles) tile(Yes{}, I1{}, t + 1);
-    if (t + 2 < my_tiles) tile(Yes{}, I0{}, t + 2);
-    if (t + 3 < my_tiles) tile(Yes{}, I1{}, t + 3);
+#pragma unroll
+    for (int u = 0; u < kPass; u += 2) {
+      const int t = kPass * j + u;
+      using Yes = std::integral_constant<bool, true>;
+      if (t < my_tiles) tile(Yes{}, I0{}, t);
+      if (t + 1 < my_tiles) tile(Yes{}, I1{}, t + 1);
+    }
   }
   // the requests past the last pass land before the workgroup's LDS is released
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");

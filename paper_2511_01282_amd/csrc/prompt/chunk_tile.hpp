@@ -50,8 +50,16 @@ __device__ __forceinline__ void dma_rows(uint32_t dst, uint64_t base, const uint
   uint32_t saved;
   dst = __builtin_amdgcn_readfirstlane(dst);
   base = uniform_u64(base);
-  static_assert(N == 2 || N == 4, "requests");
-  if constexpr (N == 2) {
+  static_assert(N == 1 || N == 2 || N == 4, "requests");
+  if constexpr (N == 1) {
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+        "global_load_lds_dwordx4 %2, %3\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "s"(dst), "v"(off[0]), "s"(base)
+        : "memory");
+  } else if constexpr (N == 2) {
     asm volatile(
         "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
         "global_load_lds_dwordx4 %2, %4\n\t"
@@ -87,23 +95,26 @@ __device__ __forceinline__ void dma_lanes(uint32_t dst, uint64_t addr) {
 }
 
 // What a wave brings of every tile: R rows (NR requests) of K and of V, rows r0 .. r0 + R - 1 of the sequence
-// into LDS at k_dst and v_dst.  The page ids of the rows lie in LDS.
+// into LDS at k_dst and v_dst.  The page ids of the rows lie in LDS.  (R and the first row's place in its tile
+// are multiples of 8; the chunks' permutation repeats every 16 rows.)
 template <int D, int R>
 struct RowFeed {
   static constexpr int CPR = D / 8, RPI = 64 / CPR, NR = R / RPI;  // chunks per row, rows per request, requests
   const char* k;   // this head of page 0
   const char* v;
   uint32_t k_off[NR], v_off[NR];  // within R rows of one page
+  int first;       // the first row's place in its tile
 
-  __device__ __forceinline__ void init(const ChunkBatch& c, int g, int lane) {
+  __device__ __forceinline__ void init(const ChunkBatch& c, int g, int first_, int lane) {
+    first = first_;
     k = c.k + (int64_t)g * c.head_stride;
     v = c.v + (int64_t)g * c.head_stride;
 #pragma unroll
     for (int q = 0; q < NR; ++q) {
       const int r = q * RPI + lane / CPR, pos = lane % CPR;
       const uint32_t row = (uint32_t)r * c.row_stride + 1024u * (NR - 1 - q);
-      k_off[q] = row + (uint32_t)((pos ^ k_chunk<D>(r)) * 16);
-      v_off[q] = row + (uint32_t)((pos ^ v_chunk<D>(r)) * 16);
+      k_off[q] = row + (uint32_t)((pos ^ k_chunk<D>(first + r)) * 16);
+      v_off[q] = row + (uint32_t)((pos ^ v_chunk<D>(first + r)) * 16);
     }
   }
   // Offset from k and v of R rows in page `id` (uniform), the first at row `at` of it, for dma_rows with k_off and v_off.
@@ -127,8 +138,8 @@ struct RowFeed {
       const int32_t id = ids[p - p0];
       const int64_t page = (uint32_t)id < (uint32_t)c.n_pages ? id : 0;
       const int64_t off = page * c.page_stride + (int64_t)((uint64_t)(row - p * c.page.d) * c.row_stride);
-      dma_lanes(k_dst + 1024 * q, (uint64_t)(k + off + (pos ^ k_chunk<D>(r)) * 16));
-      dma_lanes(v_dst + 1024 * q, (uint64_t)(v + off + (pos ^ v_chunk<D>(r)) * 16));
+      dma_lanes(k_dst + 1024 * q, (uint64_t)(k + off + (pos ^ k_chunk<D>(first + r)) * 16));
+      dma_lanes(v_dst + 1024 * q, (uint64_t)(v + off + (pos ^ v_chunk<D>(first + r)) * 16));
     }
   }
 };

@@ -74,7 +74,7 @@ struct ChunkAttnArgs {
   int32_t few_rows;
   ChunkGeom few, wide;
 };
-constexpr int kFewRows = 32;   // of bf16 chunks; float32 has the second geometry only
+constexpr int kFewRows = 64;   // of bf16 chunks; float32 has the second geometry only
 
 struct ScoreArgs {
   const void* z;

@@ -34,7 +34,7 @@ long long cdiv(long long a, long long b) { return (a + b - 1) / b; }
 
 constexpr int kCus = 256;                  // compute units
 constexpr int kMaxSplits = 64;             // a lane of the merge per split
-constexpr size_t kMaxPartRows = 1u << 18;  // 136 MB at 128 columns
+constexpr size_t kMaxPartial = 1u << 25;    // columns of partials: 134 MB
 constexpr int kMaxStride = 1 << 24;
 
 // Checks of a stride in elements: non-negative and whole 16-byte pieces.
@@ -103,7 +103,8 @@ ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long 
     rows_before = rows;
     const double wgs = (double)items * cdiv(limit, std::max(rows, 1ll)) / (kCus * per_cu);
     const double rounds = b.batch == 1 ? ceil(wgs) : std::max(1.0, wgs * 0.3) + 0.5;
-    const double merge = n == 1 ? 0 : 4 + 1e-6 * n * b.total_new * b.n_kv_heads * b.group * row_bytes * 2 / 4.5;
+    const double joined = 1e-6 * n * b.total_new * b.n_kv_heads * b.group * row_bytes * 2 / 4.5;
+    const double merge = n == 1 ? 0 : 4 + joined * (b.batch == 1 ? 1 : 0.3);
     const double t = rounds * (rows * pace.row + pace.start) + merge;
     if (n == 1 || t < best) {
       best = t;
@@ -148,7 +149,7 @@ respec_status respec_chunk_create(const respec_chunk_shape* shape, respec_chunk_
   if (!p) return RESPEC_ERR_CAPACITY;
   p->s = s;
   p->es = s.dtype == RESPEC_BF16 ? 2 : 4;
-  p->part_rows = std::min((size_t)s.max_new * s.n_q_heads * kMaxSplits, kMaxPartRows);
+  p->part_rows = std::min((size_t)s.max_new * s.n_q_heads * kMaxSplits, kMaxPartial / s.head_dim);
   p->total = align256(p->part_rows * s.head_dim * 4) + 2 * align256(p->part_rows * 4);
   *out = p;
   return RESPEC_OK;
@@ -237,12 +238,12 @@ respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chun
     if ((long long)a.wide.items + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
     if (launch_chunk_attn_f32(s.head_dim, a, status, stm) != hipSuccess) return RESPEC_ERR_HIP;
   } else {
-    a.few_rows = kFewRows;
-    a.few = geometry(a.b, kFewRows, seqs, limit, 128, 128, 1, s.head_dim == 128 ? Pace{0.03, 6} : Pace{0.015, 6}, rb, held);
-    a.wide = geometry(a.b, 256, blocks(256), limit, 128, 256, 1, s.head_dim == 128 ? Pace{0.014, 6} : Pace{0.008, 6}, rb, held);
+    a.few_rows = rows <= 32 ? 32 : kFewRows;
+    a.few = geometry(a.b, a.few_rows, seqs, limit, 128, 128, 1, s.head_dim == 128 ? Pace{0.02, 6} : Pace{0.01, 6}, rb, held);
+    a.wide = geometry(a.b, 256, blocks(256), limit, 128, 256, 1, s.head_dim == 128 ? Pace{0.032, 6} : Pace{0.018, 6}, rb, held);
     if ((long long)a.few.items + a.b.batch > INT_MAX || (long long)a.wide.items + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
     if (!raise_lds_limits(s.head_dim)) return RESPEC_ERR_HIP;
-    const bool any_wide = rows > kFewRows, any_few = !any_wide || a.b.batch > 1;
+    const bool any_wide = rows > a.few_rows, any_few = !any_wide || a.b.batch > 1;
     if (any_wide) {
       if (launch_chunk_attn_wide(s.head_dim, a, status, stm) != hipSuccess) return RESPEC_ERR_HIP;
       status = false;

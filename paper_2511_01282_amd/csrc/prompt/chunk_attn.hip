@@ -11,15 +11,22 @@
 namespace respec {
 namespace {
 
+// float32: four waves of 16 query rows, v_mfma_f32_16x16x4 (mma_k64 in common.hpp).  S^T = K Q^T leaves, in
+// lane l, the scores of row l % 16 with keys 4 (l / 16) .. + 3 of 16, which are the B operand of O^T += V^T P^T as
+// they stand.  A tile of 32 cache rows is fetched into registers while the tile before is worked on, then goes to
+// one of two LDS buffers, K rows as they are and V transposed.  The matrix cores bound it: 32 clocks per product
+// of 2048 operations.
 template <int D>
 __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
-  constexpr int ES = 4;
-  constexpr int KC = D * ES / 64;      // 64-byte K-chunks of a head row
+  constexpr int KC = D / 16;           // 64-byte K-chunks of a head row
   constexpr int DB = D / 16;
   constexpr int TK = 32;
-  constexpr int PITCH = D * ES + 16;
-  constexpr int CPR = D * ES / 16;
-  __shared__ __align__(16) unsigned char ks[TK * PITCH], vs[TK * PITCH];
+  constexpr int KP = D * 4 + 16;       // bytes between K rows
+  constexpr int VP = TK + 4;           // floats between V columns
+  constexpr int CPR = D / 4;           // 16-byte pieces of a row
+  constexpr int NP = TK * CPR / 256;   // ... per thread
+  __shared__ __align__(16) unsigned char k_lds[2][TK * KP];
+  __shared__ __align__(16) float v_lds[2][D * VP];
 
   if ((int)blockIdx.x >= a.wide.items) {
     report_status<256>(a.b, (int)blockIdx.x - a.wide.items, true);
@@ -33,13 +40,13 @@ __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
   const int limit = block_limit(a, ge, sq, it.rb);
   const int lo = it.split * ge.split_rows;
   if (lo >= limit) return;
-  const bool whole = limit <= ge.split_rows;   // the block's only split
+  const bool whole = limit <= ge.split_rows;  // the block's only split
   const int hi = whole ? limit : min(limit, lo + ge.split_rows);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c16 = lane & 15, g4 = lane >> 4;
   const int row = row0 + wave * 16 + c16, rowc = min(row, rows - 1);
   const int i = (int)div_by((uint32_t)rowc, a.group), hh = rowc - i * a.b.group;
-  const int vis = sq.L + i + 1;
+  const int end = min(sq.L + i + 1, hi);  // cache rows that this lane's row sees end here, within the split
   const int64_t t = sq.t0 + i, head = (int64_t)it.g * a.b.group + hh;
   u32x4 qf[KC];
 #pragma unroll
@@ -48,29 +55,45 @@ __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
   const char* kb = a.b.k + (int64_t)it.g * a.b.head_stride;
   const char* vb = a.b.v + (int64_t)it.g * a.b.head_stride;
 
+  // K: consecutive threads take consecutive pieces of a row; V: pieces of consecutive rows, so that the
+  // transposed stores meet every bank once
+  u32x4 kp[NP], vp[NP];
+  auto fetch = [&](int r0) {
+#pragma unroll
+    for (int x = 0; x < NP; ++x) {
+      const int idx = (int)threadIdx.x + x * 256;
+      kp[x] = ld16(kb + row_offset(a.b, table, (uint32_t)min(r0 + idx / CPR, hi - 1)) + (idx % CPR) * 16);
+      vp[x] = ld16(vb + row_offset(a.b, table, (uint32_t)min(r0 + idx % TK, hi - 1)) + (idx / TK) * 16);
+    }
+  };
   float m = kNegInf, l = 0.f;
   f32x4 o[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  for (int r0 = lo; r0 < hi; r0 += TK) {
-    __syncthreads();
-    for (int x = threadIdx.x; x < TK * CPR; x += 256) {
-      const int r = x / CPR, c = x % CPR;
-      const int64_t at = row_offset(a.b, table, (uint32_t)min(r0 + r, hi - 1)) + c * 16;
-      *reinterpret_cast<u32x4*>(ks + r * PITCH + c * 16) = ld16(kb + at);
-      *reinterpret_cast<u32x4*>(vs + r * PITCH + c * 16) = ld16(vb + at);
+  fetch(lo);
+  int buf = 0;
+  for (int r0 = lo; r0 < hi; r0 += TK, buf ^= 1) {
+    unsigned char* ks = k_lds[buf];
+    float* vs = v_lds[buf];
+#pragma unroll
+    for (int x = 0; x < NP; ++x) {
+      const int idx = (int)threadIdx.x + x * 256;
+      *reinterpret_cast<u32x4*>(ks + (idx / CPR) * KP + (idx % CPR) * 16) = kp[x];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) vs[((idx / TK) * 4 + e) * VP + idx % TK] = __uint_as_float(vp[x][e]);
     }
+    // (one barrier per tile: a wave that is here again has seen every wave past the tile between)
     __syncthreads();
+    if (r0 + TK < hi) fetch(r0 + TK);
     f32x4 s[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < KC; ++c)
-        s[u] = mma_k64(0.f, *reinterpret_cast<const u32x4*>(ks + (u * 16 + c16) * PITCH + c * 64 + g4 * 16), qf[c], s[u]);
+        s[u] = mma_k64(0.f, *reinterpret_cast<const u32x4*>(ks + (u * 16 + c16) * KP + c * 64 + g4 * 16), qf[c], s[u]);
     }
-    const int end = min(vis, hi);
     float mx = kNegInf;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -79,20 +102,22 @@ __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
         s[u][e] = r0 + u * 16 + g4 * 4 + e < end ? s[u][e] * a.scale_log2 : kNegInf;
         mx = fmaxf(mx, s[u][e]);
       }
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    mx = fmaxf(mx, xchg<4>(mx));
+    mx = fmaxf(mx, xchg<5>(mx));
     const float mn = fmaxf(m, mx), mb = mn == kNegInf ? 0.f : mn;
-    const float alpha = exp2f(m - mb);
-    m = mn;
-    l *= alpha;
+    if (__any(mn > m)) {
+      const float alpha = __builtin_amdgcn_exp2f(m - mb);
+      l *= alpha;
 #pragma unroll
-    for (int d = 0; d < DB; ++d) o[d] *= alpha;
+      for (int d = 0; d < DB; ++d) o[d] *= alpha;
+    }
+    m = mn;
     f32x4 p[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        p[u][e] = exp2f(s[u][e] - mb);
+        p[u][e] = __builtin_amdgcn_exp2f(s[u][e] - mb);
         l += p[u][e];
       }
     // V^T P^T.  A masked weight is zero, and zero times a NaN or an infinity is not: in a tile that
@@ -100,53 +125,40 @@ __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
     // afterwards for the rows that see them.
     const bool masked = __any(r0 + TK > end);
     bool odd = false;
-    auto value = [&](int key, int d) {
-      float v = Elem<float>::to_f32(vs + key * PITCH, d);
-      if (masked && !(fabsf(v) < __builtin_huge_valf())) {
-        odd = true;
-        v = 0.f;
-      }
-      return v;
-    };
 #pragma unroll
-    for (int d = 0; d < DB; ++d) {
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        u32x4 vf;
+        f32x4 vf = *reinterpret_cast<const f32x4*>(vs + (d * 16 + c16) * VP + u * 16 + g4 * 4);
+        if (masked) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) vf[e] = __float_as_uint(value(u * 16 + g4 * 4 + e, d * 16 + c16));
-        o[d] = mma_k64(0.f, vf, __builtin_bit_cast(u32x4, p[u]), o[d]);
+          for (int e = 0; e < 4; ++e)
+            if (!(fabsf(vf[e]) < __builtin_huge_valf())) {
+              odd = true;
+              vf[e] = 0.f;
+            }
+        }
+        o[d] = mma_k64(0.f, __builtin_bit_cast(u32x4, vf), __builtin_bit_cast(u32x4, p[u]), o[d]);
       }
-    }
-    if (__any(odd)) {
+    if (__any(odd)) {  // whatever the weight, they make a NaN or an infinity of the sum
+      for (int key = 0; key < TK; ++key)
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-        for (int k4 = 0; k4 < 4; ++k4)
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int key = u * 16 + k4 * 4 + e;
-            const float pk = __shfl(p[u][e], k4 * 16 + c16, 64);
-            if (r0 + key >= end) continue;
-#pragma unroll
-            for (int d = 0; d < DB; ++d)
-#pragma unroll
-              for (int x = 0; x < 4; ++x) {
-                const float v = Elem<float>::to_f32(vs + key * PITCH, d * 16 + g4 * 4 + x);
-                if (!(fabsf(v) < __builtin_huge_valf())) o[d][x] += pk * v;
-              }
+            const float v = vs[(d * 16 + g4 * 4 + e) * VP + key];
+            o[d][e] += r0 + key < end && !(fabsf(v) < __builtin_huge_valf()) ? v : 0.f;
           }
     }
   }
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
+  l += xchg<4>(l);
+  l += xchg<5>(l);
   if (row >= rows) return;
   if (whole) {
     char* to = a.out + t * a.o_tok + head * a.o_head;
     const float inv = 1.f / l;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) Elem<float>::store(to, d * 16 + g4 * 4 + e, o[d][e] * inv);
+    for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(to + (d * 16 + g4 * 4) * 4) = o[d] * inv;
   } else {
     const int64_t hq = (int64_t)a.b.n_kv_heads * a.b.group;
     const int64_t pr = ((int64_t)it.split * a.b.total_new + t) * hq + head;
@@ -169,34 +181,37 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkAttnArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % WPR;
   int b;
   const ChunkSeq sq = seq_of_token(a.b, blockIdx.x, b);
-  const int hq = a.b.n_kv_heads * a.b.group, h = (int)blockIdx.y * RPW + wave / WPR;
+  if (sq.n == 0) return;
+  const int hq = a.b.n_kv_heads * a.b.group, i = (int)blockIdx.x - sq.t0;
   const ChunkGeom& ge = sq.n * a.b.group <= a.few_rows ? a.few : a.wide;
-  int ns = 0;
-  if (sq.n > 0 && h < hq) {
-    const int hh = h - (int)div_by((uint32_t)h, a.group) * a.b.group, i = (int)blockIdx.x - sq.t0;
+  if (sq.L + sq.n <= ge.split_rows) return;
+  for (int h0 = (int)blockIdx.y * RPW; h0 < hq; h0 += gridDim.y * RPW) {
+    const int h = min(h0 + wave / WPR, hq - 1), hh = h - (int)div_by((uint32_t)h, a.group) * a.b.group;
     const int limit = block_limit(a, ge, sq, (i * a.b.group + hh) / ge.rows_per_wg);
-    ns = (limit - 1) / ge.split_rows + 1;  // (at most 64)
-  }
-  if (WPR == 1 && ns <= 1) return;
-  float acc[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = 0.f;
-  if (ns > 1) {
+    const int ns = (limit - 1) / ge.split_rows + 1;  // (at most 64)
+    if (WPR == 1 && ns <= 1) continue;
     const int64_t step = (int64_t)a.b.total_new * hq, pr = (int64_t)blockIdx.x * hq + h;
-    const float ms = lane < ns ? a.part_m[lane * step + pr] : kNegInf, ls = lane < ns ? a.part_l[lane * step + pr] : 0.f;
-    const float M = wave_max(ms);
-    float wt = ms == kNegInf ? 0.f : exp2f(ms - M);
-    const float lt = wave_sum(wt * ls);
-    wt /= lt;
     const float* o = a.part_o + pr * D + lane * E;
-    for (int s0 = w * 8; s0 < ns; s0 += WPR * 8) {
-      float x[8][E];
+    float x[8][E];
+    auto fetch = [&](int s0) {
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const float* q = o + min(s0 + u, ns - 1) * step * D;
         if constexpr (E == 2) *reinterpret_cast<float2*>(x[u]) = *reinterpret_cast<const float2*>(q);
         else x[u][0] = *q;
       }
+    };
+    fetch(w * 8);  // (under way beside the weights)
+    const float ms = lane < ns ? a.part_m[lane * step + pr] : kNegInf, ls = lane < ns ? a.part_l[lane * step + pr] : 0.f;
+    const float M = wave_max(ms);
+    float wt = ms == kNegInf ? 0.f : exp2f(ms - M);
+    const float lt = wave_sum(wt * ls);
+    wt /= lt;
+    float acc[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+    for (int s0 = w * 8; s0 < ns; s0 += WPR * 8) {
+      if (s0 > w * 8) fetch(s0);
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const float ws = __shfl(wt, min(s0 + u, 63), 64);
@@ -206,30 +221,33 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkAttnArgs a) {
         }
       }
     }
+    if constexpr (WPR > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < E; ++e) part[wave][lane * E + e] = acc[e];
+      __syncthreads();
+      if (w == 0) {
+#pragma unroll
+        for (int x = 1; x < WPR; ++x)
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[e] += part[wave + x][lane * E + e];
+      }
+    }
+    if (w != 0 || ns <= 1 || h0 + wave / WPR >= hq) continue;
+    char* to = a.out + (int64_t)blockIdx.x * a.o_tok + (int64_t)h * a.o_head;
+#pragma unroll
+    for (int e = 0; e < E; ++e) Elem<T>::store(to, lane * E + e, acc[e]);
   }
-  if constexpr (WPR > 1) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) part[wave][lane * E + e] = acc[e];
-    __syncthreads();
-    if (w != 0 || ns <= 1) return;
-#pragma unroll
-    for (int x = 1; x < WPR; ++x)
-#pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] += part[wave + x][lane * E + e];
-  }
-  char* to = a.out + (int64_t)blockIdx.x * a.o_tok + (int64_t)h * a.o_head;
-#pragma unroll
-  for (int e = 0; e < E; ++e) Elem<T>::store(to, lane * E + e, acc[e]);
 }
 
 template <typename T, int D>
 hipError_t go_merge(const ChunkAttnArgs& a, hipStream_t s) {
   const int hq = a.b.n_kv_heads * a.b.group;
-  // many splits: a row's are read by four waves at once
-  if (max(a.few.nsplit, a.wide.nsplit) > 16)
-    hipLaunchKernelGGL((chunk_merge_kernel<T, D, 4>), dim3(a.b.total_new, hq), dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((chunk_merge_kernel<T, D, 1>), dim3(a.b.total_new, (hq + 3) / 4), dim3(256), 0, s, a);
+  // many splits: a row's are read by four waves at once; many tokens: a workgroup takes several heads of its own
+  const bool many = max(a.few.nsplit, a.wide.nsplit) > 16;
+  const int per_tok = many ? hq : (hq + 3) / 4, y = max(1, min(per_tok, 16384 / a.b.total_new));
+  if (many) hipLaunchKernelGGL((chunk_merge_kernel<T, D, 4>), dim3(a.b.total_new, y), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((chunk_merge_kernel<T, D, 1>), dim3(a.b.total_new, y), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -8,6 +8,7 @@
 #include <new>
 
 #include "../../../include/respec_prompt.h"
+#include "../attn_route.hpp"
 #include "prompt.hpp"
 
 using namespace respec;
@@ -30,9 +31,8 @@ namespace {
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 bool aligned(const void* p, size_t n) { return ((uintptr_t)p % n) == 0; }
 bool known(int32_t dtype) { return dtype == RESPEC_F32 || dtype == RESPEC_BF16; }
-long long cdiv(long long a, long long b) { return (a + b - 1) / b; }
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
-constexpr int kCus = 256;                  // compute units
 constexpr int kMaxSplits = 64;             // a lane of the merge per split
 constexpr size_t kMaxPartial = 1u << 25;    // columns of partials: 134 MB
 constexpr int kMaxStride = 1 << 24;
@@ -96,12 +96,12 @@ ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long 
   ChunkGeom g{rows_per_wg, 1, INT_MAX, 0};
   const long long items = blocks * b.n_kv_heads;
   double best = 0;
-  long long most = std::min({cdiv(limit, least), (long long)kMaxSplits, held, items > 0 ? (long long)INT_MAX / items : 1});
+  long long most = std::min({ceil_div(limit, least), (long long)kMaxSplits, held, items > 0 ? (long long)INT_MAX / items : 1});
   for (long long n = 1, rows_before = 0; n <= std::max(most, 1ll); ++n) {
-    const long long rows = cdiv(cdiv(limit, n), unit) * unit;
+    const long long rows = ceil_div(ceil_div(limit, n), unit) * unit;
     if (rows == rows_before) continue;
     rows_before = rows;
-    const double wgs = (double)items * cdiv(limit, std::max(rows, 1ll)) / (kCus * per_cu);
+    const double wgs = (double)items * ceil_div(limit, std::max(rows, 1ll)) / (kCUs * per_cu);
     const double rounds = b.batch == 1 ? ceil(wgs) : std::max(1.0, wgs * 0.3) + 0.5;
     const double joined = 1e-6 * n * b.total_new * b.n_kv_heads * b.group * row_bytes * 2 / 4.5;
     const double merge = n == 1 ? 0 : 4 + joined * (b.batch == 1 ? 1 : 0.3);
@@ -111,7 +111,7 @@ ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long 
       g.split_rows = n == 1 || rows >= limit ? INT_MAX : (int)rows;
     }
   }
-  g.nsplit = g.split_rows == INT_MAX ? 1 : (int)cdiv(limit, g.split_rows);
+  g.nsplit = g.split_rows == INT_MAX ? 1 : (int)ceil_div(limit, g.split_rows);
   g.items = (int)std::min(items * g.nsplit, (long long)INT_MAX);
   return g;
 }
@@ -227,7 +227,7 @@ respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chun
   const long long seqs = std::min(a.b.batch, a.b.total_new);    // sequences that can have tokens
   const long long held = x.b.total_new > 0 ? (long long)(plan->part_rows / ((size_t)x.b.total_new * s.n_q_heads)) : 1;
   // row blocks of all sequences: each sequence's last one may be short
-  auto blocks = [&](int per_wg) { return std::min(cdiv(all_rows, per_wg) + (seqs > 1 ? seqs - 1 : 0), seqs * cdiv(rows, per_wg)); };
+  auto blocks = [&](int per_wg) { return std::min(ceil_div(all_rows, per_wg) + (seqs > 1 ? seqs - 1 : 0), seqs * ceil_div(rows, per_wg)); };
   const int rb = (s.head_dim + 2) * 4;
   hipStream_t stm = static_cast<hipStream_t>(stream);
   bool status = a.b.status != nullptr;  // (the first launch reports it)

@@ -94,6 +94,7 @@ class _Plan:
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.dtype = _TORCH[shape.dtype]
+        self._index = self.device.index if self.device.type == "cuda" else -1
         self.workspace_bytes = int(getattr(L, f"respec_{kind}_workspace_bytes")(h))
         if workspace is None:
             workspace = torch.empty(self.workspace_bytes + 256, dtype=torch.uint8, device=self.device)
@@ -115,42 +116,42 @@ class _Plan:
         except Exception:
             pass
 
-    def _tensor(self, t, name, dtype, dims):
-        if t.device != self.device:
-            raise ValueError(f"{name} is on {t.device}, the plan on {self.device}")
-        if t.dtype != dtype or t.dim() != dims:
-            raise ValueError(f"{name}: {dims} dimensions of {dtype} expected, got {tuple(t.shape)} of {t.dtype}")
-        return t.data_ptr()
+    def _refuse(self, t, name, dtype, shape):
+        raise ValueError(f"{name}: {dtype} {tuple(shape)} on {self.device}, the last dimension contiguous (every one, of "
+                         f"offsets, lengths, tokens and results), expected; got {t.dtype} {tuple(t.shape)}, strides "
+                         f"{t.stride()}, on {t.device}")
 
-    def _rows(self, t, name, dtype, dims, shape):
+    def _here(self, t):
+        return t.get_device() == self._index and (self._index >= 0 or t.device == self.device)
+
+    def _rows(self, t, name, dtype, shape):
         """Address and strides of a tensor of rows: the last dimension contiguous (where it has more than one)."""
-        p = self._tensor(t, name, dtype, dims)
-        if t.shape != shape:
-            raise ValueError(f"{name}: {tuple(shape)} expected, got {tuple(t.shape)}")
         st = t.stride()
-        if st[-1] != 1 and shape[-1] > 1:
-            raise ValueError(f"{name}: the last dimension is not contiguous")
-        return (p, *st[:-1])
+        if t.shape != shape or t.dtype != dtype or not self._here(t) or (st[-1] != 1 and shape[-1] > 1):
+            self._refuse(t, name, dtype, shape)
+        return t.data_ptr(), st
 
     def _flat(self, t, name, dtype, shape):
         """Address of a contiguous tensor."""
-        p = self._tensor(t, name, dtype, len(shape))
-        if t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{name}: a contiguous {tuple(shape)} expected, got {tuple(t.shape)}")
-        return p
+        if t.shape != shape or t.dtype != dtype or not self._here(t) or not t.is_contiguous():
+            self._refuse(t, name, dtype, shape)
+        return t.data_ptr()
 
-    def _call(self, fn, name, args, stream, *more):
+    def _call(self, fn, name, args, stream):
         if self._h is None:
             raise ValueError("the plan is closed")
         if stream is None:
-            stream = torch.cuda.current_stream(self.device)
+            # (of torch's ways to the current stream the one that makes no Python object of it: 0.1 us, not 1.9)
+            stream = torch._C._cuda_getCurrentRawStream(self._index)
         elif stream.device != self.device:
             raise ValueError(f"the stream is of {stream.device}, the plan of {self.device}")
-        if torch.cuda.current_device() == self.device.index:
-            status = fn(self._h, ctypes.byref(args), *more, stream.cuda_stream)
+        else:
+            stream = stream.cuda_stream
+        if torch.cuda.current_device() == self._index:
+            status = fn(self._h, *args, stream)
         else:
             with torch.cuda.device(self.device):
-                status = fn(self._h, ctypes.byref(args), *more, stream.cuda_stream)
+                status = fn(self._h, *args, stream)
         if status != OK:
             raise VerifyError(status, name)
 
@@ -166,20 +167,19 @@ class ChunkPlan(_Plan):
                          device, workspace)
 
     def _batch(self, k_pages, v_pages, page_table, new_off, kv_len, total_new, max_new, max_kv_len, status):
-        s = self.shape
-        n_pages, page = k_pages.shape[0], k_pages.shape[2]
+        s, i32 = self.shape, torch.int32
+        n_pages, _, page, _ = k_pages.shape
+        batch, width = page_table.shape
         dims = (n_pages, s.n_kv_heads, page, s.head_dim)
-        k, *strides = self._rows(k_pages, "k_pages", self.dtype, 4, dims)
-        v, *v_strides = self._rows(v_pages, "v_pages", self.dtype, 4, dims)
-        if strides != v_strides:
+        k, st = self._rows(k_pages, "k_pages", self.dtype, dims)
+        v, v_st = self._rows(v_pages, "v_pages", self.dtype, dims)
+        if st != v_st:
             raise ValueError("k_pages and v_pages are laid out differently")
-        batch = kv_len.shape[0]
-        table, stride = self._rows(page_table, "page_table", torch.int32, 2, (batch, page_table.shape[1]))
-        return ChunkBatch(batch, total_new, max_new, max_kv_len,
-                          self._flat(new_off, "new_off", torch.int32, (batch + 1,)),
-                          self._flat(kv_len, "kv_len", torch.int32, (batch,)),
-                          PagedCache(k, v, n_pages, page, *strides, table, page_table.shape[1], stride),
-                          None if status is None else self._flat(status, "status", torch.int32, (batch,)))
+        table, t_st = self._rows(page_table, "page_table", i32, (batch, width))
+        return ChunkBatch(batch, total_new, max_new, max_kv_len, self._flat(new_off, "new_off", i32, (batch + 1,)),
+                          self._flat(kv_len, "kv_len", i32, (batch,)),
+                          PagedCache(k, v, n_pages, page, st[0], st[1], st[2], table, width, t_st[0]),
+                          None if status is None else self._flat(status, "status", i32, (batch,)))
 
     def append(self, k_new, v_new, k_pages, v_pages, page_table, new_off, kv_len, *, max_new_in_batch, status=None,
                max_kv_len_in_batch=None, stream=None) -> None:
@@ -187,11 +187,12 @@ class ChunkPlan(_Plan):
         ``k_pages``, ``v_pages`` [pages][Hkv][page][D]."""
         s = self.shape
         dims = (k_new.shape[0], s.n_kv_heads, s.head_dim)
-        k, *k_strides = self._rows(k_new, "k_new", self.dtype, 3, dims)
-        v, *v_strides = self._rows(v_new, "v_new", self.dtype, 3, dims)
+        k, k_st = self._rows(k_new, "k_new", self.dtype, dims)
+        v, v_st = self._rows(v_new, "v_new", self.dtype, dims)
         b = self._batch(k_pages, v_pages, page_table, new_off, kv_len, dims[0], max_new_in_batch,
                         s.max_kv_len if max_kv_len_in_batch is None else max_kv_len_in_batch, status)
-        self._call(lib().respec_chunk_append, "respec_chunk_append", AppendArgs(b, k, v, *k_strides, *v_strides), stream)
+        a = AppendArgs(b, k, v, k_st[0], k_st[1], v_st[0], v_st[1])
+        self._call(lib().respec_chunk_append, "respec_chunk_append", (ctypes.byref(a),), stream)
 
     def attend(self, q, k_pages, v_pages, page_table, new_off, kv_len, out, *, max_new_in_batch, max_kv_len_in_batch,
                scale=None, status=None, stream=None) -> None:
@@ -199,17 +200,19 @@ class ChunkPlan(_Plan):
         tokens; ``scale`` defaults to 1 / sqrt(D)."""
         s = self.shape
         dims = (q.shape[0], s.n_q_heads, s.head_dim)
-        qp, *q_strides = self._rows(q, "q", self.dtype, 3, dims)
-        op, *o_strides = self._rows(out, "out", self.dtype, 3, dims)
+        qp, q_st = self._rows(q, "q", self.dtype, dims)
+        op, o_st = self._rows(out, "out", self.dtype, dims)
         if scale is not None and not scale > 0:
             raise ValueError("scale: a positive number expected")
         b = self._batch(k_pages, v_pages, page_table, new_off, kv_len, dims[0], max_new_in_batch, max_kv_len_in_batch,
                         status)
-        self._call(lib().respec_chunk_attn, "respec_chunk_attn",
-                   AttnArgs(b, qp, *q_strides, op, *o_strides, scale or 0.0), stream, self.workspace_ptr)
+        a = AttnArgs(b, qp, q_st[0], q_st[1], op, o_st[0], o_st[1], scale or 0.0)
+        self._call(lib().respec_chunk_attn, "respec_chunk_attn", (ctypes.byref(a), self.workspace_ptr), stream)
 
 
-SCORE_OUTPUTS = ("tok_logprob", "tok_rank", "lse", "entropy", "topk_id", "topk_logprob")
+# outputs of a scoring call: type, and whether they hold the top alternatives' columns
+SCORE_OUTPUTS = {"tok_logprob": (torch.float32, False), "tok_rank": (torch.int32, False), "lse": (torch.float32, False),
+                 "entropy": (torch.float32, False), "topk_id": (torch.int32, True), "topk_logprob": (torch.float32, True)}
 
 
 class ScorePlan(_Plan):
@@ -223,20 +226,17 @@ class ScorePlan(_Plan):
         ``outputs``: any of ``SCORE_OUTPUTS`` (``alloc_score_outputs``); missing ones are not written."""
         s = self.shape
         rows = logits.shape[0]
-        z, stride = self._rows(logits, "logits", self.dtype, 2, (rows, s.vocab))
-        a = ScoreArgs(rows, z, stride, None if token is None else self._flat(token, "token", torch.int32, (rows,)))
+        z, st = self._rows(logits, "logits", self.dtype, (rows, s.vocab))
+        tok = None if token is None else self._flat(token, "token", torch.int32, (rows,))
+        to = {}
         for name, t in outputs.items():
-            if name not in SCORE_OUTPUTS:
-                raise ValueError(f"unknown output {name}")
-            if t is not None:
-                setattr(a, name, self._flat(t, name, torch.int32 if name in ("tok_rank", "topk_id") else torch.float32,
-                                            (rows, s.topk_out) if name[:3] == "top" else (rows,)))
-        self._call(lib().respec_score, "respec_score", a, stream, self.workspace_ptr)
+            dtype, wide = SCORE_OUTPUTS[name]
+            to[name] = None if t is None else self._flat(t, name, dtype, (rows, s.topk_out) if wide else (rows,))
+        a = ScoreArgs(rows, z, st[0], tok, **to)
+        self._call(lib().respec_score, "respec_score", (ctypes.byref(a), self.workspace_ptr), stream)
 
 
 def alloc_score_outputs(*, rows, topk_out, device="cuda") -> dict:
     """Output tensors of one scoring call."""
-    f32, i32 = dict(dtype=torch.float32, device=device), dict(dtype=torch.int32, device=device)
-    return {"tok_logprob": torch.empty(rows, **f32), "tok_rank": torch.empty(rows, **i32),
-            "lse": torch.empty(rows, **f32), "entropy": torch.empty(rows, **f32),
-            "topk_id": torch.empty(rows, topk_out, **i32), "topk_logprob": torch.empty(rows, topk_out, **f32)}
+    return {name: torch.empty((rows, topk_out) if wide else (rows,), dtype=dtype, device=device)
+            for name, (dtype, wide) in SCORE_OUTPUTS.items()}

@@ -26,13 +26,11 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkBatch& c, int b) {
   return s;
 }
 
-// Byte offset of row r of a sequence within a KV head of the cache.  A page id out of
+// Byte offset, within a KV head of the cache, of row r of a sequence, in the page of id `id`.  An id out of
 // range (reported by report_status) reads page 0 instead.
-__device__ __forceinline__ int64_t row_offset(const ChunkBatch& c, const int32_t* table, uint32_t r) {
-  const uint32_t p = div_by(r, c.page);
-  const int32_t id = table[p];
+__device__ __forceinline__ int64_t offset_in(const ChunkBatch& c, int32_t id, uint32_t r) {
   const int64_t page = (uint32_t)id < (uint32_t)c.n_pages ? id : 0;
-  return page * c.page_stride + (int64_t)((uint64_t)(r - p * c.page.d) * c.row_stride);
+  return page * c.page_stride + (int64_t)((uint64_t)(r - div_by(r, c.page) * c.page.d) * c.row_stride);
 }
 
 // The sequence that owns packed token t (n = 0: none), by a whole wave: a lane per sequence.

@@ -23,8 +23,7 @@ __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
   constexpr int TK = 32;
   constexpr int KP = D * 4 + 16;       // bytes between K rows
   constexpr int VP = TK + 4;           // floats between V columns
-  constexpr int CPR = D / 4;           // 16-byte pieces of a row
-  constexpr int NP = TK * CPR / 256;   // ... per thread
+  constexpr int NP = TK * D / 4 / 256;  // 16-byte pieces of a tile per thread
   __shared__ __align__(16) unsigned char k_lds[2][TK * KP];
   __shared__ __align__(16) float v_lds[2][D * VP];
 
@@ -55,15 +54,19 @@ __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
   const char* kb = a.b.k + (int64_t)it.g * a.b.head_stride;
   const char* vb = a.b.v + (int64_t)it.g * a.b.head_stride;
 
-  // K: consecutive threads take consecutive pieces of a row; V: pieces of consecutive rows, so that the
-  // transposed stores meet every bank once
+  // A thread brings every eighth 16-byte piece of one row: one address per tile for all of them, and the transposed
+  // stores meet every bank once.  The row's page id is read another tile ahead.
+  const int my_row = (int)threadIdx.x % TK, my_piece = (int)threadIdx.x / TK;
   u32x4 kp[NP], vp[NP];
+  int32_t id = 0;
+  auto row_of = [&](int r0) { return (uint32_t)min(r0 + my_row, hi - 1); };
+  auto fetch_id = [&](int r0) { id = table[div_by(row_of(r0), a.b.page)]; };
   auto fetch = [&](int r0) {
+    const int64_t off = offset_in(a.b, id, row_of(r0)) + my_piece * 16;
 #pragma unroll
     for (int x = 0; x < NP; ++x) {
-      const int idx = (int)threadIdx.x + x * 256;
-      kp[x] = ld16(kb + row_offset(a.b, table, (uint32_t)min(r0 + idx / CPR, hi - 1)) + (idx % CPR) * 16);
-      vp[x] = ld16(vb + row_offset(a.b, table, (uint32_t)min(r0 + idx % TK, hi - 1)) + (idx / TK) * 16);
+      kp[x] = ld16(kb + off + x * (256 / TK * 16));
+      vp[x] = ld16(vb + off + x * (256 / TK * 16));
     }
   };
   float m = kNegInf, l = 0.f;
@@ -71,28 +74,38 @@ __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
 #pragma unroll
   for (int d = 0; d < DB; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+  fetch_id(lo);
   fetch(lo);
+  fetch_id(lo + TK);
   int buf = 0;
   for (int r0 = lo; r0 < hi; r0 += TK, buf ^= 1) {
     unsigned char* ks = k_lds[buf];
     float* vs = v_lds[buf];
 #pragma unroll
     for (int x = 0; x < NP; ++x) {
-      const int idx = (int)threadIdx.x + x * 256;
-      *reinterpret_cast<u32x4*>(ks + (idx / CPR) * KP + (idx % CPR) * 16) = kp[x];
+      const int c = my_piece + x * (256 / TK);
+      *reinterpret_cast<u32x4*>(ks + my_row * KP + c * 16) = kp[x];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) vs[((idx / TK) * 4 + e) * VP + idx % TK] = __uint_as_float(vp[x][e]);
+      for (int e = 0; e < 4; ++e) vs[(c * 4 + e) * VP + my_row] = __uint_as_float(vp[x][e]);
     }
     // (one barrier per tile: a wave that is here again has seen every wave past the tile between)
     __syncthreads();
-    if (r0 + TK < hi) fetch(r0 + TK);
-    f32x4 s[2];
+    if (r0 + TK < hi) {
+      fetch(r0 + TK);
+      fetch_id(r0 + 2 * TK);
+    }
+    // (neighbouring products are of different sums: one that waits for the product before it costs more)
+    f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < KC; ++c) {
+      f32x4 kf[2];
 #pragma unroll
-      for (int c = 0; c < KC; ++c)
-        s[u] = mma_k64(0.f, *reinterpret_cast<const u32x4*>(ks + (u * 16 + c16) * KP + c * 64 + g4 * 16), qf[c], s[u]);
+      for (int u = 0; u < 2; ++u) kf[u] = *reinterpret_cast<const f32x4*>(ks + (u * 16 + c16) * KP + c * 64 + g4 * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          s[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[u][e], __uint_as_float(qf[c][e]), s[u], 0, 0, 0);
     }
     float mx = kNegInf;
 #pragma unroll
@@ -126,19 +139,27 @@ __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
     const bool masked = __any(r0 + TK > end);
     bool odd = false;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        f32x4 vf = *reinterpret_cast<const f32x4*>(vs + (d * 16 + c16) * VP + u * 16 + g4 * 4);
-        if (masked) {
+      for (int d0 = 0; d0 < DB; d0 += 4) {
+        f32x4 vf[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (!(fabsf(vf[e]) < __builtin_huge_valf())) {
-              odd = true;
-              vf[e] = 0.f;
-            }
+        for (int d = 0; d < 4; ++d) {
+          vf[d] = *reinterpret_cast<const f32x4*>(vs + ((d0 + d) * 16 + c16) * VP + u * 16 + g4 * 4);
+          if (masked) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (!(fabsf(vf[d][e]) < __builtin_huge_valf())) {
+                odd = true;
+                vf[d][e] = 0.f;
+              }
+          }
         }
-        o[d] = mma_k64(0.f, __builtin_bit_cast(u32x4, vf), __builtin_bit_cast(u32x4, p[u]), o[d]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+            o[d0 + d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[d][e], p[u][e], o[d0 + d], 0, 0, 0);
       }
     if (__any(odd)) {  // whatever the weight, they make a NaN or an infinity of the sum
       for (int key = 0; key < TK; ++key)

@@ -4,8 +4,7 @@
 // Tiles go round an LDS ring by DMA, four of them per pass and barrier.
 #include <type_traits>
 
-#include "chunk_pages.hpp"
-#include "chunk_tile.hpp"
+#include "chunk_few.hpp"
 
 namespace respec {
 namespace {
@@ -28,17 +27,12 @@ struct WideShape {
 };
 
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a) {
+__device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, unsigned char* smem) {
   using G = WideShape<D>;
   using Feed = RowFeed<D, G::kRows>;
   constexpr int KS = D / 16, DB = D / 32, S = G::S, kPass = G::kPass, kRows = G::kRows, NR = Feed::NR;
-  extern __shared__ __align__(1024) unsigned char smem[];
-  if ((int)blockIdx.x >= a.wide.items) {
-    report_status<64 * kWaves>(a.b, (int)blockIdx.x - a.wide.items, true);
-    return;
-  }
   const ChunkGeom& ge = a.wide;
-  const Item it = find_item(a.b, ge, a.few_rows + 1, INT32_MAX, blockIdx.x);
+  const Item it = find_item(a.b, ge, a.few_rows + 1, INT32_MAX, x);
   const ChunkSeq& sq = it.seq;
   if (sq.n == 0) return;
   const int rows = sq.n * a.b.group, row0 = it.rb * ge.rows_per_wg;
@@ -176,23 +170,50 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_attn_wide_kernel(ChunkAt
   store_rows<D>(r[0], a, whole, it.split, tok, head, wrow + r32 < rows, lane);
 }
 
-template <int D>
+// MIXED: sequences of few query rows are there, too, and have workgroups of their own, of which four waves work (a
+// launch for each kind, one after the other: 13 sequences of 1-90 tokens over 146-217 rows, 28 heads on 4, 32.2 us,
+// like this 22.1; 9 of 1-307 over 352-564, 32 on 8, 47.3 and 38.8).
+template <int D, bool MIXED>
+__global__ __launch_bounds__(64 * kWaves, 1) void chunk_attn_wide_kernel(ChunkAttnArgs a) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  int x = (int)blockIdx.x;
+  if (x < a.wide.items) {
+    wide_rows_item<D>(a, x, smem);
+    return;
+  }
+  x -= a.wide.items;
+  if constexpr (MIXED) {
+    if (x < a.few.items) {
+      if (threadIdx.x < 256) few_rows_item<D, 1>(a, x, smem);
+      return;
+    }
+    x -= a.few.items;
+  }
+  report_status<64 * kWaves>(a.b, x, true);
+}
+
+template <int D, bool MIXED>
 hipError_t go(bool launch, const ChunkAttnArgs& a, bool status, hipStream_t s) {
+  constexpr int kLds = MIXED && FewShape<D>::kLds > WideShape<D>::kLds ? FewShape<D>::kLds : WideShape<D>::kLds;
   if (!launch)
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(&chunk_attn_wide_kernel<D>),
-                               hipFuncAttributeMaxDynamicSharedMemorySize, WideShape<D>::kLds);
-  hipLaunchKernelGGL(chunk_attn_wide_kernel<D>, dim3(a.wide.items + (status ? a.b.batch : 0)), dim3(64 * kWaves), WideShape<D>::kLds, s, a);
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&chunk_attn_wide_kernel<D, MIXED>),
+                               hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+  const int items = a.wide.items + (MIXED ? a.few.items : 0) + (status ? a.b.batch : 0);
+  hipLaunchKernelGGL((chunk_attn_wide_kernel<D, MIXED>), dim3(items), dim3(64 * kWaves), kLds, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_chunk_attn_wide(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s) {
-  return head_dim == 128 ? go<128>(true, a, status, s) : go<64>(true, a, status, s);
+hipError_t launch_chunk_attn_wide(int head_dim, const ChunkAttnArgs& a, bool mixed, bool status, hipStream_t s) {
+  if (mixed) return head_dim == 128 ? go<128, true>(true, a, status, s) : go<64, true>(true, a, status, s);
+  return head_dim == 128 ? go<128, false>(true, a, status, s) : go<64, false>(true, a, status, s);
 }
 hipError_t set_chunk_attn_wide_lds_limit(int head_dim) {
   const ChunkAttnArgs none{};
-  return head_dim == 128 ? go<128>(false, none, false, nullptr) : go<64>(false, none, false, nullptr);
+  const hipError_t e = head_dim == 128 ? go<128, false>(false, none, false, nullptr) : go<64, false>(false, none, false, nullptr);
+  if (e != hipSuccess) return e;
+  return head_dim == 128 ? go<128, true>(false, none, false, nullptr) : go<64, true>(false, none, false, nullptr);
 }
 
 }  // namespace respec

@@ -74,7 +74,6 @@ struct ChunkAttnArgs {
   int32_t few_rows;
   ChunkGeom few, wide;
 };
-constexpr int kFewRows = 64;   // of bf16 chunks; float32 has the second geometry only
 
 struct ScoreArgs {
   const void* z;
@@ -92,9 +91,9 @@ constexpr int kScoreParts = 512;  // workgroups that a few rows are cut into (65
 hipError_t launch_chunk_append(int es, int head_dim, const AppendArgs& a, hipStream_t s);
 // float32; `status`: whether this launch reports the sequences' status
 hipError_t launch_chunk_attn_f32(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s);
-// bf16: sequences of at most / more than kFewRows query rows per KV head
+// bf16: sequences of at most / more than few_rows query rows per KV head; mixed: of both kinds
 hipError_t launch_chunk_attn_few(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s);
-hipError_t launch_chunk_attn_wide(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s);
+hipError_t launch_chunk_attn_wide(int head_dim, const ChunkAttnArgs& a, bool mixed, bool status, hipStream_t s);
 hipError_t set_chunk_attn_few_lds_limit(int head_dim);
 hipError_t set_chunk_attn_wide_lds_limit(int head_dim);
 hipError_t launch_chunk_merge(int dtype, int head_dim, const ChunkAttnArgs& a, hipStream_t s);

@@ -90,9 +90,10 @@ struct Pace {
 // Splits of the sequences: the number n (at most `held`, each of `least` cache rows or more, in multiples of `unit`)
 // with the least estimated time  rounds * (rows / n * row + start) + merge,  rounds = items * n / CUs.  One
 // sequence's lengths are known, and its workgroups run in whole rounds; of a batch the host knows the longest
-// alone, so about a third of the work that longest sequences would be is assumed, and half a round of tail.
+// alone, so a third of the work that longest sequences would be is assumed, and half a round of tail.
 ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long long limit, int unit, int least, int per_cu, Pace pace,
                    int row_bytes, long long held) {
+  constexpr double kShare = 0.3;
   ChunkGeom g{rows_per_wg, 1, INT_MAX, 0};
   const long long items = blocks * b.n_kv_heads;
   double best = 0;
@@ -102,9 +103,9 @@ ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long 
     if (rows == rows_before) continue;
     rows_before = rows;
     const double wgs = (double)items * ceil_div(limit, std::max(rows, 1ll)) / (kCUs * per_cu);
-    const double rounds = b.batch == 1 ? ceil(wgs) : std::max(1.0, wgs * 0.3) + 0.5;
+    const double rounds = b.batch == 1 ? ceil(wgs) : std::max(1.0, wgs * kShare) + 0.5;
     const double joined = 1e-6 * n * b.total_new * b.n_kv_heads * b.group * row_bytes * 2 / 4.5;
-    const double merge = n == 1 ? 0 : 4 + joined * (b.batch == 1 ? 1 : 0.3);
+    const double merge = n == 1 ? 0 : 4 + joined * (b.batch == 1 ? 1 : kShare);
     const double t = rounds * (rows * pace.row + pace.start) + merge;
     if (n == 1 || t < best) {
       best = t;
@@ -230,28 +231,29 @@ respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chun
   auto blocks = [&](int per_wg) { return std::min(ceil_div(all_rows, per_wg) + (seqs > 1 ? seqs - 1 : 0), seqs * ceil_div(rows, per_wg)); };
   const int rb = (s.head_dim + 2) * 4;
   hipStream_t stm = static_cast<hipStream_t>(stream);
-  bool status = a.b.status != nullptr;  // (the first launch reports it)
+  const bool status = a.b.status != nullptr;
+  hipError_t e;
   if (s.dtype == RESPEC_F32) {
     a.few_rows = 0;
     a.few = ChunkGeom{1, 1, INT_MAX, 0};
-    a.wide = geometry(a.b, 64, blocks(64), limit, 32, 32, 4, s.head_dim == 128 ? Pace{0.2, 5} : Pace{0.1, 5}, rb, held);
+    a.wide = geometry(a.b, 64, blocks(64), limit, 32, 32, 4, Pace{0.2, 5}, rb, held);
     if ((long long)a.wide.items + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
-    if (launch_chunk_attn_f32(s.head_dim, a, status, stm) != hipSuccess) return RESPEC_ERR_HIP;
+    e = launch_chunk_attn_f32(s.head_dim, a, status, stm);
   } else {
-    a.few_rows = rows <= 32 ? 32 : kFewRows;
-    a.few = geometry(a.b, a.few_rows, seqs, limit, 128, 128, 1, s.head_dim == 128 ? Pace{0.02, 6} : Pace{0.01, 6}, rb, held);
-    a.wide = geometry(a.b, 256, blocks(256), limit, 128, 256, 1, s.head_dim == 128 ? Pace{0.032, 6} : Pace{0.018, 6}, rb, held);
-    if ((long long)a.few.items + a.b.batch > INT_MAX || (long long)a.wide.items + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
+    // Calls of at most 64 query rows per KV head have the few-row kernel, of one or two groups of 32; others have
+    // 256-row blocks, and sequences of up to 32 rows among them the few-row kernel's way in the same launch.
+    const bool wide = rows > 64, mixed = wide && a.b.batch > 1;
+    a.few_rows = !wide ? (rows <= 32 ? 32 : 64) : mixed ? 32 : 0;
+    a.few = !wide || mixed ? geometry(a.b, a.few_rows, seqs, limit, 128, 128, 1,
+                                      s.head_dim == 128 ? Pace{0.02, 6} : Pace{0.01, 6}, rb, held)
+                           : ChunkGeom{1, 1, INT_MAX, 0};
+    a.wide = wide ? geometry(a.b, 256, blocks(256), limit, 128, 256, 1, s.head_dim == 128 ? Pace{0.032, 6} : Pace{0.018, 6}, rb, held)
+                  : ChunkGeom{1, 1, INT_MAX, 0};
+    if ((long long)a.few.items + a.wide.items + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
     if (!raise_lds_limits(s.head_dim)) return RESPEC_ERR_HIP;
-    const bool any_wide = rows > a.few_rows, any_few = !any_wide || a.b.batch > 1;
-    if (any_wide) {
-      if (launch_chunk_attn_wide(s.head_dim, a, status, stm) != hipSuccess) return RESPEC_ERR_HIP;
-      status = false;
-    } else {
-      a.wide = a.few;
-    }
-    if (any_few && launch_chunk_attn_few(s.head_dim, a, status, stm) != hipSuccess) return RESPEC_ERR_HIP;
+    e = wide ? launch_chunk_attn_wide(s.head_dim, a, mixed, status, stm) : launch_chunk_attn_few(s.head_dim, a, status, stm);
   }
+  if (e != hipSuccess) return RESPEC_ERR_HIP;
   if (x.b.total_new > 0 && (a.few.nsplit > 1 || a.wide.nsplit > 1) &&
       launch_chunk_merge(s.dtype, s.head_dim, a, stm) != hipSuccess)
     return RESPEC_ERR_HIP;

@@ -34,7 +34,8 @@
  *    are reported per sequence in seq_status[b] (when it is not NULL): the kernels
  *    never trap and never touch memory outside the buffers described here.
  *    What a sequence with a non-zero status leaves in its own output rows is
- *    unspecified; other sequences are not affected.
+ *    unspecified, and so are those of sequences behind offsets that decrease (their
+ *    tokens may be another's, too); other sequences are not affected.
  *  - Rows of outputs behind the last sequence's tokens, and before the first's,
  *    keep what they held: total_new may exceed new_off[B] (a captured call that
  *    is replayed with fewer tokens).
@@ -65,7 +66,7 @@ typedef struct {
   int32_t max_batch;   /* capacity in sequences, at most RESPEC_CHUNK_MAX_BATCH               */
   int32_t max_new;     /* capacity in new tokens of all sequences of a call; max_new * Hq
                           < 2^31                                                              */
-  int32_t max_kv_len;  /* capacity in rows in front of a chunk, max_kv_len + max_new < 2^31   */
+  int32_t max_kv_len;  /* capacity in rows in front of a chunk, max_kv_len + max_new <= 2^30  */
 } respec_chunk_shape;
 
 /* A paged cache.  k and v are laid out alike; strides are in elements, each a

@@ -111,6 +111,7 @@ __device__ __forceinline__ Item find_item(const ChunkBatch& c, const ChunkGeom& 
       it.b = b0 + l;
       it.split = y / blocks;
       it.rb = blocks - 1 - (y - it.split * blocks);
+      if ((uint32_t)it.rb >= (uint32_t)blocks) return it;  // (offsets that overlap: more entries than 32 bits count)
       it.seq = ChunkSeq{__builtin_amdgcn_readlane(s.t0, l), __builtin_amdgcn_readlane(s.n, l),
                         __builtin_amdgcn_readlane(s.L, l), 0};
       return it;

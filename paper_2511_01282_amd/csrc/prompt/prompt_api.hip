@@ -36,6 +36,7 @@ long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 constexpr int kMaxSplits = 64;             // a lane of the merge per split
 constexpr size_t kMaxPartial = 1u << 25;    // columns of partials: 134 MB
 constexpr int kMaxStride = 1 << 24;
+constexpr int kMaxRows = 1 << 30;         // cache rows of a sequence: positions a tile further fit 32 bits
 
 // Checks of a stride in elements: non-negative and whole 16-byte pieces.
 bool stride_ok(int64_t s, int es) { return s >= 0 && s < (1ll << 50) && s * es % 16 == 0; }
@@ -87,7 +88,7 @@ struct Pace {
   double row, start;
 };
 
-// Splits of the sequences: the number n (at most `held`, each of `least` cache rows or more, in multiples of `unit`)
+// Splits of the sequences: the number n (of a coarser choice upwards; at most `held`, each of `least` cache rows or more, in multiples of `unit`)
 // with the least estimated time  rounds * (rows / n * row + start) + merge,  rounds = items * n / CUs.  One
 // sequence's lengths are known, and its workgroups run in whole rounds; of a batch the host knows the longest
 // alone, so a third of the work that longest sequences would be is assumed, and half a round of tail.
@@ -98,7 +99,7 @@ ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long 
   const long long items = blocks * b.n_kv_heads;
   double best = 0;
   long long most = std::min({ceil_div(limit, least), (long long)kMaxSplits, held, items > 0 ? (long long)INT_MAX / items : 1});
-  for (long long n = 1, rows_before = 0; n <= std::max(most, 1ll); ++n) {
+  for (long long n = 1, rows_before = 0; n <= std::max(most, 1ll); n += 1 + n / 6) {
     const long long rows = ceil_div(ceil_div(limit, n), unit) * unit;
     if (rows == rows_before) continue;
     rows_before = rows;
@@ -145,7 +146,7 @@ respec_status respec_chunk_create(const respec_chunk_shape* shape, respec_chunk_
   if (s.n_q_heads < 1 || s.n_q_heads > RESPEC_CHUNK_MAX_HEADS || s.n_kv_heads < 1 || s.n_q_heads % s.n_kv_heads != 0)
     return RESPEC_ERR_SHAPE;
   if (s.max_batch < 1 || s.max_batch > RESPEC_CHUNK_MAX_BATCH || s.max_new < 1 || s.max_kv_len < 0) return RESPEC_ERR_SHAPE;
-  if ((long long)s.max_new * s.n_q_heads > INT_MAX || (long long)s.max_new + s.max_kv_len > INT_MAX) return RESPEC_ERR_SHAPE;
+  if ((long long)s.max_new * s.n_q_heads > INT_MAX || (long long)s.max_new + s.max_kv_len > kMaxRows) return RESPEC_ERR_SHAPE;
   respec_chunk_plan* p = new (std::nothrow) respec_chunk_plan();
   if (!p) return RESPEC_ERR_CAPACITY;
   p->s = s;
@@ -223,6 +224,7 @@ respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chun
   a.part_m = reinterpret_cast<float*>(ws + o_bytes);
   a.part_l = reinterpret_cast<float*>(ws + o_bytes + m_bytes);
   a.scale_log2 = (float)(1.4426950408889634 * (x.scale > 0.f ? (double)x.scale : 1.0 / sqrt((double)s.head_dim)));
+  if (isinf(a.scale_log2)) return RESPEC_ERR_PARAM;
   const long long limit = (long long)a.b.max_kv + a.b.max_new;  // rows that the last token of the longest sequence sees
   const long long all_rows = (long long)a.b.total_new * a.b.group, rows = (long long)a.b.max_new * a.b.group;  // per KV head
   const long long seqs = std::min(a.b.batch, a.b.total_new);    // sequences that can have tokens

@@ -89,6 +89,10 @@ def test_attention(lib, name, dtype, heads, kv_heads, head_dim, page):
     (BF, [(300, 1000), (1, 3000), (40, 0)], 2, 1, 64, 48),
     (BF, [(700, 0)], 1, 2, 128, 700),            # several row blocks, one page
     (BF, [(4, 2049), (5, 2047)], 4, 4, 128, 33),
+    (BF, [(300, 1000), (1, 3000), (40, 0), (9, 2500)], 2, 4, 128, 16),   # both kinds in one launch, joined
+    (BF, [(16, 1500), (9, 70), (1, 129)], 2, 4, 64, 16),                 # up to 64 rows per head
+    (BF, [(8, 1500), (5, 4000)], 1, 8, 128, 40),
+    (BF, [(2, 6000)], 3, 16, 128, 128),          # 32 rows per head
     (F32, [(1, 5000)], 2, 2, 64, 16),
     (F32, [(90, 2000), (1, 100)], 1, 3, 128, 20),
 ])
@@ -114,7 +118,7 @@ def test_attention_in_place(lib):
 
 
 @pytest.mark.parametrize("dtype,head_dim", [(BF, 64), (BF, 128), (F32, 64), (F32, 128)])
-@pytest.mark.parametrize("sizes", [[(40, 25)], [(300, 10)], [(9, 1500)]])
+@pytest.mark.parametrize("sizes", [[(40, 25)], [(300, 10)], [(9, 1500)], [(20, 30)]])
 def test_rows_not_seen_have_no_part(lib, dtype, head_dim, sizes):
     """A new token's NaN or infinite key and value reach the tokens from it on, and none before."""
     c = pc.make(sizes, dtype=dtype, heads=4, kv_heads=2, head_dim=head_dim, page=16, seed=5)
@@ -175,9 +179,12 @@ def test_append(lib, name, dtype, heads, kv_heads, head_dim, page):
         assert torch.equal(k, want_k) and torch.equal(v, want_v)
 
 
-def test_many_sequences(lib):
-    """More sequences than a wave has lanes, many of them empty."""
+@pytest.mark.parametrize("longest", [0, 70])
+def test_many_sequences(lib, longest):
+    """More sequences than a wave has lanes, many of them empty; with longer chunks among them."""
     sizes = [((b * 7) % 4, (b * 13) % 50) for b in range(150)]
+    if longest:
+        sizes[3], sizes[100] = (longest, 200), (longest - 3, 0)
     c = pc.make(sizes, heads=2, kv_heads=1, head_dim=64, page=16, seed=2, stale=0.0)
     _close(_attend(lib, c), *pc.attention(c))
     k, v, st = _append(lib, c)
@@ -392,6 +399,43 @@ def test_captured_chain_replays(lib):
         assert torch.equal(cache[0], e_cache[0]) and torch.equal(cache[1], e_cache[1])
         for name in results:
             assert torch.equal(results[name][lo:hi], e_results[name][lo:hi]), (k, name)
+
+
+def test_nothing_to_do(lib):
+    """No sequences, and sequences without tokens: nothing is written but their status."""
+    for sizes in ([], [(0, 5), (0, 0)]):
+        c = pc.make(sizes, heads=4, kv_heads=2, head_dim=64, page=16)
+        plan = _plan(lib, c, max_batch=2, max_new=4, max_kv_len=10)
+        st = torch.full((len(sizes),), -9, dtype=torch.int32, device="cuda")
+        out = torch.full((4, 4, 64), 7.0, dtype=BF, device="cuda")
+        cache = _cache(c)
+        before = cache[0].clone()
+        kw = dict(max_new_in_batch=0, status=st)
+        plan.attend(out[:0], *cache, out[:0], max_kv_len_in_batch=10, **kw)
+        assert st.tolist() == [0] * len(sizes)
+        st.fill_(-9)
+        plan.append(c.k_new.cuda(), c.v_new.cuda(), *cache, **kw)
+        assert st.tolist() == [0] * len(sizes) and bool((out == 7.0).all())
+        assert torch.equal(cache[0].nan_to_num(3.0), before.nan_to_num(3.0))
+    prompt, binding = lib
+    score = prompt.ScorePlan(vocab=100, max_rows=4, device="cuda:0")
+    score.score(torch.zeros(0, 100, device="cuda"), None, prompt.alloc_score_outputs(rows=0, topk_out=8))
+
+
+def test_two_plans_at_once(lib):
+    """Calls that overlap on two streams, a workspace each."""
+    cases = [pc.make([(1, 4000), (70, 600)], heads=8, kv_heads=2, head_dim=d, page=16, seed=20 + d) for d in (64, 128)]
+    runs = []
+    for c in cases:
+        q = c.q.cuda()
+        runs.append((_plan(lib, c), q, _cache(c), torch.empty_like(q), torch.cuda.Stream(), c))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for plan, q, cache, out, stream, c in runs:
+            plan.attend(q, *cache, out, max_new_in_batch=c.max_new, max_kv_len_in_batch=c.max_kv, stream=stream)
+    torch.cuda.synchronize()
+    for plan, q, cache, out, stream, c in runs:
+        _close(out.cpu(), *pc.attention(c))
 
 
 def test_results_repeat_on_another_stream(lib):

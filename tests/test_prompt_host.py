@@ -73,8 +73,8 @@ def _chunk_shape(p, **over):
 @pytest.mark.parametrize("over,status", [
     ({}, OK), ({"dtype": 2}, DTYPE), ({"head_dim": 96}, SHAPE), ({"n_q_heads": 7}, SHAPE), ({"n_kv_heads": 0}, SHAPE),
     ({"n_q_heads": 512}, SHAPE), ({"max_batch": 0}, SHAPE), ({"max_batch": 65536}, SHAPE), ({"max_new": 0}, SHAPE),
-    ({"max_kv_len": -1}, SHAPE), ({"max_new": 1 << 28}, SHAPE), ({"max_kv_len": 2**31 - 1}, SHAPE),
-    ({"max_kv_len": 2**31 - 101}, OK), ({"dtype": 0, "head_dim": 128, "n_kv_heads": 8}, OK),
+    ({"max_kv_len": -1}, SHAPE), ({"max_new": 1 << 28}, SHAPE), ({"max_kv_len": 2**30 - 99}, SHAPE),
+    ({"max_kv_len": 2**30 - 100}, OK), ({"dtype": 0, "head_dim": 128, "n_kv_heads": 8}, OK),
 ])
 def test_chunk_create(p, over, status):
     st, h = _create(p, "chunk", _chunk_shape(p, **over))
@@ -144,7 +144,7 @@ def test_append_refusals(p, over, status):
     ({"q": None}, NULL), ({"out": None}, NULL), ({"q": FAKE + 8}, SHAPE), ({"out": FAKE + 8}, SHAPE),
     ({"q_token_stride": 4}, SHAPE), ({"q_head_stride": -8}, SHAPE), ({"out_token_stride": 2}, SHAPE),
     ({"out_head_stride": 68}, SHAPE), ({"scale": -1.0}, PARAM), ({"scale": float("nan")}, PARAM),
-    ({"scale": float("inf")}, PARAM),
+    ({"scale": float("inf")}, PARAM), ({"scale": 3e38}, PARAM),
 ])
 def test_attn_refusals(p, over, status):
     _, h = _create(p, "chunk", _chunk_shape(p))

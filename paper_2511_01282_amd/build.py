@@ -23,7 +23,7 @@ FLAGS = [
 
 # matrix products accumulate in ordinary registers, on which the softmax works (accumulation registers would be moved to
 # and fro)
-FILE_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for f in ("chunk_attn_wide.hip", "chunk_attn_few.hip")}
+FILE_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for f in ("chunk_attn.hip", "chunk_attn_wide.hip", "chunk_attn_few.hip")}
 
 
 CXX = os.environ.get("CXX", "g++")

@@ -47,6 +47,9 @@ __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
   const int i = (int)div_by((uint32_t)rowc, a.group), hh = rowc - i * a.b.group;
   const int end = min(sq.L + i + 1, hi);  // cache rows that this lane's row sees end here, within the split
   const int64_t t = sq.t0 + i, head = (int64_t)it.g * a.b.group + hh;
+  // cache rows that every row of the wave sees end here
+  const int unmasked = __builtin_amdgcn_readfirstlane(
+      min(sq.L + (int)div_by((uint32_t)min(row0 + wave * 16, rows - 1), a.group) + 1, hi));
   u32x4 qf[KC];
 #pragma unroll
   for (int c = 0; c < KC; ++c) qf[c] = ld16(a.q + t * a.q_tok + head * a.q_head + c * 64 + g4 * 16);
@@ -107,12 +110,19 @@ __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
         for (int u = 0; u < 2; ++u)
           s[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[u][e], __uint_as_float(qf[c][e]), s[u], 0, 0, 0);
     }
+    f32x4 vf[2][DB];  // (under way beside the weights)
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int d = 0; d < DB; ++d) vf[u][d] = *reinterpret_cast<const f32x4*>(vs + (d * 16 + c16) * VP + u * 16 + g4 * 4);
+    const bool masked = r0 + TK > unmasked;  // (uniform) some row of the wave does not see the whole tile
     float mx = kNegInf;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        s[u][e] = r0 + u * 16 + g4 * 4 + e < end ? s[u][e] * a.scale_log2 : kNegInf;
+        s[u][e] *= a.scale_log2;
+        if (masked) s[u][e] = r0 + u * 16 + g4 * 4 + e < end ? s[u][e] : kNegInf;
         mx = fmaxf(mx, s[u][e]);
       }
     mx = fmaxf(mx, xchg<4>(mx));
@@ -136,32 +146,32 @@ __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
     // V^T P^T.  A masked weight is zero, and zero times a NaN or an infinity is not: in a tile that
     // some row does not see whole, values that are not finite stay out of the products and are added
     // afterwards for the rows that see them.
-    const bool masked = __any(r0 + TK > end);
     bool odd = false;
+    if (masked) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = max(top, __float_as_uint(vf[u][d][e]) & 0x7FFFFFFFu);
+      odd = __any(top >= 0x7F800000u);
+      if (odd) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vf[u][d][e] = fabsf(vf[u][d][e]) < __builtin_huge_valf() ? vf[u][d][e] : 0.f;
+      }
+    }
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int d0 = 0; d0 < DB; d0 += 4) {
-        f32x4 vf[4];
+      for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          vf[d] = *reinterpret_cast<const f32x4*>(vs + ((d0 + d) * 16 + c16) * VP + u * 16 + g4 * 4);
-          if (masked) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (!(fabsf(vf[d][e]) < __builtin_huge_valf())) {
-                odd = true;
-                vf[d][e] = 0.f;
-              }
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int d = 0; d < 4; ++d)
-            o[d0 + d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[d][e], p[u][e], o[d0 + d], 0, 0, 0);
-      }
-    if (__any(odd)) {  // whatever the weight, they make a NaN or an infinity of the sum
+        for (int d = 0; d < DB; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[u][d][e], p[u][e], o[d], 0, 0, 0);
+    if (odd) {  // whatever the weight, they make a NaN or an infinity of the sum
       for (int key = 0; key < TK; ++key)
 #pragma unroll
         for (int d = 0; d < DB; ++d)

@@ -15,7 +15,8 @@ namespace {
 // lane l, the scores of row l % 16 with keys 4 (l / 16) .. + 3 of 16, which are the B operand of O^T += V^T P^T as
 // they stand.  A tile of 32 cache rows is fetched into registers while the tile before is worked on, then goes to
 // one of two LDS buffers, K rows as they are and V transposed.  The matrix cores bound it: 32 clocks per product
-// of 2048 operations.
+// of 2048 operations.  Measured: 1500 tokens, 16 heads of 64, 66 us and 7 us for the merge (4.6 GFLOP: 71 TFLOP/s, where
+// a large float32 matrix product reaches 154); one token of 4 heads over 512 rows, 7.2 us.
 template <int D>
 __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
   constexpr int KC = D / 16;           // 64-byte K-chunks of a head row
@@ -202,83 +203,107 @@ __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
   }
 }
 
-// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over a row's splits, M = max_s m_s.  A row (token
-// and head) is joined by WPR waves, each a part of its splits, eight at a time; rows of one split are
-// written already.
-template <typename T, int D, int WPR>
+constexpr int kMergeMany = 16;  // splits of a sequence above which a row has a workgroup of the merge
+
+// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over a row's splits, M = max_s m_s.  A row is a (token, head)
+// pair; D / 4 lanes take four of its columns each.  Rows of few splits: such a group of lanes per row, four splits at a
+// time with a running M.  Rows of more: all the groups of the workgroup take splits of one row, each all of its own at
+// once, and are joined through LDS.  Rows of one split are written already.
+//
+// Bound by the partials' bytes where there are many rows: 512 tokens of 32 heads of 128 in 4 splits (38 MB), 9.8 us, 3.9 TB/s;
+// 1500 tokens of 16 heads of 64, 6.8 us (a wave per row with a lane per split: 11.8; workgroups per row from 5 splits
+// on: 103 us for the whole call, not 69).  One token of 28 heads in 64 splits (0.9 MB): 4.4 us (four at a time, all groups: 5.8).
+template <typename T, int D>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkAttnArgs a) {
-  constexpr int E = D / 64, RPW = 4 / WPR;  // columns per lane, rows per workgroup
-  __shared__ float part[4][D];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % WPR;
+  constexpr int G = D / 4, NG = 256 / G;
+  __shared__ __align__(16) float part[NG][D];
+  const int c = threadIdx.x % G, g = threadIdx.x / G, lane = threadIdx.x & 63;
   int b;
   const ChunkSeq sq = seq_of_token(a.b, blockIdx.x, b);
   if (sq.n == 0) return;
   const int hq = a.b.n_kv_heads * a.b.group, i = (int)blockIdx.x - sq.t0;
   const ChunkGeom& ge = sq.n * a.b.group <= a.few_rows ? a.few : a.wide;
   if (sq.L + sq.n <= ge.split_rows) return;
-  for (int h0 = (int)blockIdx.y * RPW; h0 < hq; h0 += gridDim.y * RPW) {
-    const int h = min(h0 + wave / WPR, hq - 1), hh = h - (int)div_by((uint32_t)h, a.group) * a.b.group;
+  const bool many = (sq.L + sq.n - 1) / ge.split_rows >= kMergeMany;  // (1 + that: the splits)
+  const int per = many ? 1 : NG;
+  const int64_t step = (int64_t)a.b.total_new * hq;  // rows between a row's splits
+  for (int h0 = (int)blockIdx.y * per; h0 < hq; h0 += gridDim.y * per) {
+    const int h = many ? h0 : min(h0 + g, hq - 1), hh = h - (int)div_by((uint32_t)h, a.group) * a.b.group;
     const int limit = block_limit(a, ge, sq, (i * a.b.group + hh) / ge.rows_per_wg);
     const int ns = (limit - 1) / ge.split_rows + 1;  // (at most 64)
-    if (WPR == 1 && ns <= 1) continue;
-    const int64_t step = (int64_t)a.b.total_new * hq, pr = (int64_t)blockIdx.x * hq + h;
-    const float* o = a.part_o + pr * D + lane * E;
-    float x[8][E];
-    auto fetch = [&](int s0) {
+    if (ns <= 1) continue;                           // (where `many`: the whole workgroup)
+    const int64_t pr = (int64_t)blockIdx.x * hq + h;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    if (many) {
+      constexpr int U = 64 / NG;
+      f32x4 o[U];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const float* q = o + min(s0 + u, ns - 1) * step * D;
-        if constexpr (E == 2) *reinterpret_cast<float2*>(x[u]) = *reinterpret_cast<const float2*>(q);
-        else x[u][0] = *q;
-      }
-    };
-    fetch(w * 8);  // (under way beside the weights)
-    const float ms = lane < ns ? a.part_m[lane * step + pr] : kNegInf, ls = lane < ns ? a.part_l[lane * step + pr] : 0.f;
-    const float M = wave_max(ms);
-    float wt = ms == kNegInf ? 0.f : exp2f(ms - M);
-    const float lt = wave_sum(wt * ls);
-    wt /= lt;
-    float acc[E];
+      for (int u = 0; u < U; ++u)
+        if (g + u * NG < ns) o[u] = *reinterpret_cast<const f32x4*>(a.part_o + ((g + u * NG) * step + pr) * D + c * 4);
+      const float ms = lane < ns ? a.part_m[lane * step + pr] : kNegInf, ls = lane < ns ? a.part_l[lane * step + pr] : 0.f;
+      const float M = wave_max(ms);
+      float wt = ms == kNegInf ? 0.f : exp2f(ms - M);  // of split `lane`
+      wt /= wave_sum(wt * ls);
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    for (int s0 = w * 8; s0 < ns; s0 += WPR * 8) {
-      if (s0 > w * 8) fetch(s0);
+      for (int u = 0; u < U; ++u) {
+        const float w = __shfl(wt, g + u * NG, 64);
+        if (g + u * NG < ns) {
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const float ws = __shfl(wt, min(s0 + u, 63), 64);
-        if (s0 + u < ns) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) acc[e] += ws * x[u][e];
+          for (int x = 0; x < 4; ++x) acc[x] = __builtin_fmaf(w, o[u][x], acc[x]);
         }
       }
-    }
-    if constexpr (WPR > 1) {
+      __syncthreads();  // (the row before has been read)
+      *reinterpret_cast<f32x4*>(&part[g][c * 4]) = acc;
       __syncthreads();
+      if (g != 0) continue;
 #pragma unroll
-      for (int e = 0; e < E; ++e) part[wave][lane * E + e] = acc[e];
-      __syncthreads();
-      if (w == 0) {
+      for (int k = 1; k < NG; ++k) acc += *reinterpret_cast<const f32x4*>(&part[k][c * 4]);
+    } else {
+      float M = kNegInf, l = 0.f;
+      for (int s0 = 0; s0 < ns; s0 += 4) {
+        f32x4 o[4];
+        float m[4], lw[4];
 #pragma unroll
-        for (int x = 1; x < WPR; ++x)
+        for (int u = 0; u < 4; ++u) {
+          const int64_t r = min(s0 + u, ns - 1) * step + pr;
+          o[u] = *reinterpret_cast<const f32x4*>(a.part_o + r * D + c * 4);
+          m[u] = a.part_m[r];
+          lw[u] = a.part_l[r];
+        }
+        const float to = fmaxf(fmaxf(fmaxf(M, m[0]), fmaxf(m[1], m[2])), m[3]), ref = to == kNegInf ? 0.f : to;
+        const float e = exp2f(M - ref);
+        l *= e;
+        acc *= e;
+        M = to;
 #pragma unroll
-          for (int e = 0; e < E; ++e) acc[e] += part[wave + x][lane * E + e];
+        for (int u = 0; u < 4; ++u) {
+          if (s0 + u < ns) {
+            const float w = m[u] == kNegInf ? 0.f : exp2f(m[u] - ref);
+            l = __builtin_fmaf(w, lw[u], l);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) acc[x] = __builtin_fmaf(w, o[u][x], acc[x]);
+          }
+        }
       }
+      acc /= l;
+      if (h0 + g >= hq) continue;
     }
-    if (w != 0 || ns <= 1 || h0 + wave / WPR >= hq) continue;
     char* to = a.out + (int64_t)blockIdx.x * a.o_tok + (int64_t)h * a.o_head;
+    if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<f32x4*>(to + c * 16) = acc;
+    } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) Elem<T>::store(to, lane * E + e, acc[e]);
+      for (int x = 0; x < 4; ++x) Elem<T>::store(to, c * 4 + x, acc[x]);
+    }
   }
 }
 
 template <typename T, int D>
 hipError_t go_merge(const ChunkAttnArgs& a, hipStream_t s) {
-  const int hq = a.b.n_kv_heads * a.b.group;
-  // many splits: a row's are read by four waves at once; many tokens: a workgroup takes several heads of its own
-  const bool many = max(a.few.nsplit, a.wide.nsplit) > 16;
-  const int per_tok = many ? hq : (hq + 3) / 4, y = max(1, min(per_tok, 16384 / a.b.total_new));
-  if (many) hipLaunchKernelGGL((chunk_merge_kernel<T, D, 4>), dim3(a.b.total_new, y), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((chunk_merge_kernel<T, D, 1>), dim3(a.b.total_new, y), dim3(256), 0, s, a);
+  // rows of many tokens have several heads to a workgroup
+  const int hq = a.b.n_kv_heads * a.b.group, per = max(a.few.nsplit, a.wide.nsplit) > kMergeMany ? 1 : 1024 / D;
+  const int y = max(1, min((hq + per - 1) / per, 16384 / a.b.total_new));
+  hipLaunchKernelGGL((chunk_merge_kernel<T, D>), dim3(a.b.total_new, y), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -86,7 +86,8 @@ struct ScoreArgs {
 constexpr int kAppendMaxTok = 16;  // tokens of an append workgroup
 constexpr int kScoreWords = 4;  // m, S, T, rank count
 constexpr int kScoreMaxKeys = 256;
-constexpr int kScoreParts = 512;  // workgroups that a few rows are cut into (65 rows of 152064 float32 logits: 384 20.4 us, 512 18.9, 1024 19.7)
+constexpr int kScoreParts = 512;  // workgroups that a few rows are cut into (65 rows of 152064 float32
+                                  // logits: 384 20.4 us, 512 18.9, 1024 19.7)
 
 hipError_t launch_chunk_append(int es, int head_dim, const AppendArgs& a, hipStream_t s);
 // float32; `status`: whether this launch reports the sequences' status

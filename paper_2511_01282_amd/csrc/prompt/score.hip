@@ -11,6 +11,11 @@
 // of the threads' maxima, H, is at most the K-th largest logit, so every one of the top K is in a vector
 // of one of the few threads whose maximum reaches H; only those threads' vectors are read again.
 //
+// Memory bounds it, with the vector instructions close behind (93% of their issue slots): 2048 rows of 128256 bf16
+// logits (526 MB), 114 us, 4.6 TB/s; 65 rows of 152064 float32 logits (40 MB, in parts), 15.5 us and 3.9 us to join them.
+// (Steps without the bounds' selects, the rank counted by the scalar unit and the best vector read again took fewer
+// vector instructions, and 121 and 18.7 us against 114 and 19.0.)
+//
 // Keys: (value, id) pairs as 64-bit integers (common.hpp), all distinct, so ties go to the lowest id.
 #include "topk.hpp"
 #include "prompt.hpp"

@@ -70,6 +70,18 @@ __device__ __forceinline__ void report_status(const ChunkBatch& c, int b, bool f
   if (threadIdx.x == 0) c.status[b] = s.status ? s.status : (bad ? kStPage : 0);
 }
 
+__device__ __forceinline__ int wave_prefix_sum(int v) {  // inclusive
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // from 1, 2, 4 and 8 lanes below in rows of 16,
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // lanes 15 and 47 to the rows after theirs,
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // and lane 31 to the upper half
+  return v;
+}
+
+__device__ __forceinline__ int row_block(const ChunkGeom& ge, int row) { return row >> __builtin_ctz(ge.rows_per_wg); }
+
 // A workgroup's item.  Item x is of KV head x % Hkv (a head's workgroups meet on one XCD where the heads are a
 // multiple of 8, and read its tiles at about the same time) and entry x / Hkv of the list of (sequence, split, row
 // block), a block's rows descending: the longest first.  A sequence of `rows` query rows from `least` to `most`
@@ -81,8 +93,8 @@ struct Item {
 };
 __device__ __forceinline__ Item find_item(const ChunkBatch& c, const ChunkGeom& ge, int least, int most, int x) {
   const int lane = (int)(threadIdx.x & 63);
-  Item it{0, x % c.n_kv_heads, 0, 0, ChunkSeq{0, 0, 0, 0}};
-  int y = x / c.n_kv_heads;
+  int y = (int)div_by((uint32_t)x, c.kv_heads);
+  Item it{0, x - y * c.n_kv_heads, 0, 0, ChunkSeq{0, 0, 0, 0}};
   for (int b0 = 0; b0 < c.batch; b0 += 64) {
     ChunkSeq s{0, 0, 0, 0};
     int blocks = 0, splits = 1;
@@ -90,26 +102,20 @@ __device__ __forceinline__ Item find_item(const ChunkBatch& c, const ChunkGeom& 
       s = chunk_seq(c, b0 + lane);
       const int rows = s.n * c.group;
       if (rows >= least && rows <= most) {
-        blocks = (rows - 1) / ge.rows_per_wg + 1;
-        splits = (s.L + s.n - 1) / ge.split_rows + 1;
+        blocks = row_block(ge, rows - 1) + 1;
+        splits = (int)div_by((uint32_t)(s.L + s.n - 1), ge.split) + 1;
       }
     }
     // (a lane's entries: at most n_rowblk * nsplit; 64 lanes' fit 32 bits, as the grid does)
     int incl = blocks * splits;
-    if (c.batch > 1) {
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int z = __shfl_up(incl, o, 64);
-        incl += lane >= o ? z : 0;
-      }
-    }
+    if (c.batch > 1) incl = wave_prefix_sum(incl);
     const uint64_t past = __ballot(y < incl);
     if (past) {
       const int l = __builtin_ctzll(past);
       blocks = __builtin_amdgcn_readlane(blocks, l);
       y -= __builtin_amdgcn_readlane(incl, l) - blocks * __builtin_amdgcn_readlane(splits, l);
       it.b = b0 + l;
-      it.split = y / blocks;
+      it.split = __popcll(__ballot((uint32_t)(lane + 1) * (uint32_t)blocks <= (uint32_t)y));  // y / blocks, at most 63
       it.rb = blocks - 1 - (y - it.split * blocks);
       if ((uint32_t)it.rb >= (uint32_t)blocks) return it;  // (offsets that overlap: more entries than 32 bits count)
       it.seq = ChunkSeq{__builtin_amdgcn_readlane(s.t0, l), __builtin_amdgcn_readlane(s.n, l),

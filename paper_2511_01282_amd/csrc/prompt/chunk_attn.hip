@@ -224,13 +224,13 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkAttnArgs a) {
   const int hq = a.b.n_kv_heads * a.b.group, i = (int)blockIdx.x - sq.t0;
   const ChunkGeom& ge = sq.n * a.b.group <= a.few_rows ? a.few : a.wide;
   if (sq.L + sq.n <= ge.split_rows) return;
-  const bool many = (sq.L + sq.n - 1) / ge.split_rows >= kMergeMany;  // (1 + that: the splits)
+  const bool many = (int)div_by((uint32_t)(sq.L + sq.n - 1), ge.split) >= kMergeMany;  // (1 + that: the splits)
   const int per = many ? 1 : NG;
   const int64_t step = (int64_t)a.b.total_new * hq;  // rows between a row's splits
   for (int h0 = (int)blockIdx.y * per; h0 < hq; h0 += gridDim.y * per) {
     const int h = many ? h0 : min(h0 + g, hq - 1), hh = h - (int)div_by((uint32_t)h, a.group) * a.b.group;
-    const int limit = block_limit(a, ge, sq, (i * a.b.group + hh) / ge.rows_per_wg);
-    const int ns = (limit - 1) / ge.split_rows + 1;  // (at most 64)
+    const int limit = block_limit(a, ge, sq, row_block(ge, i * a.b.group + hh));
+    const int ns = (int)div_by((uint32_t)(limit - 1), ge.split) + 1;  // (at most 64)
     if (ns <= 1) continue;                           // (where `many`: the whole workgroup)
     const int64_t pr = (int64_t)blockIdx.x * hq + h;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};

@@ -101,7 +101,7 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
     asm volatile("s_barrier" ::: "memory");
   };
   static_assert(G::kAhead <= 3, "landed() tells two newer units apart");
-#pragma unroll
+#pragma unroll 1
   for (int u = -1; u < G::kAhead; ++u) request();
 
   Rows<D> r[1];
@@ -163,7 +163,7 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
   for (; j < np; ++j) {
     if (j > 0) landed(j);
     request();
-#pragma unroll
+#pragma unroll 1
     for (int u = 0; u < kPass; u += 2) {
       const int t = kPass * j + u;
       using Yes = std::integral_constant<bool, true>;

@@ -41,6 +41,7 @@ struct ChunkBatch {
   FastDiv page;            // rows per page
   int32_t batch, total_new, max_new, max_kv, n_pages, table_width;
   int32_t n_kv_heads, group;
+  FastDiv kv_heads;        // by n_kv_heads
 };
 
 struct AppendArgs {
@@ -54,10 +55,11 @@ struct AppendArgs {
 
 // How an attention kernel cuts its sequences: a workgroup per (row block, split, KV head, sequence).
 struct ChunkGeom {
-  int32_t rows_per_wg;  // query rows, (token, head-in-group) pairs, of a block
+  int32_t rows_per_wg;  // query rows, (token, head-in-group) pairs, of a block: a power of two
   int32_t nsplit;       // splits of the longest sequence; 1: no partials
   int32_t split_rows;   // cache rows of a split
   int32_t items;        // grid: (row block, split, sequence, KV head), see find_item
+  FastDiv split;        // by split_rows
 };
 
 struct ChunkAttnArgs {

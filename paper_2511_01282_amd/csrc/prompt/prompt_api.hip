@@ -80,6 +80,7 @@ ChunkBatch device_batch(const respec_chunk_plan* plan, const respec_chunk_batch&
   d.table_width = c.table_width;
   d.n_kv_heads = plan->s.n_kv_heads;
   d.group = plan->s.n_q_heads / plan->s.n_kv_heads;
+  d.kv_heads = fast_div((uint32_t)d.n_kv_heads);
   return d;
 }
 
@@ -95,7 +96,7 @@ struct Pace {
 ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long long limit, int unit, int least, int per_cu, Pace pace,
                    int row_bytes, long long held) {
   constexpr double kShare = 0.3;
-  ChunkGeom g{rows_per_wg, 1, INT_MAX, 0};
+  ChunkGeom g{rows_per_wg, 1, INT_MAX, 0, fast_div(INT_MAX)};
   const long long items = blocks * b.n_kv_heads;
   double best = 0;
   long long most = std::min({ceil_div(limit, least), (long long)kMaxSplits, held, items > 0 ? (long long)INT_MAX / items : 1});
@@ -113,6 +114,7 @@ ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long 
       g.split_rows = n == 1 || rows >= limit ? INT_MAX : (int)rows;
     }
   }
+  g.split = fast_div((uint32_t)g.split_rows);
   g.nsplit = g.split_rows == INT_MAX ? 1 : (int)ceil_div(limit, g.split_rows);
   g.items = (int)std::min(items * g.nsplit, (long long)INT_MAX);
   return g;
@@ -237,7 +239,7 @@ respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chun
   hipError_t e;
   if (s.dtype == RESPEC_F32) {
     a.few_rows = 0;
-    a.few = ChunkGeom{1, 1, INT_MAX, 0};
+    a.few = ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
     a.wide = geometry(a.b, 64, blocks(64), limit, 32, 32, 4, Pace{0.2, 5}, rb, held);
     if ((long long)a.wide.items + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
     e = launch_chunk_attn_f32(s.head_dim, a, status, stm);
@@ -248,9 +250,9 @@ respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chun
     a.few_rows = !wide ? (rows <= 32 ? 32 : 64) : mixed ? 32 : 0;
     a.few = !wide || mixed ? geometry(a.b, a.few_rows, seqs, limit, 128, 128, 1,
                                       s.head_dim == 128 ? Pace{0.02, 6} : Pace{0.01, 6}, rb, held)
-                           : ChunkGeom{1, 1, INT_MAX, 0};
+                           : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
     a.wide = wide ? geometry(a.b, 256, blocks(256), limit, 128, 256, 1, s.head_dim == 128 ? Pace{0.032, 6} : Pace{0.018, 6}, rb, held)
-                  : ChunkGeom{1, 1, INT_MAX, 0};
+                  : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
     if ((long long)a.few.items + a.wide.items + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
     if (!raise_lds_limits(s.head_dim)) return RESPEC_ERR_HIP;
     e = wide ? launch_chunk_attn_wide(s.head_dim, a, mixed, status, stm) : launch_chunk_attn_few(s.head_dim, a, status, stm);

@@ -92,10 +92,11 @@ struct Pace {
 // Splits of the sequences: the number n (of a coarser choice upwards; at most `held`, each of `least` cache rows or more, in multiples of `unit`)
 // with the least estimated time  rounds * (rows / n * row + start) + merge,  rounds = items * n / CUs.  One
 // sequence's lengths are known, and its workgroups run in whole rounds; of a batch the host knows the longest
-// alone, so a third of the work that longest sequences would be is assumed, and half a round of tail.
+// alone, so half the work that longest sequences would be is assumed, and half a round of tail
+// (80 drawn batches of chunks, geometric mean: a third 30.5 us, 0.4 29.5, 0.5 29.4, 0.8 29.2; of decoding tokens 21.8, 21.2, 21.8, 21.9).
 ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long long limit, int unit, int least, int per_cu, Pace pace,
                    int row_bytes, long long held) {
-  constexpr double kShare = 0.3;
+  constexpr double kShare = 0.5;
   ChunkGeom g{rows_per_wg, 1, INT_MAX, 0, fast_div(INT_MAX)};
   const long long items = blocks * b.n_kv_heads;
   double best = 0;

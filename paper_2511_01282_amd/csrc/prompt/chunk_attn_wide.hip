@@ -3,11 +3,11 @@
 // Eight waves, two per SIMD, own 32 query rows each and walk over the same cache rows, tile by tile of 32.
 // Tiles go round an LDS ring by DMA, four of them per pass and barrier.
 //
-// The matrix cores bound it, and on long prompts the card's power: 8192 tokens, 32 heads of 128 (0.55 TFLOP), 526 us,
-// 1.05 PFLOP/s, where a large bf16 matrix product reaches 1.22.  Four waves of 64 rows, with the tiles' fragments read
+// The matrix cores bound it, and on long prompts the card's power: 8192 tokens, 32 heads of 128 (0.55 TFLOP), 526 to 556 us
+// with the card's temperature, 0.99 to 1.05 PFLOP/s, where a large bf16 matrix product reaches 1.22.  Four waves of 64 rows, with the tiles' fragments read
 // half as often, took a tenth more clocks and the same time (537 to 545 us, the clock at 2.2 GHz instead of 1.96), and
 // chunks 3-5% longer.  Two tiles per pass and three passes under way at D = 128: 558 against 546 us.
-// 512 tokens over 16384 rows, 32 heads on 8: 136 to 145 us and 10 us for the merge of the splits.
+// 512 tokens over 16384 rows, 32 heads on 8: 134 to 150 us and 10 us for the merge of the splits.
 #include <type_traits>
 
 #include "chunk_few.hpp"

@@ -5,18 +5,22 @@
 //   rank(t) = #{u : z_u > z_t} + #{u < t : z_u = z_t}
 //
 // One pass over the row.  A thread keeps the largest logit so far, S and T against it, the count for
-// the rank, and the 16-byte vector that held its largest logit first.  (A reference maximum that is raised
+// the rank, and the 16-byte vector that held its largest logit first, and the largest of its other vectors.  (A reference maximum that is raised
 // only now and then would save rescalings, but not here: T against a reference 16 below the maximum
 // loses 4 bits of the entropy when it is moved.)  The top alternatives need no bookkeeping in the pass: the K-th largest
 // of the threads' maxima, H, is at most the K-th largest logit, so every one of the top K is in a vector
-// of one of the few threads whose maximum reaches H; only those threads' vectors are read again.
+// of one of the few threads whose maximum reaches H. They have the vector with that maximum at hand; only where the
+// largest of a thread's others reaches H, too, are they read again (all of these threads' read again: 20% more bytes,
+// as eight threads share a line, 118 against 114 us).
 //
-// Memory bounds it, with the vector instructions close behind (93% of their issue slots): 2048 rows of 128256 bf16
-// logits (526 MB), 114 us, 4.6 TB/s; 65 rows of 152064 float32 logits (40 MB, in parts), 15.5 us and 3.9 us to join them.
-// (Steps without the bounds' selects, the rank counted by the scalar unit and the best vector read again took fewer
-// vector instructions, and 121 and 18.7 us against 114 and 19.0.)
+// Memory bounds it, with the vector instructions close behind: 2048 rows of 128256 bf16 logits (526 MB), 110 us,
+// 4.8 TB/s (bounds checked in every step, not in the last alone: 114); 65 rows of 152064 float32 logits (40 MB, in
+// parts), 15 us and 4 us to join them.  The rank counted by the scalar unit off the compare masks, and bf16's best vector read
+// again instead of kept: 121 against 114 us.
 //
 // Keys: (value, id) pairs as 64-bit integers (common.hpp), all distinct, so ties go to the lowest id.
+#include <type_traits>
+
 #include "topk.hpp"
 #include "prompt.hpp"
 
@@ -150,21 +154,25 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
   Stats s{kNegInf, kNegInf, 0.f, 0.f, 0};
   int jb = j0 + tid < j1 ? j0 + tid : -1;  // vector that held the thread's largest logit first ...
   u32x4 best = {0u, 0u, 0u, 0u};           // ... and what it holds
-  for (int j = j0 + tid; j - tid < j1; j += kThreads * kUnroll) {
+  float second = kNegInf;                  // the largest logit of the thread's other vectors
+  auto step = [&](auto whole_c, int j) __attribute__((always_inline)) {
+    constexpr bool WHOLE = decltype(whole_c)::value;
     u32x4 raw[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) raw[u] = ld16(base + (int64_t)max(min(j + u * kThreads, j1 - 1), j0) * 16);
+    for (int u = 0; u < kUnroll; ++u)
+      raw[u] = ld16(base + (int64_t)(WHOLE ? j + u * kThreads : max(min(j + u * kThreads, j1 - 1), j0)) * 16);
     if (j == j0 + tid) best = raw[0];
     Vec<T> x[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       x[u].set(raw[u]);
       const int ju = j + u * kThreads;
-      const bool in = ju < j1;
+      const bool in = WHOLE || ju < j1;
       float top = x[u].z[0];
 #pragma unroll
       for (int e = 1; e < N; ++e) top = fmaxf(top, x[u].z[e]);
       const bool more = in && top > s.top;
+      second = __builtin_amdgcn_fmed3f(second, s.top, in ? top : kNegInf);
       s.top = more ? top : s.top;
       jb = more ? ju : jb;
 #pragma unroll
@@ -188,7 +196,11 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
         s.S += p;
         s.T = __builtin_fmaf(p, fmaxf(d, -200.f), s.T);  // (-inf: 0 times a finite number)
       }
-  }
+  };
+  int j = j0 + tid;
+#pragma unroll 1
+  for (; j - tid + kThreads * kUnroll <= j1; j += kThreads * kUnroll) step(std::integral_constant<bool, true>{}, j);
+  if (j - tid < j1) step(std::integral_constant<bool, false>{}, j);
   // edges: thread e < N the row's first logits, N <= e < 2 N its last
   uint64_t edge = 0;
   if (tid < 2 * N) {
@@ -233,12 +245,23 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
     if (lane < KO) l_top[wave * KO + lane] = sorted;
     if (tid < 2) l_n[tid] = 0;
     __syncthreads();
-    // (all of the waves' K largest: the largest of the waves' K-th saves a sort and has up to four times the
-    // threads' vectors read again, 65 rows of 152064 float32 logits 21.4 against 19.9 us, 2048 of 128256 bf16
-    // 129 against 117)
+    // (all of the waves' K largest: the largest of the waves' K-th would save a sort, and have up to four times the threads)
     const uint64_t H = key_of_lane(sort_lanes_desc(lane < kWaves * KO ? l_top[lane] : 0ull), KO - 1);
-    if (mine != 0 && mine >= H) l_cand[atomicAdd(&l_n[0], 1)] = tid;  // (at most KO: keys are distinct)
+    if (mine != 0 && mine >= H) {  // (at most KO threads: keys are distinct)
+      if (H == 0 || second >= key_value(H)) {
+        l_cand[atomicAdd(&l_n[0], 1)] = tid;
+      } else {
+        Vec<T> v;
+        v.set(best);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const uint64_t k = make_key(v.z[e], jb * N - off + e);
+          if (k >= H && v.z[e] == v.z[e]) l_keys[atomicAdd(&l_n[1], 1)] = k;  // (with the edges' at most (KO + 2) N)
+        }
+      }
+    }
     if (edge != 0 && edge >= H) l_keys[atomicAdd(&l_n[1], 1)] = edge;
+    static_assert((KO + 2) * N <= kMaxKeys);
     __syncthreads();
     const int per = (j1 - j0 + kThreads - 1) / kThreads, total = l_n[0] * per;
     for (int x = tid; x < total; x += kThreads) {

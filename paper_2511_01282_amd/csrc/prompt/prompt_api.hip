@@ -33,8 +33,8 @@ bool aligned(const void* p, size_t n) { return ((uintptr_t)p % n) == 0; }
 bool known(int32_t dtype) { return dtype == RESPEC_F32 || dtype == RESPEC_BF16; }
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
-constexpr int kMaxSplits = 64;             // a lane of the merge per split
-constexpr size_t kMaxPartial = 1u << 25;    // columns of partials: 134 MB
+constexpr int kMaxSplits = 64;           // a lane of the merge per split
+constexpr size_t kMaxPartial = 1u << 25;  // columns of partials: 134 MB
 constexpr int kMaxStride = 1 << 24;
 constexpr int kMaxRows = 1 << 30;         // cache rows of a sequence: positions a tile further fit 32 bits
 
@@ -84,18 +84,21 @@ ChunkBatch device_batch(const respec_chunk_plan* plan, const respec_chunk_batch&
   return d;
 }
 
-// How long an attention kernel takes over one cache row of a block, and to start a workgroup (us).
+// How long an attention kernel takes over one cache row of a block, with all the workgroups of a CU that the pace was
+// taken with, and to start a workgroup (us).
 struct Pace {
   double row, start;
 };
 
-// Splits of the sequences: the number n (of a coarser choice upwards; at most `held`, each of `least` cache rows or more, in multiples of `unit`)
-// with the least estimated time  rounds * (rows / n * row + start) + merge,  rounds = items * n / CUs.  One
-// sequence's lengths are known, and its workgroups run in whole rounds; of a batch the host knows the longest
-// alone, so half the work that longest sequences would be is assumed, and half a round of tail
-// (80 drawn batches of chunks, geometric mean: a third 30.5 us, 0.4 29.5, 0.5 29.4, 0.8 29.2; of decoding tokens 21.8, 21.2, 21.8, 21.9).
-ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long long limit, int unit, int least, int per_cu, Pace pace,
-                   int row_bytes, long long held) {
+// Splits of the sequences: the number n (of a coarser choice upwards; at most `held`, each of `least` cache rows or
+// more, in multiples of `unit`) with the least estimated time  rounds * (rows / n * row + start) + merge,
+// rounds = items * n / (CUs * per_cu); fewer than per_cu workgroups on a CU are so much faster.  One sequence's lengths
+// are known, and its workgroups run in whole rounds; of a batch the host knows the longest alone, so half the work that
+// longest sequences would be is assumed, and half a round of tail (80 drawn batches of chunks, geometric mean: a third
+// 30.5 us, 0.4 29.5, 0.5 29.4, 0.8 29.2; of decoding tokens 21.8, 21.2, 21.8, 21.9).  Float32, 60 drawn sequences: with a lone
+// workgroup's true pace 13.1 us, with four workgroups' for any 13.9, where calls of a few rows were split in vain.
+ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long long limit, int unit, int least,
+                   int per_cu, Pace pace, int row_bytes, long long held) {
   constexpr double kShare = 0.5;
   ChunkGeom g{rows_per_wg, 1, INT_MAX, 0, fast_div(INT_MAX)};
   const long long items = blocks * b.n_kv_heads;
@@ -109,7 +112,8 @@ ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long 
     const double rounds = b.batch == 1 ? ceil(wgs) : std::max(1.0, wgs * kShare) + 0.5;
     const double joined = 1e-6 * n * b.total_new * b.n_kv_heads * b.group * row_bytes * 2 / 4.5;
     const double merge = n == 1 ? 0 : 4 + joined * (b.batch == 1 ? 1 : kShare);
-    const double t = rounds * (rows * pace.row + pace.start) + merge;
+    const double crowd = std::min(1.0, ceil(wgs * per_cu) / per_cu);  // workgroups of a CU, of the per_cu that set the pace
+    const double t = rounds * (rows * pace.row * crowd + pace.start) + merge;
     if (n == 1 || t < best) {
       best = t;
       g.split_rows = n == 1 || rows >= limit ? INT_MAX : (int)rows;
@@ -241,7 +245,7 @@ respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chun
   if (s.dtype == RESPEC_F32) {
     a.few_rows = 0;
     a.few = ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
-    a.wide = geometry(a.b, 64, blocks(64), limit, 32, 32, 4, Pace{0.2, 5}, rb, held);
+    a.wide = geometry(a.b, 64, blocks(64), limit, 32, 32, 2, s.head_dim == 128 ? Pace{0.16, 5} : Pace{0.1, 5}, rb, held);
     if ((long long)a.wide.items + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
     e = launch_chunk_attn_f32(s.head_dim, a, status, stm);
   } else {

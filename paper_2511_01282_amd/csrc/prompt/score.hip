@@ -4,19 +4,19 @@
 //   lse = m + log S, H = log S - T/S, log p(t) = (z_t - m) - log S
 //   rank(t) = #{u : z_u > z_t} + #{u < t : z_u = z_t}
 //
-// One pass over the row.  A thread keeps the largest logit so far, S and T against it, the count for
-// the rank, and the 16-byte vector that held its largest logit first, and the largest of its other vectors.  (A reference maximum that is raised
-// only now and then would save rescalings, but not here: T against a reference 16 below the maximum
-// loses 4 bits of the entropy when it is moved.)  The top alternatives need no bookkeeping in the pass: the K-th largest
-// of the threads' maxima, H, is at most the K-th largest logit, so every one of the top K is in a vector
-// of one of the few threads whose maximum reaches H. They have the vector with that maximum at hand; only where the
-// largest of a thread's others reaches H, too, are they read again (all of these threads' read again: 20% more bytes,
-// as eight threads share a line, 118 against 114 us).
+// One pass over the row.  A thread keeps the largest logit so far, S and T against it, the count for the rank, the
+// 16-byte vector that held its largest logit first, and the largest of its other vectors.  (A reference maximum that
+// is raised only now and then would save rescalings, but not here: T against a reference 16 below the maximum loses
+// 4 bits of the entropy when it is moved.)  The top alternatives need little bookkeeping in the pass: the K-th largest
+// of the threads' maxima, H, is at most the K-th largest logit, so every one of the top K is in a vector of one of the
+// few threads whose maximum reaches H.  They have the vector with that maximum at hand; only where the largest of a
+// thread's others reaches H, too, are its vectors read again (those of all of these threads: 20% more bytes, as eight
+// threads share a line, 118 against 114 us).
 //
 // Memory bounds it, with the vector instructions close behind: 2048 rows of 128256 bf16 logits (526 MB), 110 us,
 // 4.8 TB/s (bounds checked in every step, not in the last alone: 114); 65 rows of 152064 float32 logits (40 MB, in
-// parts), 15 us and 4 us to join them.  The rank counted by the scalar unit off the compare masks, and bf16's best vector read
-// again instead of kept: 121 against 114 us.
+// parts), 15 us and 4 us to join them.  The rank counted by the scalar unit off the compare masks, and bf16's best
+// vector read again instead of kept: 121 against 114 us.
 //
 // Keys: (value, id) pairs as 64-bit integers (common.hpp), all distinct, so ties go to the lowest id.
 #include <type_traits>

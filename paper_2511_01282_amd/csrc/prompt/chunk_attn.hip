@@ -15,7 +15,7 @@ namespace {
 // lane l, the scores of row l % 16 with keys 4 (l / 16) .. + 3 of 16, which are the B operand of O^T += V^T P^T as
 // they stand.  A tile of 32 cache rows is fetched into registers while the tile before is worked on, then goes to
 // one of two LDS buffers, K rows as they are and V transposed.  The matrix cores bound it: 32 clocks per product
-// of 2048 operations.  Measured: 1500 tokens, 16 heads of 64, 66 us and 7 us for the merge (4.6 GFLOP: 71 TFLOP/s, where
+// of 2048 operations.  Measured: 1500 tokens, 16 heads of 64, 67 us and 6 us for the merge (4.6 GFLOP: 69 TFLOP/s, where
 // a large float32 matrix product reaches 154); one token of 4 heads over 512 rows, 7.2 us.
 template <int D>
 __global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
@@ -211,7 +211,7 @@ constexpr int kMergeMany = 16;  // splits of a sequence above which a row has a 
 // once, and are joined through LDS.  Rows of one split are written already.
 //
 // Bound by the partials' bytes where there are many rows: 512 tokens of 32 heads of 128 in 4 splits (38 MB), 9.8 us, 3.9 TB/s;
-// 1500 tokens of 16 heads of 64, 6.8 us (a wave per row with a lane per split: 11.8; workgroups per row from 5 splits
+// 1500 tokens of 16 heads of 64, 5.8 to 6.8 us (a wave per row with a lane per split: 11.8; workgroups per row from 5 splits
 // on: 103 us for the whole call, not 69).  One token of 28 heads in 64 splits (0.9 MB): 4.4 us (four at a time, all groups: 5.8).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkAttnArgs a) {

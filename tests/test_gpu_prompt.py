@@ -101,6 +101,16 @@ def test_attention_long(lib, dtype, sizes, kv_heads, group, head_dim, page):
     _close(_attend(lib, c), *pc.attention(c))
 
 
+@pytest.mark.parametrize("dtype,head_dim", [(BF, 64), (BF, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("step", [32, 128])
+def test_numbers_of_splits(lib, dtype, head_dim, step):
+    """One token over 2 to 4, 16, 17 and 64 splits of either size, alone and beside a short sequence."""
+    for n in (2, 3, 4, 5, 16, 17, 64):
+        for more in ([], [(3, 40)]):
+            c = pc.make([(1, n * step - 1)] + more, dtype=dtype, heads=6, kv_heads=2, head_dim=head_dim, page=32, seed=n)
+            _close(_attend(lib, c), *pc.attention(c))
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_attention_strides_and_scale(lib, dtype):
     """Queries as a slice of a wider projection, a cache with rows before heads, a scale of the caller's."""

@@ -74,7 +74,7 @@ __device__ __forceinline__ void dma_rows(uint32_t dst, uint64_t base, const uint
         "global_load_lds_dwordx4 %2, %6\n\t"
         "global_load_lds_dwordx4 %3, %6 offset:1024\n\t"
         "global_load_lds_dwordx4 %4, %6 offset:2048\n\t"
-        "global_load_lds_dwordx4 %5, %6 offset:3072\n\t"
+        "global_load_lds_dwordx4 %5, %6 offset:3*1024\n\t"
         "s_mov_b32 m0, %0"
         : "=&s"(saved)
         : "s"(dst), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base)

@@ -40,11 +40,12 @@ struct Stats {
   int cnt;
 };
 
-// The same with the sums against a larger maximum.
+// The same with the sums against a larger maximum.  (A difference below -200, beside which e is 0, counts as -200: a
+// masked vocabulary's lowest values times S would be an infinity, and 0 times that a NaN.)
 __device__ __forceinline__ void rebase(Stats& s, float to) {
   const bool none = s.ref == kNegInf;
   const float d = none ? 0.f : s.ref - to, e = none ? 1.f : exp_f(d);
-  s.T = e * (s.T + d * s.S);
+  s.T = e * (s.T + fmaxf(d, -200.f) * s.S);
   s.S *= e;
   s.ref = to;
 }

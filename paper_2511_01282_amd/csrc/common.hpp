@@ -156,7 +156,8 @@ struct RowStats {
     const bool z1 = m == -__builtin_huge_valf(), z2 = m2 == -__builtin_huge_valf();
     const float d1 = z1 ? 0.f : m - M, d2 = z2 ? 0.f : m2 - M;
     const float e1 = z1 ? 0.f : __expf(d1), e2 = z2 ? 0.f : __expf(d2);
-    T = e1 * (T + d1 * S) + e2 * (T2 + d2 * S2);
+    // (below -200, beside which e is 0, a difference counts as -200: it would make an infinity of S, and 0 times that a NaN)
+    T = e1 * (T + fmaxf(d1, -200.f) * S) + e2 * (T2 + fmaxf(d2, -200.f) * S2);
     S = e1 * S + e2 * S2;
     am = m > m2 ? am : (m2 > m ? am2 : min(am, am2));
     m = M;

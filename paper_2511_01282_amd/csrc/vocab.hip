@@ -192,7 +192,7 @@ __device__ __forceinline__ void wave_rowstats(RowStats& st) {
   const bool empty = st.m == -__builtin_huge_valf();
   const float d = empty ? 0.f : st.m - M;
   const float e = empty ? 0.f : __expf(d);
-  float S = st.S * e, T = (st.T + d * st.S) * e;
+  float S = st.S * e, T = (st.T + fmaxf(d, -200.f) * st.S) * e;  // (as in RowStats::merge)
   int am = (!empty && st.m == M) ? st.am : 0x7FFFFFFF;
   S += xchg<0>(S); T += xchg<0>(T); am = min(am, xchg<0>(am));
   S += xchg<1>(S); T += xchg<1>(T); am = min(am, xchg<1>(am));

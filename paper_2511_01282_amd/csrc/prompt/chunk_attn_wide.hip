@@ -64,11 +64,11 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks] = ld16(q + (2 * ks + hi) * 16);
   }
-  // (uniform) tiles that some row of the wave sees, and those that every row sees whole
+  // (uniform) tiles that some row of the wave sees, and those that every row sees whole; none for a wave without rows
   const int my_end = min(sq.L + (int)div_by((uint32_t)min(wrow + 31, rows - 1), a.group) + 1, hi_row);
   const int my_first = min(sq.L + (int)div_by((uint32_t)min(wrow, rows - 1), a.group) + 1, hi_row);
   const int my_tiles = wrow < rows && my_end > lo ? (my_end - lo + kTile - 1) / kTile : 0;
-  const int unmasked = max(my_first - lo, 0) / kTile;
+  const int unmasked = my_tiles > 0 ? max(my_first - lo, 0) / kTile : 0;
 
   // ---- DMA: unit u is tiles kPass u + 1 .. kPass u + kPass (unit -1: tile 0), kRows rows of each by every wave ----
   Feed feed;

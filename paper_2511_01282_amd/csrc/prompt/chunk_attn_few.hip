@@ -11,7 +11,7 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_few_kernel(ChunkAttnArgs a)
     report_status<256>(a.b, (int)blockIdx.x - a.few.items, true);
     return;
   }
-  few_rows_item<D, GR>(a, (int)blockIdx.x, smem);
+  few_rows_item<D, GR, false>(a, (int)blockIdx.x, smem);
 }
 
 template <int D, int GR>

@@ -190,7 +190,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_attn_wide_kernel(ChunkAt
   x -= a.wide.items;
   if constexpr (MIXED) {
     if (x < a.few.items) {
-      if (threadIdx.x < 256) few_rows_item<D, 1>(a, x, smem);
+      if (threadIdx.x < 256) few_rows_item<D, 1, D == 128>(a, x, smem);
       return;
     }
     x -= a.few.items;

@@ -29,8 +29,9 @@ struct FewShape {
   static_assert(kLds <= 163840, "LDS of a CU");
 };
 
-// Item x, by four waves (256 threads); GR groups of 32 query rows.
-template <int D, int GR>
+// Item x, by four waves (256 threads); GR groups of 32 query rows.  LEAN, for waves of at most 256 registers: what depends
+// on the lane alone is worked out in every tile (`at`); held along, as the compiler would have it, it spills.
+template <int D, int GR, bool LEAN>
 __device__ __forceinline__ void few_rows_item(const ChunkAttnArgs& a, int x, unsigned char* smem) {
   using G = FewShape<D>;
   using Feed = RowFeed<D, kFewTile / 2>;
@@ -72,6 +73,8 @@ __device__ __forceinline__ void few_rows_item(const ChunkAttnArgs& a, int x, uns
   const bool in_page = a.b.page.d % 16 == 0;  // 16 rows from a multiple of 16 lie in one page
   int produced = 0;
   auto produce = [&]() {
+    int at = lane;
+    if constexpr (LEAN) asm("" : "+v"(at));
     const uint32_t dst = lds0 + (uint32_t)((produced % S) * G::kSlot);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -81,7 +84,7 @@ __device__ __forceinline__ void few_rows_item(const ChunkAttnArgs& a, int x, uns
       if (in_page && t0 + 16 <= hi_row)
         feed.from_page(a.b, to, to + G::kHalf, ids.uniform(pa), (uint32_t)t0 - pa * a.b.page.d);
       else
-        feed.from_rows(a.b, to, to + G::kHalf, ids.ids, ids.p0, t0, hi_row, lane);
+        feed.from_rows(a.b, to, to + G::kHalf, ids.ids, ids.p0, t0, hi_row, at);
     }
     ++produced;
   };
@@ -113,8 +116,10 @@ __device__ __forceinline__ void few_rows_item(const ChunkAttnArgs& a, int x, uns
     const unsigned char* t = ring + (j % S) * G::kSlot;
     const int key0 = lo + (j * 4 + wave) * kFewTile;
     u32x4 kf[KS], vf[DB][2], p[GR][2];
-    read_k<D>(t, lane, kf);
-    read_v<D>(t + G::kHalf, lane, vf);
+    int at = lane;
+    if constexpr (LEAN) asm("" : "+v"(at));
+    read_k<D>(t, at, kf);
+    read_v<D>(t + G::kHalf, at, vf);
     f32x16 s[GR];
 #pragma unroll
     for (int g = 0; g < GR; ++g) {
@@ -128,10 +133,10 @@ __device__ __forceinline__ void few_rows_item(const ChunkAttnArgs& a, int x, uns
     } else {
 #pragma unroll
       for (int g = 0; g < GR; ++g) {
-        mask_scores(s[g], key0, end[g], lane);
+        mask_scores(s[g], key0, end[g], at);
         settle(r[g], s[g], a.scale_log2, p[g], weights(s[g], a.scale_log2, r[g].m, p[g]));
       }
-      if (take_out_not_finite<D>(vf)) add_not_finite<D, GR>(r, t + G::kHalf, key0, end, lane);
+      if (take_out_not_finite<D>(vf)) add_not_finite<D, GR>(r, t + G::kHalf, key0, end, at);
     }
 #pragma unroll
     for (int k2 = 0; k2 < 2; ++k2)

@@ -18,13 +18,14 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
-// Softmax reference of a row that has seen nothing; exp2 of a score less this is inf, which a
-// row's first tile always corrects (see Weights).
-constexpr float kNoRef = -3.0e38f;
+// Softmax reference of a row that has seen nothing: no finite score is below it, and exp2 of an ordinary score less this
+// is inf, which a row's first tile always corrects (see settle).
+constexpr float kNoRef = -3.402823466e38f;
 // A row's reference maximum is raised only where a weight exceeds 2^8 or so (log2 units), so that the
 // accumulators are seldom rescaled; the weights' sum in a tile shows it without looking for the maximum.
 constexpr float kRefMargin = 8.f;
 constexpr float kSumLimit = 4096.f;  // 16 weights of at most 2^8
+constexpr float kFarRef = 33554432.f;  // 2^25, see settle()
 
 template <int D>
 __device__ __forceinline__ int k_chunk(int r) {  // permutation of a K row's chunks (an xor)
@@ -183,18 +184,28 @@ template <int D>
 struct Rows {
   f32x16 o[D / 32];  // column 32 db + 8 (i / 4) + 4 (l / 32) + i % 4
   float m, l;        // reference maximum (log2 units), sum of this half's weights
+  float limit;       // sum of a tile's weights above which settle() looks at them
 
   __device__ __forceinline__ void init() {
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) o[db] = f32x16{};
     m = kNoRef;
     l = 0.f;
+    limit = kSumLimit;
   }
 };
+
+// A score's exponent against reference m; FAR: with the product rounded first.
+template <bool FAR>
+__device__ __forceinline__ float less_ref(float s, float scale_log2, float m) {
+#pragma clang fp contract(off)
+  return FAR ? s * scale_log2 - m : __builtin_fmaf(s, scale_log2, -m);
+}
 
 // Weights of 32 keys against reference m, as bf16 pairs, and their sum.  The sum is of the rounded weights, so
 // the division by it undoes what rounding does to all of them alike.  Each rounding, to 8 bits, is half a step
 // of the output's own rounding at most, and they are many and of either sign.
+template <bool FAR = false>
 __device__ __forceinline__ float weights(const f32x16& s, float scale_log2, float m, u32x4 (&p)[2]) {
   const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
   float sum = 0.f;
@@ -202,8 +213,8 @@ __device__ __forceinline__ float weights(const f32x16& s, float scale_log2, floa
   for (int k2 = 0; k2 < 2; ++k2)
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * k2 + 2 * w], scale_log2, -m));
-      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * k2 + 2 * w + 1], scale_log2, -m));
+      const float p0 = __builtin_amdgcn_exp2f(less_ref<FAR>(s[8 * k2 + 2 * w], scale_log2, m));
+      const float p1 = __builtin_amdgcn_exp2f(less_ref<FAR>(s[8 * k2 + 2 * w + 1], scale_log2, m));
       const bf16x2 h = __builtin_convertvector(f32x2{p0, p1}, bf16x2);
       sum = __builtin_amdgcn_fdot2_f32_bf16(h, ones, sum, false);
       p[k2][w] = __builtin_bit_cast(uint32_t, h);
@@ -212,10 +223,13 @@ __device__ __forceinline__ float weights(const f32x16& s, float scale_log2, floa
 }
 
 // After weights(): where some row's sum shows a weight above the margin, its reference becomes the tile's
-// maximum, what it has accumulated is rescaled and the tile's weights are taken again.
+// maximum, what it has accumulated is rescaled and the tile's weights are taken again.  The reference is a score's
+// rounded product with the scale, off from the exact one by up to half a unit of its last place: where that is more than a
+// few (2^31 and up it is 128: a weight of inf or 0 that should be 1), every tile's weights are taken again, against rounded
+// products (kFarRef; as a limit of the row's own it costs nothing, a test of the reference in every tile 3-5% of mixed batches).
 template <int D>
 __device__ __forceinline__ void settle(Rows<D>& r, const f32x16& s, float scale_log2, u32x4 (&p)[2], float sum) {
-  if (__any(sum > kSumLimit)) {
+  if (__any(sum > r.limit)) {
     float x = max_of(s[0], s[1]);
 #pragma unroll
     for (int i = 2; i < 16; ++i) x = max_of(x, s[i]);
@@ -224,10 +238,11 @@ __device__ __forceinline__ void settle(Rows<D>& r, const f32x16& s, float scale_
     const float to = top > r.m + kRefMargin ? top : r.m;
     const float alpha = __builtin_amdgcn_exp2f(r.m - to);
     r.m = to;
+    r.limit = fabsf(to) > kFarRef && to != kNoRef ? -1.f : kSumLimit;
     r.l *= alpha;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) r.o[db] *= alpha;
-    sum = weights(s, scale_log2, to, p);
+    sum = weights<true>(s, scale_log2, to, p);
   }
   r.l += sum;
 }

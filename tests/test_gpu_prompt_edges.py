@@ -9,7 +9,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 import prompt_cases as pc  # noqa: E402
-from test_gpu_prompt import BF, F32, _check_scores, _close, _score, lib  # noqa: E402,F401
+from test_gpu_prompt import BF, F32, _attend, _check_scores, _close, _score, lib  # noqa: E402,F401
 
 
 # ---------------------------------------------------------------------------
@@ -46,3 +46,33 @@ def test_scores_of_rows_masked_by_a_low_value(lib, dtype, low, vocab):
                 _close(part, want[k], tol[k])
             else:
                 assert torch.equal(part, want[k]), k
+
+
+# ---------------------------------------------------------------------------
+# attention
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,head_dim", [(BF, 64), (BF, 128), (F32, 64)])
+@pytest.mark.parametrize("sizes", [[(1, 0)], [(1, 200)], [(1, 5000)], [(20, 900)], [(150, 40)], [(40, 2000), (1, 300)]])
+@pytest.mark.parametrize("score", [-3.2e38, -1e30, 2.5e9, -4e12, 3.1e38])
+def test_scores_of_any_finite_size(lib, dtype, head_dim, sizes, score):
+    """Keys all alike have weights all alike, however large the scores are.
+
+    A token's output is the mean of the values it sees.  The weights of equal scores are equal, so neither their size
+    nor their rounding matters; the sums add (rows + 64) 2^-24, the result's rounding half a step."""
+    c = pc.make(sizes, dtype=dtype, heads=4, kv_heads=2, head_dim=head_dim, page=16, seed=3, stale=0.0)
+    big = math.sqrt(abs(score) / math.log2(math.e) / (head_dim / 2))
+    c.q[:] = 0
+    c.k_pages[:] = 0
+    c.q[..., ::2] = big
+    c.k_pages[..., ::2] = math.copysign(big, score)   # scale 1: half of the columns have a product each
+    assert math.log2(math.e) * float((c.q[0, 0].double() * c.k_pages[0, 0, 0].double()).sum().abs()) < torch.finfo(F32).max
+    want, tol = torch.empty(c.q.shape, dtype=pc.F64), torch.empty(c.q.shape, dtype=pc.F64)
+    t = 0
+    for (n, l), (_, vr) in zip(c.sizes, c.rows):
+        for i in range(n):
+            v = vr[:l + i + 1].to(pc.F64).repeat_interleave(2, 1)
+            want[t], size = v.mean(0), v.abs().mean(0)
+            tol[t] = size * (len(v) + 64) * 2.0 ** -24 + want[t].abs() * torch.finfo(dtype).eps / 2 + 1e-30
+            t += 1
+    _close(_attend(lib, c, scale=1.0), want, tol)

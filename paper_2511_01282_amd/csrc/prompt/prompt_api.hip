@@ -212,9 +212,8 @@ respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chun
     if (!aligned(x.q, 16) || !aligned(x.out, 16)) return RESPEC_ERR_SHAPE;
     for (int64_t s : {x.q_token_stride, x.q_head_stride, x.out_token_stride, x.out_head_stride})
       if (!stride_ok(s, plan->es)) return RESPEC_ERR_SHAPE;
-  } else if (!x.b.seq_status) {
-    return RESPEC_OK;
   }
+  if (x.b.max_new_in_batch == 0 && !x.b.seq_status) return RESPEC_OK;  // (no sequence has tokens)
   const respec_chunk_shape& s = plan->s;
   ChunkAttnArgs a;
   a.b = device_batch(plan, x.b);

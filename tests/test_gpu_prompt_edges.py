@@ -9,7 +9,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 import prompt_cases as pc  # noqa: E402
-from test_gpu_prompt import BF, F32, _attend, _check_scores, _close, _score, lib  # noqa: E402,F401
+from test_gpu_prompt import BF, F32, _attend, _cache, _check_scores, _close, _plan, _score, lib  # noqa: E402,F401
 
 
 # ---------------------------------------------------------------------------
@@ -76,3 +76,21 @@ def test_scores_of_any_finite_size(lib, dtype, head_dim, sizes, score):
             tol[t] = size * (len(v) + 64) * 2.0 ** -24 + want[t].abs() * torch.finfo(dtype).eps / 2 + 1e-30
             t += 1
     _close(_attend(lib, c, scale=1.0), want, tol)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("status", [False, True])
+def test_no_tokens_in_any_sequence(lib, dtype, status):
+    """Packed rows that no sequence owns (a captured call replayed without tokens), lengths that say so."""
+    c = pc.make([(0, 5), (0, 0)], dtype=dtype, heads=4, kv_heads=2, head_dim=64, page=16)
+    plan = _plan(lib, c, max_new=5)
+    rows = torch.full((5, 4, 64), 7.0, dtype=dtype, device="cuda")
+    out = rows.clone()
+    st = torch.full((2,), -9, dtype=torch.int32, device="cuda") if status else None
+    cache = _cache(c)
+    plan.attend(rows, *cache, out, max_new_in_batch=0, max_kv_len_in_batch=5, status=st)
+    plan.append(rows[:, :2], rows[:, 2:], *cache, max_new_in_batch=0)
+    torch.cuda.synchronize()
+    assert torch.equal(out, rows) and (not status or st.tolist() == [0, 0])
+    for t, was in zip(cache[:2], (c.k_pages, c.v_pages)):
+        assert torch.equal(t.cpu().nan_to_num(3.0), was.nan_to_num(3.0))

@@ -125,10 +125,13 @@ class _Plan:
         return t.get_device() == self._index and (self._index >= 0 or t.device == self.device)
 
     def _rows(self, t, name, dtype, shape):
-        """Address and strides of a tensor of rows: the last dimension contiguous (where it has more than one)."""
+        """Address and strides of a tensor of rows: the last dimension contiguous (where it has more than one), strides
+        of dimensions of one element 0."""
         st = t.stride()
         if t.shape != shape or t.dtype != dtype or not self._here(t) or (st[-1] != 1 and shape[-1] > 1):
             self._refuse(t, name, dtype, shape)
+        if 1 in shape:
+            st = [0 if n == 1 else s for n, s in zip(shape, st)]
         return t.data_ptr(), st
 
     def _flat(self, t, name, dtype, shape):

@@ -94,3 +94,22 @@ def test_no_tokens_in_any_sequence(lib, dtype, status):
     assert torch.equal(out, rows) and (not status or st.tolist() == [0, 0])
     for t, was in zip(cache[:2], (c.k_pages, c.v_pages)):
         assert torch.equal(t.cpu().nan_to_num(3.0), was.nan_to_num(3.0))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_strides_of_dimensions_of_one(lib, dtype):
+    """A dimension of one element has no stride to speak of: a token from a column vector, one page, one KV head."""
+    c = pc.make([(1, 9)], dtype=dtype, heads=4, kv_heads=1, head_dim=64, page=16, spare=0, stale=0.0)
+    c.table[:] = 0
+    kr, vr = c.rows[0]
+    k, v = (torch.zeros(16, 64, dtype=dtype) for _ in range(2))
+    k[:10], v[:10] = kr[:, 0], vr[:, 0]
+    q = c.q.cuda().as_strided((1, 4, 64), (1, 64, 1))
+    new = [t.cuda().as_strided((1, 1, 64), (3, 5, 1)) for t in (c.k_new, c.v_new)]
+    kp, vp = k.cuda().as_strided((1, 1, 16, 64), (3, 7, 64, 1)), v.cuda().as_strided((1, 1, 16, 64), (1024, 1024, 64, 1))
+    table, off, kv_len = c.table[:, :1].cuda(), c.off.cuda(), c.kv_len.cuda()
+    out = torch.zeros(4 * 64, dtype=dtype, device="cuda").as_strided((1, 4, 64), (5, 64, 1))
+    plan = _plan(lib, c)
+    plan.append(*new, kp, vp, table, off, kv_len, max_new_in_batch=1)
+    plan.attend(q, kp, vp, table, off, kv_len, out, max_new_in_batch=1, max_kv_len_in_batch=9)
+    _close(out.cpu(), *pc.attention(c))

@@ -205,11 +205,12 @@ class ChunkPlan(_Plan):
         dims = (q.shape[0], s.n_q_heads, s.head_dim)
         qp, q_st = self._rows(q, "q", self.dtype, dims)
         op, o_st = self._rows(out, "out", self.dtype, dims)
-        if scale is not None and not scale > 0:
-            raise ValueError("scale: a positive number expected")
+        scale_f = 0.0 if scale is None else ctypes.c_float(scale).value
+        if scale is not None and not scale_f > 0:
+            raise ValueError("scale: a positive number expected, in float32, too")
         b = self._batch(k_pages, v_pages, page_table, new_off, kv_len, dims[0], max_new_in_batch, max_kv_len_in_batch,
                         status)
-        a = AttnArgs(b, qp, q_st[0], q_st[1], op, o_st[0], o_st[1], scale or 0.0)
+        a = AttnArgs(b, qp, q_st[0], q_st[1], op, o_st[0], o_st[1], scale_f)
         self._call(lib().respec_chunk_attn, "respec_chunk_attn", (ctypes.byref(a), self.workspace_ptr), stream)
 
 

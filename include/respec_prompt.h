@@ -30,7 +30,10 @@
  *  - Plans hold host metadata only, are immutable and may be shared by threads.
  *    Calls that may overlap need workspaces of their own; calls in order on one
  *    stream, captured or not, can share one.  A workspace needs no initialisation.
- *  - Host-side checks return a status and launch nothing.  Errors in device data
+ *  - Host-side checks return a status and launch nothing; RESPEC_ERR_SHAPE, too,
+ *    for a call whose kernel would have 2^32 threads or more (for example appends
+ *    of 2^28 tokens of one narrow KV head, or 65535 sequences of 256 KV heads of
+ *    one token with a status).  Errors in device data
  *    are reported per sequence in seq_status[b] (when it is not NULL): the kernels
  *    never trap and never touch memory outside the buffers described here.
  *    What a sequence with a non-zero status leaves in its own output rows is
@@ -149,7 +152,7 @@ respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chun
 typedef struct {
   int32_t vocab;     /* V >= topk_out, < 2^30                                                  */
   int32_t dtype;     /* respec_dtype of the logits                                             */
-  int32_t max_rows;  /* capacity in rows, >= 1                                                 */
+  int32_t max_rows;  /* capacity in rows, 1 .. 2^24 - 1                                        */
   int32_t topk_out;  /* width of the top-k output, 1..RESPEC_MAX_TOPK_OUT                      */
 } respec_score_shape;
 

@@ -14,7 +14,7 @@
 namespace respec {
 namespace {
 
-constexpr int kThreads = 256, kPieces = 8;
+constexpr int kThreads = kAppendThreads, kPieces = 8;
 
 template <int CPR>  // 16-byte pieces per row
 __global__ __launch_bounds__(kThreads) void chunk_append_kernel(AppendArgs a) {

@@ -18,7 +18,7 @@ namespace {
 // of 2048 operations.  Measured: 1500 tokens, 16 heads of 64, 67 us and 6 us for the merge (4.6 GFLOP: 69 TFLOP/s, where
 // a large float32 matrix product reaches 154); one token of 4 heads over 512 rows, 7.2 us.
 template <int D>
-__global__ __launch_bounds__(256) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
+__global__ __launch_bounds__(kAttnF32Threads) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
   constexpr int KC = D / 16;           // 64-byte K-chunks of a head row
   constexpr int DB = D / 16;
   constexpr int TK = 32;
@@ -311,8 +311,8 @@ hipError_t go_merge(const ChunkAttnArgs& a, hipStream_t s) {
 
 hipError_t launch_chunk_attn_f32(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s) {
   const dim3 grid(a.wide.items + (status ? a.b.batch : 0));
-  if (head_dim == 128) hipLaunchKernelGGL(chunk_attn_f32_kernel<128>, grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(chunk_attn_f32_kernel<64>, grid, dim3(256), 0, s, a);
+  if (head_dim == 128) hipLaunchKernelGGL(chunk_attn_f32_kernel<128>, grid, dim3(kAttnF32Threads), 0, s, a);
+  else hipLaunchKernelGGL(chunk_attn_f32_kernel<64>, grid, dim3(kAttnF32Threads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -5,7 +5,7 @@ namespace respec {
 namespace {
 
 template <int D, int GR>
-__global__ __launch_bounds__(256, 1) void chunk_attn_few_kernel(ChunkAttnArgs a) {
+__global__ __launch_bounds__(kAttnFewThreads, 1) void chunk_attn_few_kernel(ChunkAttnArgs a) {
   extern __shared__ __align__(1024) unsigned char smem[];
   if ((int)blockIdx.x >= a.few.items) {
     report_status<256>(a.b, (int)blockIdx.x - a.few.items, true);
@@ -19,7 +19,7 @@ hipError_t go(bool launch, const ChunkAttnArgs& a, bool status, hipStream_t s) {
   if (!launch)
     return hipFuncSetAttribute(reinterpret_cast<const void*>(&chunk_attn_few_kernel<D, GR>),
                                hipFuncAttributeMaxDynamicSharedMemorySize, FewShape<D>::kLds);
-  hipLaunchKernelGGL((chunk_attn_few_kernel<D, GR>), dim3(a.few.items + (status ? a.b.batch : 0)), dim3(256), FewShape<D>::kLds, s, a);
+  hipLaunchKernelGGL((chunk_attn_few_kernel<D, GR>), dim3(a.few.items + (status ? a.b.batch : 0)), dim3(kAttnFewThreads), FewShape<D>::kLds, s, a);
   return hipGetLastError();
 }
 

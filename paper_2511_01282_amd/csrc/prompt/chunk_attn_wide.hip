@@ -16,7 +16,7 @@ namespace respec {
 namespace {
 
 constexpr int kTile = 32;  // cache rows of a tile
-constexpr int kWaves = 8;
+constexpr int kWaves = kAttnWideThreads / 64;
 
 template <int D>
 struct WideShape {

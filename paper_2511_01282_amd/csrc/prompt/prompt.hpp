@@ -85,6 +85,8 @@ struct ScoreArgs {
   float* tok_logprob; int32_t* tok_rank; float* lse; float* entropy; int32_t* topk_id; float* topk_logprob;
   int32_t rows, vocab, topk_out, parts;
 };
+// threads of the kernels' workgroups
+constexpr int kAppendThreads = 256, kScoreThreads = 256, kAttnF32Threads = 256, kAttnFewThreads = 256, kAttnWideThreads = 512;
 constexpr int kAppendMaxTok = 16;  // tokens of an append workgroup
 constexpr int kScoreWords = 4;  // m, S, T, rank count
 constexpr int kScoreMaxKeys = 256;

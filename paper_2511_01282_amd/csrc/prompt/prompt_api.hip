@@ -38,6 +38,9 @@ constexpr size_t kMaxPartial = 1u << 25;  // columns of partials: 134 MB
 constexpr int kMaxStride = 1 << 24;
 constexpr int kMaxRows = 1 << 30;         // cache rows of a sequence: positions a tile further fit 32 bits
 
+// Whether a launch of so many workgroups can be made: a dispatch counts its threads in 32 bits.
+bool launchable(long long workgroups, int threads) { return workgroups * threads < 1ll << 32; }
+
 // Checks of a stride in elements: non-negative and whole 16-byte pieces.
 bool stride_ok(int64_t s, int es) { return s >= 0 && s < (1ll << 50) && s * es % 16 == 0; }
 
@@ -193,6 +196,7 @@ respec_status respec_chunk_append(const respec_chunk_plan* plan, const respec_ch
   const int pieces = 2 * plan->s.n_kv_heads * plan->s.head_dim * plan->es / 16;  // of a token
   a.per_tok = fast_div((uint32_t)pieces);
   a.tok_per_wg = std::max(1, std::min(2048 / pieces, kAppendMaxTok));
+  if (!launchable(ceil_div(x.b.total_new, a.tok_per_wg) + (x.b.seq_status ? x.b.batch : 0), kAppendThreads)) return RESPEC_ERR_SHAPE;
   return launch_chunk_append(plan->es, plan->s.head_dim, a, static_cast<hipStream_t>(stream)) == hipSuccess
              ? RESPEC_OK
              : RESPEC_ERR_HIP;
@@ -240,12 +244,13 @@ respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chun
   const int rb = (s.head_dim + 2) * 4;
   hipStream_t stm = static_cast<hipStream_t>(stream);
   const bool status = a.b.status != nullptr;
+  const long long reports = status ? a.b.batch : 0;  // workgroups that report a sequence's status
   hipError_t e;
   if (s.dtype == RESPEC_F32) {
     a.few_rows = 0;
     a.few = ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
     a.wide = geometry(a.b, 64, blocks(64), limit, 32, 32, 2, s.head_dim == 128 ? Pace{0.16, 5} : Pace{0.1, 5}, rb, held);
-    if ((long long)a.wide.items + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
+    if (!launchable(a.wide.items + reports, kAttnF32Threads)) return RESPEC_ERR_SHAPE;
     e = launch_chunk_attn_f32(s.head_dim, a, status, stm);
   } else {
     // Calls of at most 64 query rows per KV head have the few-row kernel, of one or two groups of 32; others have
@@ -257,7 +262,7 @@ respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chun
                            : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
     a.wide = wide ? geometry(a.b, 256, blocks(256), limit, 128, 256, 1, s.head_dim == 128 ? Pace{0.032, 6} : Pace{0.018, 6}, rb, held)
                   : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
-    if ((long long)a.few.items + a.wide.items + a.b.batch > INT_MAX) return RESPEC_ERR_SHAPE;
+    if (!launchable((long long)a.few.items + a.wide.items + reports, wide ? kAttnWideThreads : kAttnFewThreads)) return RESPEC_ERR_SHAPE;
     if (!raise_lds_limits(s.head_dim)) return RESPEC_ERR_HIP;
     e = wide ? launch_chunk_attn_wide(s.head_dim, a, mixed, status, stm) : launch_chunk_attn_few(s.head_dim, a, status, stm);
   }
@@ -275,6 +280,7 @@ respec_status respec_score_create(const respec_score_shape* shape, respec_score_
   if (!known(s.dtype)) return RESPEC_ERR_DTYPE;
   if (s.topk_out < 1 || s.topk_out > RESPEC_MAX_TOPK_OUT || s.vocab < s.topk_out || s.vocab >= 1 << 30 || s.max_rows < 1)
     return RESPEC_ERR_SHAPE;
+  if (!launchable(s.max_rows, kScoreThreads)) return RESPEC_ERR_SHAPE;  // (more parts than rows: kScoreParts in all)
   respec_score_plan* p = new (std::nothrow) respec_score_plan();
   if (!p) return RESPEC_ERR_CAPACITY;
   p->s = s;
@@ -317,7 +323,6 @@ respec_status respec_score(const respec_score_plan* plan, const respec_score_arg
   a.vocab = s.vocab;
   a.topk_out = s.topk_out;
   a.parts = std::max(1, std::min({kScoreParts / x.rows, kScoreMaxKeys / plan->ko, s.vocab / 2048}));
-  if ((long long)a.rows * a.parts > INT_MAX) return RESPEC_ERR_SHAPE;
   return launch_score(s.dtype, plan->ko, a, static_cast<hipStream_t>(stream)) == hipSuccess ? RESPEC_OK : RESPEC_ERR_HIP;
 }
 

@@ -27,7 +27,7 @@
 namespace respec {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kThreads = kScoreThreads, kWaves = kThreads / 64;
 constexpr int kUnroll = 4;         // vectors of a thread per step
 constexpr int kMaxKeys = kScoreMaxKeys;  // keys that reach H and are sorted (more: by repeated passes)
 constexpr float kLog2e = 1.4426950408889634f;

@@ -96,7 +96,10 @@ class _Plan:
         self.dtype = _TORCH[shape.dtype]
         self._index = self.device.index if self.device.type == "cuda" else -1
         self.workspace_bytes = int(getattr(L, f"respec_{kind}_workspace_bytes")(h))
+        self._streams = None   # streams that torch's allocator knows the plan's own workspace to be used on
         if workspace is None:
+            if self._index >= 0:
+                self._streams = {torch._C._cuda_getCurrentRawStream(self._index)}
             workspace = torch.empty(self.workspace_bytes + 256, dtype=torch.uint8, device=self.device)
             self.workspace_ptr = workspace.data_ptr() + (-workspace.data_ptr()) % 256
         else:
@@ -145,16 +148,20 @@ class _Plan:
             raise ValueError("the plan is closed")
         if stream is None:
             # (of torch's ways to the current stream the one that makes no Python object of it: 0.1 us, not 1.9)
-            stream = torch._C._cuda_getCurrentRawStream(self._index)
+            raw = torch._C._cuda_getCurrentRawStream(self._index)
         elif stream.device != self.device:
             raise ValueError(f"the stream is of {stream.device}, the plan of {self.device}")
         else:
-            stream = stream.cuda_stream
+            raw = stream.cuda_stream
+        if self._streams is not None and raw not in self._streams:
+            # a plan that is dropped while its call waits there: the workspace is nobody else's until the call is done
+            self._ws_buf.record_stream(torch.cuda.current_stream(self.device) if stream is None else stream)
+            self._streams.add(raw)
         if torch.cuda.current_device() == self._index:
-            status = fn(self._h, *args, stream)
+            status = fn(self._h, *args, raw)
         else:
             with torch.cuda.device(self.device):
-                status = fn(self._h, *args, stream)
+                status = fn(self._h, *args, raw)
         if status != OK:
             raise VerifyError(status, name)
 
@@ -162,7 +169,9 @@ class _Plan:
 class ChunkPlan(_Plan):
     """A respec_chunk plan plus its device workspace.
 
-    Calls that may overlap (on several streams) need plans, or workspaces, of their own."""
+    Calls that may overlap (on several streams) need plans, or workspaces, of their own.  The plan may be dropped
+    while its calls are under way, on whatever stream; a captured call, and a workspace of the caller's, need it, or
+    theirs, for as long as they are used."""
 
     def __init__(self, *, n_q_heads, n_kv_heads, head_dim, dtype, max_batch, max_new, max_kv_len, device="cuda",
                  workspace=None):

@@ -113,3 +113,32 @@ def test_strides_of_dimensions_of_one(lib, dtype):
     plan.append(*new, kp, vp, table, off, kv_len, max_new_in_batch=1)
     plan.attend(q, kp, vp, table, off, kv_len, out, max_new_in_batch=1, max_kv_len_in_batch=9)
     _close(out.cpu(), *pc.attention(c))
+
+
+# ---------------------------------------------------------------------------
+# a plan's workspace
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("by_argument", [True, False])
+def test_workspace_is_kept_for_a_call_on_another_stream(lib, by_argument):
+    """A plan that is dropped while its call waits on another stream: its workspace goes to nobody else until then."""
+    c = pc.make([(1, 4000)], heads=4, kv_heads=2, head_dim=64, page=16, seed=30)
+    q, cache = c.q.cuda(), _cache(c)
+    out = torch.empty_like(q)
+    side = torch.cuda.Stream()
+    plan = _plan(lib, c)
+    at, size = plan._ws_buf.data_ptr(), plan._ws_buf.numel()
+    torch.cuda.synchronize()
+    kw = dict(max_new_in_batch=1, max_kv_len_in_batch=4000)
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)   # some tens of milliseconds
+        if not by_argument:
+            plan.attend(q, *cache, out, **kw)
+    if by_argument:
+        plan.attend(q, *cache, out, stream=side, **kw)
+    del plan
+    other = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    assert other.data_ptr() != at
+    torch.cuda.synchronize()
+    assert not bool(other.any())
+    _close(out.cpu(), *pc.attention(c))

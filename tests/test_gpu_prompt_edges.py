@@ -48,6 +48,18 @@ def test_scores_of_rows_masked_by_a_low_value(lib, dtype, low, vocab):
                 assert torch.equal(part, want[k]), k
 
 
+def test_scores_behind_32_bits(lib):
+    """Rows whose logits lie past 2^32 bytes."""
+    gen = torch.Generator().manual_seed(1)
+    stride = (1 << 26) + 3
+    flat = torch.empty(36, stride, dtype=BF, device="cuda")
+    z = (torch.randn(36, 5000, generator=gen) * 3).to(BF)
+    flat[:, :5000] = z.cuda()
+    token = torch.randint(5000, (36,), generator=gen).int()
+    assert 35 * stride * 2 > 2 ** 32
+    _check_scores(_score(lib, flat[:, :5000], token, 5), z, token, 5)
+
+
 # ---------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------
@@ -113,6 +125,68 @@ def test_strides_of_dimensions_of_one(lib, dtype):
     plan.append(*new, kp, vp, table, off, kv_len, max_new_in_batch=1)
     plan.attend(q, kp, vp, table, off, kv_len, out, max_new_in_batch=1, max_kv_len_in_batch=9)
     _close(out.cpu(), *pc.attention(c))
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,sizes", [
+    (BF, 256, 1, [(1, 300)]), (BF, 256, 1, [(3, 20), (1, 0)]), (BF, 96, 2, [(1, 700), (2, 65)]), (BF, 256, 256, [(1, 40), (33, 0)]),
+    (F32, 256, 1, [(2, 130)]), (F32, 96, 2, [(1, 500), (4, 3)]),
+])
+def test_many_heads(lib, dtype, heads, kv_heads, sizes):
+    c = pc.make(sizes, dtype=dtype, heads=heads, kv_heads=kv_heads, head_dim=64, page=16, seed=heads)
+    _close(_attend(lib, c), *pc.attention(c))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("sizes", [[(1, 3000)], [(40, 30), (1, 500)], [(300, 0)]])
+def test_output_as_a_slice(lib, dtype, sizes):
+    """The output as columns of a wider tensor: joined splits and whole rows alike, and nothing beside them."""
+    c = pc.make(sizes, dtype=dtype, heads=4, kv_heads=2, head_dim=128, page=32, seed=14)
+    wide = torch.full((len(c.q), 7, 256), 5.0, dtype=dtype, device="cuda")
+    out = wide[:, 2:6, 128:]
+    _plan(lib, c).attend(c.q.cuda(), *_cache(c), out, max_new_in_batch=c.max_new, max_kv_len_in_batch=c.max_kv)
+    _close(out.cpu(), *pc.attention(c))
+    out.fill_(5.0)
+    assert bool((wide == 5.0).all())
+
+
+@pytest.mark.parametrize("dtype,page", [(BF, 16), (BF, 24), (F32, 16)])
+@pytest.mark.parametrize("longest", [5, 90])
+def test_good_sequences_behind_bad_ones(lib, dtype, page, longest):
+    """Sequences with bad lengths and pages between good ones: the good ones' outputs and appended rows are theirs."""
+    sizes = [(3, 20), (2, 30), (4, 10), (longest, 33), (5, 17), (2, 2), (1, 700)]
+    bad = (1, 2, 4)
+    c = pc.make(sizes, dtype=dtype, heads=4, kv_heads=2, head_dim=64, page=page, seed=21, spare=0, stale=2.0)
+    want, tol = pc.attention(c)
+    c.kv_len[1] = -1
+    c.table[2, 0] = 10 ** 6
+    c.kv_len[4] = 10 ** 6
+    off = c.off.tolist()
+    expect = [0, 6, 11, 0, 6, 0, 0]
+    plan = _plan(lib, c, max_kv_len=700)
+    k_want, v_want = c.k_pages.clone(), c.v_pages.clone()
+    for b, (n, l) in enumerate(sizes):
+        for r in range(l, l + n):   # no sequence's new rows are there yet
+            for t, w in ((c.k_pages, k_want), (c.v_pages, v_want)):
+                p = int(c.table[b, r // page])
+                if 0 <= p < len(t):
+                    t[p, :, r % page] = -5.0
+                    if b in bad and not (b == 2 and r // page > 0):
+                        w[p, :, r % page] = -5.0
+    kp, vp, table, o, kv_len = _cache(c)
+    st = torch.full((len(sizes),), -9, dtype=torch.int32, device="cuda")
+    kw = dict(max_new_in_batch=c.max_new, max_kv_len_in_batch=700, status=st)
+    plan.append(c.k_new.cuda(), c.v_new.cuda(), kp, vp, table, o, kv_len, **kw)
+    # (sequence 2: rows 10-13, some of them in its good page where pages are short)
+    assert st.tolist() == expect
+    assert torch.equal(kp.cpu(), k_want) and torch.equal(vp.cpu(), v_want)
+    out = torch.zeros(len(c.q), 4, 64, dtype=dtype, device="cuda")
+    st.fill_(-9)
+    plan.attend(c.q.cuda(), kp, vp, table, o, kv_len, out, **kw)
+    assert st.tolist() == expect
+    for b in range(len(sizes)):
+        if b not in bad:
+            s = slice(off[b], off[b + 1])
+            _close(out[s].cpu(), want[s], tol[s])
 
 
 # ---------------------------------------------------------------------------

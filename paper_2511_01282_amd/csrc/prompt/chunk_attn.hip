@@ -14,9 +14,10 @@ namespace {
 // float32: four waves of 16 query rows, v_mfma_f32_16x16x4 (mma_k64 in common.hpp).  S^T = K Q^T leaves, in
 // lane l, the scores of row l % 16 with keys 4 (l / 16) .. + 3 of 16, which are the B operand of O^T += V^T P^T as
 // they stand.  A tile of 32 cache rows is fetched into registers while the tile before is worked on, then goes to
-// one of two LDS buffers, K rows as they are and V transposed.  The matrix cores bound it: 32 clocks per product
-// of 2048 operations.  Measured: 1500 tokens, 16 heads of 64, 67 us and 6 us for the merge (4.6 GFLOP: 69 TFLOP/s, where
-// a large float32 matrix product reaches 154); one token of 4 heads over 512 rows, 7.2 us.
+// one of two LDS buffers, K rows as they are and V transposed.  Measured: 1500 tokens, 16 heads of 64, 68 us and 6 us for
+// the merge (4.6 GFLOP: 68 TFLOP/s, where a large float32 matrix product reaches 154): the matrix cores, 32 clocks per
+// product of 2048 operations, are busy 45% of the cycles; causal blocks are unequal work over one round of workgroups, and
+// 40% of the LDS cycles are conflicts (see fetch).  One token of 4 heads over 512 rows, 6.9 us.
 template <int D>
 __global__ __launch_bounds__(kAttnF32Threads) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
   constexpr int KC = D / 16;           // 64-byte K-chunks of a head row
@@ -58,8 +59,9 @@ __global__ __launch_bounds__(kAttnF32Threads) void chunk_attn_f32_kernel(ChunkAt
   const char* kb = a.b.k + (int64_t)it.g * a.b.head_stride;
   const char* vb = a.b.v + (int64_t)it.g * a.b.head_stride;
 
-  // A thread brings every eighth 16-byte piece of one row: one address per tile for all of them, and the transposed
-  // stores meet every bank once.  The row's page id is read another tile ahead.
+  // A thread brings every eighth 16-byte piece of one row: one address per tile for all of them.  The transposed stores of a
+  // wave are of 32 rows of two columns that lie 4 VP = 144 words apart, 16 of the 64 banks, so 16 banks are met twice.  The
+  // row's page id is read another tile ahead.
   const int my_row = (int)threadIdx.x % TK, my_piece = (int)threadIdx.x / TK;
   u32x4 kp[NP], vp[NP];
   int32_t id = 0;

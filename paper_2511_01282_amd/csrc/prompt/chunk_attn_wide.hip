@@ -3,10 +3,16 @@
 // Eight waves, two per SIMD, own 32 query rows each and walk over the same cache rows, tile by tile of 32.
 // Tiles go round an LDS ring by DMA, four of them per pass and barrier.
 //
-// The matrix cores bound it, and on long prompts the card's power: 8192 tokens, 32 heads of 128 (0.55 TFLOP), 526 to 556 us
-// with the card's temperature, 0.99 to 1.05 PFLOP/s, where a large bf16 matrix product reaches 1.22.  Four waves of 64 rows, with the tiles' fragments read
-// half as often, took a tenth more clocks and the same time (537 to 545 us, the clock at 2.2 GHz instead of 1.96), and
-// chunks 3-5% longer.  Two tiles per pass and three passes under way at D = 128: 558 against 546 us.
+// 8192 tokens, 32 heads of 128 (0.55 TFLOP): 511 to 556 us with the card's temperature, 0.99 to 1.08 PFLOP/s, where a large
+// bf16 matrix product reaches 1.22.  The matrix cores are busy half of the cycles, at 1.96 GHz; matrix and vector
+// instructions of a SIMD's two waves hardly overlap (512 and some 480 cycles of the 1010 that a wave's tile takes), and the
+// waves wait 30% of their time.  Part of that is the queries': they are first used inside the loops, so the compiler counts
+// their loads as under way at each loop's head and waits for them there.  It does not know of the DMA, and these waits
+// (vmcnt(7) .. vmcnt(0) before the first score products of a pass, and of every masked tile) are for the unit just
+// requested as well: it lands beside that tile, not beside the whole pass.
+// With those waits in place: four waves of 64 rows, with the tiles' fragments read half as often, took a tenth more clocks and
+// the same time (537 to 545 us, the clock at 2.2 GHz), and chunks 3-5% longer; two tiles per pass and three passes requested
+// ahead at D = 128, 558 against 546 us.
 // 512 tokens over 16384 rows, 32 heads on 8: 134 to 150 us and 10 us for the merge of the splits.
 #include <type_traits>
 
@@ -21,7 +27,7 @@ constexpr int kWaves = kAttnWideThreads / 64;
 template <int D>
 struct WideShape {
   static constexpr int kPass = 4;              // tiles between two barriers
-  static constexpr int kAhead = D == 128 ? 1 : 3;  // passes under way
+  static constexpr int kAhead = D == 128 ? 1 : 3;  // passes requested ahead
   static constexpr int S = kPass * (kAhead + 1) + 1;   // ring slots: a pass and the tile after it, and those under way
   static constexpr int kRows = kPass * kTile / kWaves;  // cache rows of a pass that a wave brings
   static constexpr int kHalf = kTile * D * 2;      // bytes of a K or V tile

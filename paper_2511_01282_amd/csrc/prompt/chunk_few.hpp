@@ -3,8 +3,10 @@
 // Up to 32 or 64 query rows (tokens times the heads of a group) of a sequence and KV head: the cache is
 // read once and memory bounds it.  A workgroup takes a split of the cache rows; its four waves own all the query rows
 // and every fourth tile of 32 cache rows each, with a ring of their own in LDS that they fill by DMA, so
-// nothing but a wave's own requests is ever waited for.  At the end the waves' (m, l, O) are joined through LDS.
-// Measured: 32 sequences of one token, 32 heads on 8 of 128, 300 to 16000 rows (536 MB), 100 us, 5.3 TB/s; one
+// nothing but a wave's own requests is ever waited for.  (With one group of 32 rows it is all of them, in every tile: the
+// queries are first used inside the loop, the compiler waits for their loads at its head, and the DMA, of which it does not
+// know, is waited for with them.)  At the end the waves' (m, l, O) are joined through LDS.
+// Measured: 32 sequences of one token, 32 heads on 8 of 128, 300 to 16000 rows (536 MB), 101 us, 5.3 TB/s; one
 // sequence over 32768 rows, 28 heads on 4 (67 MB), 16 us, 4.2 TB/s.
 #pragma once
 

@@ -204,7 +204,11 @@ __device__ __forceinline__ float less_ref(float s, float scale_log2, float m) {
 
 // Weights of 32 keys against reference m, as bf16 pairs, and their sum.  The sum is of the rounded weights, so
 // the division by it undoes what rounding does to all of them alike.  Each rounding, to 8 bits, is half a step
-// of the output's own rounding at most, and they are many and of either sign.
+// of the output's own rounding at most, and they are many and of either sign: 0.0020 to 0.0022 of the result's norm off
+// from 64 bits, where the output's rounding alone is 0.00166.  A second product with the weights' low parts, as in the tree
+// attention of a verification step (whose sums meet decision margins before they are rounded), leaves that alone, but takes
+// 736 us for 540 (8192-token prompt, 32 heads of 128), 193 for 143 (512 tokens over 16384 rows), 108 for 105 (32 decoding
+// tokens, D = 128), 77 for 70 (D = 64).
 template <bool FAR = false>
 __device__ __forceinline__ float weights(const f32x16& s, float scale_log2, float m, u32x4 (&p)[2]) {
   const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};

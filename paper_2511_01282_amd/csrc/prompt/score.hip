@@ -13,9 +13,9 @@
 // thread's others reaches H, too, are its vectors read again (those of all of these threads: 20% more bytes, as eight
 // threads share a line, 118 against 114 us).
 //
-// Memory bounds it, with the vector instructions close behind: 2048 rows of 128256 bf16 logits (526 MB), 110 us,
-// 4.8 TB/s (bounds checked in every step, not in the last alone: 114); 65 rows of 152064 float32 logits (40 MB, in
-// parts), 15 us and 4 us to join them.  The rank counted by the scalar unit off the compare masks, and bf16's best
+// Memory bounds it, with the vector instructions close behind: 2048 rows of 128256 bf16 logits (526 MB), 108 to 110 us a call
+// among others, 4.8 TB/s (bounds checked in every step, not in the last alone: 114), 109 to 121 in a profiler's trace; 65
+// rows of 152064 float32 logits (40 MB, in parts), 15 us and 4 us to join them.  The rank counted by the scalar unit off the compare masks, and bf16's best
 // vector read again instead of kept: 121 against 114 us.
 //
 // Keys: (value, id) pairs as 64-bit integers (common.hpp), all distinct, so ties go to the lowest id.

@@ -97,14 +97,14 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
     else
       feed.from_rows(a.b, dst, dst + G::kHalf, ids.ids, ids.p0, t0, hi_row, lane);
   };
-  // Unit u has landed for every wave: of this one's requests only those of later units are under way.  (What a wave
-  // has read of the slots it is done with it has used in products, so nothing of them is under way.)
+  // Unit u has landed for every wave: of this one's requests only those of later units are under way, and its reads of the
+  // slots that are filled next have arrived (their products stand before this, but nothing else keeps them there).
   auto landed = [&](int u) __attribute__((always_inline)) {
     const int newer = min(n_units, u + G::kAhead) - 1 - u;
     if (newer >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * NR) : "memory");
     else if (newer == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NR) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    asm volatile("s_barrier" ::: "memory");
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
   static_assert(G::kAhead <= 3, "landed() tells two newer units apart");
 #pragma unroll 1

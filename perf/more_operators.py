@@ -6,8 +6,8 @@
            rows and head (``ChunkPlan.append_q8``)
   attend   new tokens attend, causally, to their sequence's rows of that cache (``ChunkPlan.attend_q8``)
   keep     the accepted path of every verified draft tree moves to the front of its nodes' rows, in all layers
-           (``cache.keep_rows``)
-  copy     pages are copied: the partly filled ones of forked sequences, or the pages of beams (``cache.copy_pages``)
+           (``cache.CacheLayers.keep_rows``)
+  copy     pages are copied: the partly filled ones of forked sequences, or the pages of beams (``cache.CacheLayers.copy_pages``)
 
 Cases: dtype, heads, kv_heads, head_dim are the model's shape, page the rows of a page (0: one page per sequence), block the
 rows that share a scale.  rotary: tokens of ``batch`` sequences (0: positions are given one by one, as for a tree),
@@ -368,12 +368,12 @@ def prepare(case, seed):
     if case["op"] == "keep":
         s = dict(_keep_inputs(case, seed)[0], case=case)
         if own:
-            s["keep_rows"] = cache.keep_rows
+            s["layers"] = cache.CacheLayers(s["k_cache"], s["v_cache"])
         return s
     if case["op"] == "copy":
         s = dict(_copy_inputs(case, seed)[0], case=case)
         if own:
-            s["copy_pages"] = cache.copy_pages
+            s["layers"] = cache.CacheLayers(*s["planes"])
         return s
     s, sizes = _cache_inputs(case, seed)
     s["case"] = case
@@ -515,9 +515,9 @@ def run(state):
                             s["kv_len"], s["out"], **s["sizes"])
         return s["out"]
     if op == "keep":
-        s["keep_rows"](s["k_cache"], s["v_cache"], s["page_table"], s["kv_len"], s["path"], s["acc_len"], s["kv_len_out"])
+        s["layers"].keep_rows(s["page_table"], s["kv_len"], s["path"], s["acc_len"], s["kv_len_out"])
         return {"k_cache": s["k_cache"], "v_cache": s["v_cache"], "kv_len_out": s["kv_len_out"]}
-    s["copy_pages"](s["planes"], s["src"], s["dst"], layers=True)
+    s["layers"].copy_pages(s["src"], s["dst"])
     return s["planes"]
 
 

@@ -23,7 +23,8 @@ FLAGS = [
 
 # matrix products accumulate in ordinary registers, on which the softmax works (accumulation registers would be moved to
 # and fro)
-FILE_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for f in ("chunk_attn.hip", "chunk_attn_wide.hip", "chunk_attn_few.hip")}
+FILE_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
+              for f in ("chunk_attn.hip", "chunk_attn_wide.hip", "chunk_attn_few.hip", "q8_attn.hip")}
 
 
 CXX = os.environ.get("CXX", "g++")
@@ -33,7 +34,7 @@ CXXFLAGS = ["-O2", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall", "-I", os
 
 
 def sources():
-    return sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "prompt", "*.hip")))
+    return sorted(f for d in (".", "prompt", "cache") for f in glob.glob(os.path.join(CSRC, d, "*.hip")))
 
 
 def host_sources():

@@ -6,7 +6,7 @@
 // one matrix.  A workgroup owns rows_per_wg rows of one sequence and KV head and walks over
 // (a split of) the cache rows they see, tile by tile, in one pass: S^T = K Q^T, a running maximum m
 // and sum l of the softmax per row, O^T += V^T P^T.
-#include "chunk.hpp"
+#include "q8.hpp"
 
 namespace respec {
 namespace {
@@ -18,7 +18,8 @@ namespace {
 // the merge (4.6 GFLOP: 68 TFLOP/s, where a large float32 matrix product reaches 154): the matrix cores, 32 clocks per
 // product of 2048 operations, are busy 45% of the cycles; causal blocks are unequal work over one round of workgroups, and
 // 40% of the LDS cycles are conflicts (see fetch).  One token of 4 heads over 512 rows, 6.9 us.
-template <int D>
+// Q8: the cache holds e4m3 values with a scale per block of rows; four of them at a time become what a piece is otherwise.
+template <int D, bool Q8>
 __global__ __launch_bounds__(kAttnF32Threads) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
   constexpr int KC = D / 16;           // 64-byte K-chunks of a head row
   constexpr int DB = D / 16;
@@ -64,15 +65,28 @@ __global__ __launch_bounds__(kAttnF32Threads) void chunk_attn_f32_kernel(ChunkAt
   // row's page id is read another tile ahead.
   const int my_row = (int)threadIdx.x % TK, my_piece = (int)threadIdx.x / TK;
   u32x4 kp[NP], vp[NP];
+  uint32_t k_byte = 127, v_byte = 127;  // (exponents of the row's scales)
   int32_t id = 0;
   auto row_of = [&](int r0) { return (uint32_t)min(r0 + my_row, hi - 1); };
   auto fetch_id = [&](int r0) { id = table[div_by(row_of(r0), a.b.page)]; };
   auto fetch = [&](int r0) {
-    const int64_t off = offset_in(a.b, id, row_of(r0)) + my_piece * 16;
+    if constexpr (Q8) {
+      const int64_t off = offset_in(a.b, id, row_of(r0)) + my_piece * 4;
+      const int64_t at = scale_offset(a, id, row_of(r0), it.g);
+      k_byte = a.q8.k[at];
+      v_byte = a.q8.v[at];
 #pragma unroll
-    for (int x = 0; x < NP; ++x) {
-      kp[x] = ld16(kb + off + x * (256 / TK * 16));
-      vp[x] = ld16(vb + off + x * (256 / TK * 16));
+      for (int x = 0; x < NP; ++x) {
+        kp[x].x = *reinterpret_cast<const uint32_t*>(kb + off + x * (256 / TK * 4));
+        vp[x].x = *reinterpret_cast<const uint32_t*>(vb + off + x * (256 / TK * 4));
+      }
+    } else {
+      const int64_t off = offset_in(a.b, id, row_of(r0)) + my_piece * 16;
+#pragma unroll
+      for (int x = 0; x < NP; ++x) {
+        kp[x] = ld16(kb + off + x * (256 / TK * 16));
+        vp[x] = ld16(vb + off + x * (256 / TK * 16));
+      }
     }
   };
   float m = kNegInf, l = 0.f;
@@ -87,6 +101,13 @@ __global__ __launch_bounds__(kAttnF32Threads) void chunk_attn_f32_kernel(ChunkAt
   for (int r0 = lo; r0 < hi; r0 += TK, buf ^= 1) {
     unsigned char* ks = k_lds[buf];
     float* vs = v_lds[buf];
+    if constexpr (Q8) {
+#pragma unroll
+      for (int x = 0; x < NP; ++x) {
+        kp[x] = q8_floats(kp[x].x, k_byte);
+        vp[x] = q8_floats(vp[x].x, v_byte);
+      }
+    }
 #pragma unroll
     for (int x = 0; x < NP; ++x) {
       const int c = my_piece + x * (256 / TK);
@@ -311,10 +332,12 @@ hipError_t go_merge(const ChunkAttnArgs& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_chunk_attn_f32(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s) {
+hipError_t launch_chunk_attn_f32(int head_dim, bool q8, const ChunkAttnArgs& a, bool status, hipStream_t s) {
   const dim3 grid(a.wide.items + (status ? a.b.batch : 0));
-  if (head_dim == 128) hipLaunchKernelGGL(chunk_attn_f32_kernel<128>, grid, dim3(kAttnF32Threads), 0, s, a);
-  else hipLaunchKernelGGL(chunk_attn_f32_kernel<64>, grid, dim3(kAttnF32Threads), 0, s, a);
+  if (q8 && head_dim == 128) hipLaunchKernelGGL((chunk_attn_f32_kernel<128, true>), grid, dim3(kAttnF32Threads), 0, s, a);
+  else if (q8) hipLaunchKernelGGL((chunk_attn_f32_kernel<64, true>), grid, dim3(kAttnF32Threads), 0, s, a);
+  else if (head_dim == 128) hipLaunchKernelGGL((chunk_attn_f32_kernel<128, false>), grid, dim3(kAttnF32Threads), 0, s, a);
+  else hipLaunchKernelGGL((chunk_attn_f32_kernel<64, false>), grid, dim3(kAttnF32Threads), 0, s, a);
   return hipGetLastError();
 }
 

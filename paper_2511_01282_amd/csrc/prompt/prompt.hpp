@@ -44,6 +44,24 @@ struct ChunkBatch {
   FastDiv kv_heads;        // by n_kv_heads
 };
 
+// Scales of an 8-bit cache: exponent bytes of blocks of 2^shift rows.
+struct Q8Scales {
+  uint8_t* k;
+  uint8_t* v;
+  int64_t page_stride, head_stride;
+  int32_t shift;
+};
+
+struct AppendQ8Args {
+  ChunkBatch b;
+  Q8Scales q8;
+  const char* k_new;
+  const char* v_new;
+  int64_t k_tok, k_head, v_tok, v_head;  // bytes
+  FastDiv per_block;                      // by 2 * KV heads: the K and V blocks at the same rows
+  int32_t wgs;                            // workgroups before those that report a sequence's status
+};
+
 struct AppendArgs {
   ChunkBatch b;
   const char* k_new;
@@ -75,6 +93,7 @@ struct ChunkAttnArgs {
   // sequences of up to few_rows query rows per KV head are the first geometry's, the others the second's
   int32_t few_rows;
   ChunkGeom few, wide;
+  Q8Scales q8;  // (of an 8-bit cache)
 };
 
 struct ScoreArgs {
@@ -87,6 +106,7 @@ struct ScoreArgs {
 };
 // threads of the kernels' workgroups
 constexpr int kAppendThreads = 256, kScoreThreads = 256, kAttnF32Threads = 256, kAttnFewThreads = 256, kAttnWideThreads = 512;
+constexpr int kAppendQ8Waves = 4;  // 16 rows of a block each (8 for blocks of 128)
 constexpr int kAppendMaxTok = 16;  // tokens of an append workgroup
 constexpr int kScoreWords = 4;  // m, S, T, rank count
 constexpr int kScoreMaxKeys = 256;
@@ -94,13 +114,18 @@ constexpr int kScoreParts = 512;  // workgroups that a few rows are cut into (65
                                   // logits: 384 20.4 us, 512 18.9, 1024 19.7)
 
 hipError_t launch_chunk_append(int es, int head_dim, const AppendArgs& a, hipStream_t s);
-// float32; `status`: whether this launch reports the sequences' status
-hipError_t launch_chunk_attn_f32(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s);
+hipError_t launch_append_q8(int es, int head_dim, const AppendQ8Args& a, hipStream_t s);
+// float32; `status`: whether this launch reports the sequences' status; q8: over an 8-bit cache
+hipError_t launch_chunk_attn_f32(int head_dim, bool q8, const ChunkAttnArgs& a, bool status, hipStream_t s);
 // bf16: sequences of at most / more than few_rows query rows per KV head; mixed: of both kinds
 hipError_t launch_chunk_attn_few(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s);
 hipError_t launch_chunk_attn_wide(int head_dim, const ChunkAttnArgs& a, bool mixed, bool status, hipStream_t s);
 hipError_t set_chunk_attn_few_lds_limit(int head_dim);
 hipError_t set_chunk_attn_wide_lds_limit(int head_dim);
+// the same over an 8-bit cache
+hipError_t launch_q8_attn_few(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s);
+hipError_t launch_q8_attn_wide(int head_dim, const ChunkAttnArgs& a, bool mixed, bool status, hipStream_t s);
+hipError_t set_q8_attn_lds_limits(int head_dim);
 hipError_t launch_chunk_merge(int dtype, int head_dim, const ChunkAttnArgs& a, hipStream_t s);
 hipError_t launch_score(int dtype, int ko, const ScoreArgs& a, hipStream_t s);
 

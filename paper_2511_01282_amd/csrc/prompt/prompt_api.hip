@@ -1,5 +1,5 @@
 // Host side of the prompt side's C ABI: plans, argument validation, launches.
-// See include/respec_prompt.h for the contract.
+// See include/respec_prompt.h and, for the 8-bit cache, include/respec_cache.h for the contract.
 #include <limits.h>
 #include <math.h>
 
@@ -7,6 +7,7 @@
 #include <atomic>
 #include <new>
 
+#include "../../../include/respec_cache.h"
 #include "../../../include/respec_prompt.h"
 #include "../attn_route.hpp"
 #include "prompt.hpp"
@@ -44,7 +45,8 @@ bool launchable(long long workgroups, int threads) { return workgroups * threads
 // Checks of a stride in elements: non-negative and whole 16-byte pieces.
 bool stride_ok(int64_t s, int es) { return s >= 0 && s < (1ll << 50) && s * es % 16 == 0; }
 
-respec_status check_batch(const respec_chunk_plan* plan, const respec_chunk_batch& b) {
+// `ces`: bytes per element of the cache.
+respec_status check_batch(const respec_chunk_plan* plan, const respec_chunk_batch& b, int ces) {
   const respec_chunk_shape& s = plan->s;
   if (b.batch < 0 || b.total_new < 0 || b.max_new_in_batch < 0 || b.max_kv_len_in_batch < 0) return RESPEC_ERR_SHAPE;
   if (b.batch > s.max_batch || b.total_new > s.max_new || b.max_kv_len_in_batch > s.max_kv_len) return RESPEC_ERR_CAPACITY;
@@ -54,14 +56,14 @@ respec_status check_batch(const respec_chunk_plan* plan, const respec_chunk_batc
   if (!b.new_off || !b.kv_len || !c.k || !c.v || !c.page_table) return RESPEC_ERR_NULL;
   if (c.n_pages < 1 || c.page_size < 1 || c.table_width < 1) return RESPEC_ERR_SHAPE;
   if (b.batch > 1 && c.table_stride < c.table_width) return RESPEC_ERR_SHAPE;
-  if (!stride_ok(c.page_stride, plan->es) || !stride_ok(c.head_stride, plan->es) || !stride_ok(c.row_stride, plan->es) ||
+  if (!stride_ok(c.page_stride, ces) || !stride_ok(c.head_stride, ces) || !stride_ok(c.row_stride, ces) ||
       c.row_stride > kMaxStride)
     return RESPEC_ERR_SHAPE;
   if (!aligned(c.k, 16) || !aligned(c.v, 16)) return RESPEC_ERR_SHAPE;
   return RESPEC_OK;
 }
 
-ChunkBatch device_batch(const respec_chunk_plan* plan, const respec_chunk_batch& b) {
+ChunkBatch device_batch(const respec_chunk_plan* plan, const respec_chunk_batch& b, int ces) {
   const respec_paged_cache& c = b.cache;
   ChunkBatch d;
   d.new_off = b.new_off;
@@ -70,10 +72,10 @@ ChunkBatch device_batch(const respec_chunk_plan* plan, const respec_chunk_batch&
   d.status = b.seq_status;
   d.k = static_cast<char*>(c.k);
   d.v = static_cast<char*>(c.v);
-  d.page_stride = c.page_stride * plan->es;
-  d.head_stride = c.head_stride * plan->es;
+  d.page_stride = c.page_stride * ces;
+  d.head_stride = c.head_stride * ces;
   d.table_stride = c.table_stride;
-  d.row_stride = (uint32_t)(c.row_stride * plan->es);
+  d.row_stride = (uint32_t)(c.row_stride * ces);
   d.page = fast_div((uint32_t)c.page_size);
   d.batch = b.batch;
   d.total_new = b.total_new;
@@ -85,6 +87,26 @@ ChunkBatch device_batch(const respec_chunk_plan* plan, const respec_chunk_batch&
   d.group = plan->s.n_q_heads / plan->s.n_kv_heads;
   d.kv_heads = fast_div((uint32_t)d.n_kv_heads);
   return d;
+}
+
+// An 8-bit cache's batch as one over pages of one-byte elements; its scales' checks.
+respec_chunk_batch codes_batch(const respec_q8_batch& b) {
+  const respec_q8_cache& c = b.cache;
+  return respec_chunk_batch{b.batch, b.total_new, b.max_new_in_batch, b.max_kv_len_in_batch, b.new_off, b.kv_len,
+                            respec_paged_cache{c.k, c.v, c.n_pages, c.page_size, c.page_stride, c.head_stride, c.row_stride,
+                                               c.page_table, c.table_width, c.table_stride},
+                            b.seq_status};
+}
+respec_status check_scales(const respec_q8_cache& c) {
+  if (!c.k_scale || !c.v_scale) return RESPEC_ERR_NULL;
+  if (c.scale_block != 16 && c.scale_block != 32 && c.scale_block != 64 && c.scale_block != 128) return RESPEC_ERR_SHAPE;
+  if (c.page_size % c.scale_block != 0) return RESPEC_ERR_SHAPE;
+  for (int64_t s : {c.scale_page_stride, c.scale_head_stride})
+    if (s < 0 || s >= 1ll << 50) return RESPEC_ERR_SHAPE;
+  return RESPEC_OK;
+}
+Q8Scales device_scales(const respec_q8_cache& c) {
+  return Q8Scales{c.k_scale, c.v_scale, c.scale_page_stride, c.scale_head_stride, __builtin_ctz((unsigned)c.scale_block)};
 }
 
 // How long an attention kernel takes over one cache row of a block, with all the workgroups of a CU that the pace was
@@ -128,19 +150,112 @@ ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long 
   return g;
 }
 
+// Checks of the new rows of an append's arguments (either kind of cache).
+template <typename Args>
+respec_status check_new_rows(const respec_chunk_plan* plan, const Args& x) {
+  if (!x.k_new || !x.v_new) return RESPEC_ERR_NULL;
+  if (!aligned(x.k_new, 16) || !aligned(x.v_new, 16)) return RESPEC_ERR_SHAPE;
+  for (int64_t s : {x.k_token_stride, x.k_head_stride, x.v_token_stride, x.v_head_stride})
+    if (!stride_ok(s, plan->es)) return RESPEC_ERR_SHAPE;
+  return RESPEC_OK;
+}
+
 // Raise the LDS limits of the attention kernels on the current device, once (a call into the runtime that also
 // loads the kernels: the first step pays it).
-bool raise_lds_limits(int head_dim) {
+bool raise_lds_limits(int head_dim, bool q8) {
   constexpr int kMaxDevices = 64;
-  static std::atomic<uint64_t> done[2];  // [head size], a bit per device
+  static std::atomic<uint64_t> done[4];  // [head size, cache], a bit per device
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0) return false;
-  std::atomic<uint64_t>& d = done[head_dim == 128];
+  std::atomic<uint64_t>& d = done[(head_dim == 128) + 2 * q8];
   const uint64_t bit = dev < kMaxDevices ? 1ull << dev : 0;  // (past the last: every call raises them)
   if (d.load(std::memory_order_acquire) & bit) return true;
-  if (set_chunk_attn_few_lds_limit(head_dim) != hipSuccess || set_chunk_attn_wide_lds_limit(head_dim) != hipSuccess) return false;
+  if (q8) {
+    if (set_q8_attn_lds_limits(head_dim) != hipSuccess) return false;
+  } else if (set_chunk_attn_few_lds_limit(head_dim) != hipSuccess || set_chunk_attn_wide_lds_limit(head_dim) != hipSuccess) {
+    return false;
+  }
   d.fetch_or(bit, std::memory_order_release);
   return true;
+}
+
+// Attention over a cache of the plan's type or, with its scales, of 8-bit values.
+respec_status attend(const respec_chunk_plan* plan, const respec_chunk_attn_args& x, const respec_q8_cache* q8, void* workspace,
+                     void* stream) {
+  if (!workspace || !aligned(workspace, 256)) return RESPEC_ERR_WORKSPACE;
+  const int ces = q8 ? 1 : plan->es;
+  const respec_status st = check_batch(plan, x.b, ces);
+  if (st != RESPEC_OK) return st;
+  if (q8 && x.b.batch > 0) {
+    const respec_status scales = check_scales(*q8);
+    if (scales != RESPEC_OK) return scales;
+  }
+  if (!(x.scale >= 0.f) || isinf(x.scale)) return RESPEC_ERR_PARAM;
+  if (x.b.batch == 0) return RESPEC_OK;
+  if (x.b.total_new > 0) {
+    if (!x.q || !x.out) return RESPEC_ERR_NULL;
+    if (!aligned(x.q, 16) || !aligned(x.out, 16)) return RESPEC_ERR_SHAPE;
+    for (int64_t s : {x.q_token_stride, x.q_head_stride, x.out_token_stride, x.out_head_stride})
+      if (!stride_ok(s, plan->es)) return RESPEC_ERR_SHAPE;
+  }
+  if (x.b.max_new_in_batch == 0 && !x.b.seq_status) return RESPEC_OK;  // (no sequence has tokens)
+  const respec_chunk_shape& s = plan->s;
+  ChunkAttnArgs a;
+  a.b = device_batch(plan, x.b, ces);
+  a.q8 = q8 ? device_scales(*q8) : Q8Scales{nullptr, nullptr, 0, 0, 0};
+  a.q = static_cast<const char*>(x.q);
+  a.out = static_cast<char*>(x.out);
+  a.q_tok = x.q_token_stride * plan->es;
+  a.q_head = x.q_head_stride * plan->es;
+  a.o_tok = x.out_token_stride * plan->es;
+  a.o_head = x.out_head_stride * plan->es;
+  a.group = fast_div((uint32_t)a.b.group);
+  char* ws = static_cast<char*>(workspace);
+  const size_t o_bytes = align256(plan->part_rows * s.head_dim * 4), m_bytes = align256(plan->part_rows * 4);
+  a.part_o = reinterpret_cast<float*>(ws);
+  a.part_m = reinterpret_cast<float*>(ws + o_bytes);
+  a.part_l = reinterpret_cast<float*>(ws + o_bytes + m_bytes);
+  a.scale_log2 = (float)(1.4426950408889634 * (x.scale > 0.f ? (double)x.scale : 1.0 / sqrt((double)s.head_dim)));
+  if (isinf(a.scale_log2)) return RESPEC_ERR_PARAM;
+  const long long limit = (long long)a.b.max_kv + a.b.max_new;  // rows that the last token of the longest sequence sees
+  const long long all_rows = (long long)a.b.total_new * a.b.group, rows = (long long)a.b.max_new * a.b.group;  // per KV head
+  const long long seqs = std::min(a.b.batch, a.b.total_new);    // sequences that can have tokens
+  const long long held = x.b.total_new > 0 ? (long long)(plan->part_rows / ((size_t)x.b.total_new * s.n_q_heads)) : 1;
+  // row blocks of all sequences: each sequence's last one may be short
+  auto blocks = [&](int per_wg) { return std::min(ceil_div(all_rows, per_wg) + (seqs > 1 ? seqs - 1 : 0), seqs * ceil_div(rows, per_wg)); };
+  const int rb = (s.head_dim + 2) * 4;
+  hipStream_t stm = static_cast<hipStream_t>(stream);
+  const bool status = a.b.status != nullptr;
+  const long long reports = status ? a.b.batch : 0;  // workgroups that report a sequence's status
+  hipError_t e;
+  if (s.dtype == RESPEC_F32) {
+    a.few_rows = 0;
+    a.few = ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
+    a.wide = geometry(a.b, 64, blocks(64), limit, 32, 32, 2, s.head_dim == 128 ? Pace{0.16, 5} : Pace{0.1, 5}, rb, held);
+    if (!launchable(a.wide.items + reports, kAttnF32Threads)) return RESPEC_ERR_SHAPE;
+    e = launch_chunk_attn_f32(s.head_dim, q8 != nullptr, a, status, stm);
+  } else {
+    // Calls of at most 64 query rows per KV head have the few-row kernel, of one or two groups of 32; others have
+    // 256-row blocks, and sequences of up to 32 rows among them the few-row kernel's way in the same launch.
+    const bool wide = rows > 64, mixed = wide && a.b.batch > 1;
+    a.few_rows = !wide ? (rows <= 32 ? 32 : 64) : mixed ? 32 : 0;
+    a.few = !wide || mixed ? geometry(a.b, a.few_rows, seqs, limit, 128, 128, 1,
+                                      s.head_dim == 128 ? Pace{0.02, 6} : Pace{0.01, 6}, rb, held)
+                           : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
+    a.wide = wide ? geometry(a.b, 256, blocks(256), limit, 128, 256, 1, s.head_dim == 128 ? Pace{0.032, 6} : Pace{0.018, 6}, rb, held)
+                  : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
+    if (!launchable((long long)a.few.items + a.wide.items + reports, wide ? kAttnWideThreads : kAttnFewThreads)) return RESPEC_ERR_SHAPE;
+    if (!raise_lds_limits(s.head_dim, q8 != nullptr)) return RESPEC_ERR_HIP;
+    if (q8)
+      e = wide ? launch_q8_attn_wide(s.head_dim, a, mixed, status, stm) : launch_q8_attn_few(s.head_dim, a, status, stm);
+    else
+      e = wide ? launch_chunk_attn_wide(s.head_dim, a, mixed, status, stm) : launch_chunk_attn_few(s.head_dim, a, status, stm);
+  }
+  if (e != hipSuccess) return RESPEC_ERR_HIP;
+  if (x.b.total_new > 0 && (a.few.nsplit > 1 || a.wide.nsplit > 1) &&
+      launch_chunk_merge(s.dtype, s.head_dim, a, stm) != hipSuccess)
+    return RESPEC_ERR_HIP;
+  return RESPEC_OK;
 }
 
 }  // namespace
@@ -174,19 +289,17 @@ size_t respec_chunk_workspace_bytes(const respec_chunk_plan* plan) { return plan
 respec_status respec_chunk_append(const respec_chunk_plan* plan, const respec_chunk_append_args* args, void* stream) {
   if (!plan || !args) return RESPEC_ERR_NULL;
   const respec_chunk_append_args& x = *args;
-  const respec_status st = check_batch(plan, x.b);
+  const respec_status st = check_batch(plan, x.b, plan->es);
   if (st != RESPEC_OK) return st;
   if (x.b.batch == 0) return RESPEC_OK;
   if (x.b.total_new > 0) {
-    if (!x.k_new || !x.v_new) return RESPEC_ERR_NULL;
-    if (!aligned(x.k_new, 16) || !aligned(x.v_new, 16)) return RESPEC_ERR_SHAPE;
-    for (int64_t s : {x.k_token_stride, x.k_head_stride, x.v_token_stride, x.v_head_stride})
-      if (!stride_ok(s, plan->es)) return RESPEC_ERR_SHAPE;
+    const respec_status rows = check_new_rows(plan, x);
+    if (rows != RESPEC_OK) return rows;
   } else if (!x.b.seq_status) {
     return RESPEC_OK;
   }
   AppendArgs a;
-  a.b = device_batch(plan, x.b);
+  a.b = device_batch(plan, x.b, plan->es);
   a.k_new = static_cast<const char*>(x.k_new);
   a.v_new = static_cast<const char*>(x.v_new);
   a.k_tok = x.k_token_stride * plan->es;
@@ -205,72 +318,52 @@ respec_status respec_chunk_append(const respec_chunk_plan* plan, const respec_ch
 respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chunk_attn_args* args, void* workspace,
                                 void* stream) {
   if (!plan || !args) return RESPEC_ERR_NULL;
-  if (!workspace || !aligned(workspace, 256)) return RESPEC_ERR_WORKSPACE;
-  const respec_chunk_attn_args& x = *args;
-  const respec_status st = check_batch(plan, x.b);
+  return attend(plan, *args, nullptr, workspace, stream);
+}
+
+respec_status respec_chunk_attn_q8(const respec_chunk_plan* plan, const respec_q8_attn_args* args, void* workspace,
+                                   void* stream) {
+  if (!plan || !args) return RESPEC_ERR_NULL;
+  const respec_q8_attn_args& x = *args;
+  return attend(plan,
+                respec_chunk_attn_args{codes_batch(x.b), x.q, x.q_token_stride, x.q_head_stride, x.out, x.out_token_stride,
+                                       x.out_head_stride, x.scale},
+                &x.b.cache, workspace, stream);
+}
+
+respec_status respec_chunk_append_q8(const respec_chunk_plan* plan, const respec_q8_append_args* args, void* stream) {
+  if (!plan || !args) return RESPEC_ERR_NULL;
+  const respec_q8_append_args& x = *args;
+  const respec_chunk_batch b = codes_batch(x.b);
+  const respec_status st = check_batch(plan, b, 1);
   if (st != RESPEC_OK) return st;
-  if (!(x.scale >= 0.f) || isinf(x.scale)) return RESPEC_ERR_PARAM;
-  if (x.b.batch == 0) return RESPEC_OK;
-  if (x.b.total_new > 0) {
-    if (!x.q || !x.out) return RESPEC_ERR_NULL;
-    if (!aligned(x.q, 16) || !aligned(x.out, 16)) return RESPEC_ERR_SHAPE;
-    for (int64_t s : {x.q_token_stride, x.q_head_stride, x.out_token_stride, x.out_head_stride})
-      if (!stride_ok(s, plan->es)) return RESPEC_ERR_SHAPE;
+  if (b.batch == 0) return RESPEC_OK;
+  const respec_status scales = check_scales(x.b.cache);
+  if (scales != RESPEC_OK) return scales;
+  if (b.total_new > 0) {
+    const respec_status rows = check_new_rows(plan, x);
+    if (rows != RESPEC_OK) return rows;
   }
-  if (x.b.max_new_in_batch == 0 && !x.b.seq_status) return RESPEC_OK;  // (no sequence has tokens)
-  const respec_chunk_shape& s = plan->s;
-  ChunkAttnArgs a;
-  a.b = device_batch(plan, x.b);
-  a.q = static_cast<const char*>(x.q);
-  a.out = static_cast<char*>(x.out);
-  a.q_tok = x.q_token_stride * plan->es;
-  a.q_head = x.q_head_stride * plan->es;
-  a.o_tok = x.out_token_stride * plan->es;
-  a.o_head = x.out_head_stride * plan->es;
-  a.group = fast_div((uint32_t)a.b.group);
-  char* ws = static_cast<char*>(workspace);
-  const size_t o_bytes = align256(plan->part_rows * s.head_dim * 4), m_bytes = align256(plan->part_rows * 4);
-  a.part_o = reinterpret_cast<float*>(ws);
-  a.part_m = reinterpret_cast<float*>(ws + o_bytes);
-  a.part_l = reinterpret_cast<float*>(ws + o_bytes + m_bytes);
-  a.scale_log2 = (float)(1.4426950408889634 * (x.scale > 0.f ? (double)x.scale : 1.0 / sqrt((double)s.head_dim)));
-  if (isinf(a.scale_log2)) return RESPEC_ERR_PARAM;
-  const long long limit = (long long)a.b.max_kv + a.b.max_new;  // rows that the last token of the longest sequence sees
-  const long long all_rows = (long long)a.b.total_new * a.b.group, rows = (long long)a.b.max_new * a.b.group;  // per KV head
-  const long long seqs = std::min(a.b.batch, a.b.total_new);    // sequences that can have tokens
-  const long long held = x.b.total_new > 0 ? (long long)(plan->part_rows / ((size_t)x.b.total_new * s.n_q_heads)) : 1;
-  // row blocks of all sequences: each sequence's last one may be short
-  auto blocks = [&](int per_wg) { return std::min(ceil_div(all_rows, per_wg) + (seqs > 1 ? seqs - 1 : 0), seqs * ceil_div(rows, per_wg)); };
-  const int rb = (s.head_dim + 2) * 4;
-  hipStream_t stm = static_cast<hipStream_t>(stream);
-  const bool status = a.b.status != nullptr;
-  const long long reports = status ? a.b.batch : 0;  // workgroups that report a sequence's status
-  hipError_t e;
-  if (s.dtype == RESPEC_F32) {
-    a.few_rows = 0;
-    a.few = ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
-    a.wide = geometry(a.b, 64, blocks(64), limit, 32, 32, 2, s.head_dim == 128 ? Pace{0.16, 5} : Pace{0.1, 5}, rb, held);
-    if (!launchable(a.wide.items + reports, kAttnF32Threads)) return RESPEC_ERR_SHAPE;
-    e = launch_chunk_attn_f32(s.head_dim, a, status, stm);
-  } else {
-    // Calls of at most 64 query rows per KV head have the few-row kernel, of one or two groups of 32; others have
-    // 256-row blocks, and sequences of up to 32 rows among them the few-row kernel's way in the same launch.
-    const bool wide = rows > 64, mixed = wide && a.b.batch > 1;
-    a.few_rows = !wide ? (rows <= 32 ? 32 : 64) : mixed ? 32 : 0;
-    a.few = !wide || mixed ? geometry(a.b, a.few_rows, seqs, limit, 128, 128, 1,
-                                      s.head_dim == 128 ? Pace{0.02, 6} : Pace{0.01, 6}, rb, held)
-                           : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
-    a.wide = wide ? geometry(a.b, 256, blocks(256), limit, 128, 256, 1, s.head_dim == 128 ? Pace{0.032, 6} : Pace{0.018, 6}, rb, held)
-                  : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
-    if (!launchable((long long)a.few.items + a.wide.items + reports, wide ? kAttnWideThreads : kAttnFewThreads)) return RESPEC_ERR_SHAPE;
-    if (!raise_lds_limits(s.head_dim)) return RESPEC_ERR_HIP;
-    e = wide ? launch_chunk_attn_wide(s.head_dim, a, mixed, status, stm) : launch_chunk_attn_few(s.head_dim, a, status, stm);
-  }
-  if (e != hipSuccess) return RESPEC_ERR_HIP;
-  if (x.b.total_new > 0 && (a.few.nsplit > 1 || a.wide.nsplit > 1) &&
-      launch_chunk_merge(s.dtype, s.head_dim, a, stm) != hipSuccess)
-    return RESPEC_ERR_HIP;
-  return RESPEC_OK;
+  AppendQ8Args a;
+  a.b = device_batch(plan, b, 1);
+  a.q8 = device_scales(x.b.cache);
+  a.k_new = static_cast<const char*>(x.k_new);
+  a.v_new = static_cast<const char*>(x.v_new);
+  a.k_tok = x.k_token_stride * plan->es;
+  a.k_head = x.k_head_stride * plan->es;
+  a.v_tok = x.v_token_stride * plan->es;
+  a.v_head = x.v_head_stride * plan->es;
+  a.per_block = fast_div((uint32_t)(2 * plan->s.n_kv_heads));
+  // blocks that the new rows can touch: a sequence's n tokens at most (n + block - 2) / block + 1 and n
+  const long long block = x.b.cache.scale_block, total = b.total_new, seqs = std::min((long long)b.batch, total);
+  const long long each = std::min((long long)b.max_new_in_batch, (b.max_new_in_batch + block - 2) / block + 1);
+  const long long blocks = std::min({total, total / block + 2 * seqs, seqs * each});
+  const int waves = block == 128 ? 8 : kAppendQ8Waves, per_wg = waves / (int)(block / 16);
+  const long long wgs = ceil_div(blocks * 2 * plan->s.n_kv_heads, per_wg), reports = b.seq_status ? b.batch : 0;
+  if (wgs + reports == 0) return RESPEC_OK;
+  if (!launchable(wgs + reports, 64 * waves)) return RESPEC_ERR_SHAPE;
+  a.wgs = (int)wgs;
+  return launch_append_q8(plan->es, plan->s.head_dim, a, static_cast<hipStream_t>(stream)) == hipSuccess ? RESPEC_OK : RESPEC_ERR_HIP;
 }
 
 respec_status respec_score_create(const respec_score_shape* shape, respec_score_plan** out) {

@@ -1,9 +1,9 @@
 """ctypes binding of the prompt side of librespec_verify.so (include/respec_prompt.h).
 
 Argument marshalling only: a paged cache filled and attended to by chunks of new
-tokens (``ChunkPlan``), and the scores of given tokens (``ScorePlan``).  Tensors live
-on the plan's device; strides are taken from the tensors, the last dimension is
-contiguous.
+tokens (``ChunkPlan``; its 8-bit forms are of include/respec_cache.h), and the scores of given
+tokens (``ScorePlan``).  Tensors live on the plan's device; strides are taken from the tensors,
+the last dimension is contiguous.
 """
 from __future__ import annotations
 
@@ -19,6 +19,7 @@ EXPORTS = ("respec_chunk_create", "respec_chunk_destroy", "respec_chunk_workspac
            "respec_score")
 _P, _I32, _I64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
 _TORCH = {F32: torch.float32, BF16: torch.bfloat16}
+_E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 
 
 class ChunkShape(ctypes.Structure):
@@ -47,6 +48,26 @@ class AttnArgs(ctypes.Structure):
                 ("out_token_stride", _I64), ("out_head_stride", _I64), ("scale", ctypes.c_float)]
 
 
+class Q8Cache(ctypes.Structure):
+    _fields_ = [("k", _P), ("v", _P), ("k_scale", _P), ("v_scale", _P), ("n_pages", _I32), ("page_size", _I32),
+                ("scale_block", _I32), ("page_stride", _I64), ("head_stride", _I64), ("row_stride", _I64),
+                ("scale_page_stride", _I64), ("scale_head_stride", _I64), ("page_table", _P), ("table_width", _I32),
+                ("table_stride", _I64)]
+
+
+class Q8Batch(ctypes.Structure):
+    _fields_ = [("batch", _I32), ("total_new", _I32), ("max_new_in_batch", _I32), ("max_kv_len_in_batch", _I32),
+                ("new_off", _P), ("kv_len", _P), ("cache", Q8Cache), ("seq_status", _P)]
+
+
+class Q8AppendArgs(ctypes.Structure):
+    _fields_ = [("b", Q8Batch), *AppendArgs._fields_[1:]]
+
+
+class Q8AttnArgs(ctypes.Structure):
+    _fields_ = [("b", Q8Batch), *AttnArgs._fields_[1:]]
+
+
 class ScoreShape(ctypes.Structure):
     _fields_ = [(n, _I32) for n in ("vocab", "dtype", "max_rows", "topk_out")]
 
@@ -64,7 +85,8 @@ def lib() -> ctypes.CDLL:
     L = _verify_lib()
     if not _READY:
         for name, args in (("respec_chunk_create", [_P, _P]), ("respec_chunk_append", [_P, _P, _P]),
-                           ("respec_chunk_attn", [_P, _P, _P, _P]), ("respec_score_create", [_P, _P]),
+                           ("respec_chunk_attn", [_P, _P, _P, _P]), ("respec_chunk_append_q8", [_P, _P, _P]),
+                           ("respec_chunk_attn_q8", [_P, _P, _P, _P]), ("respec_score_create", [_P, _P]),
                            ("respec_score", [_P, _P, _P, _P])):
             f = getattr(L, name)
             f.argtypes, f.restype = args, ctypes.c_int
@@ -79,14 +101,14 @@ def lib() -> ctypes.CDLL:
 
 
 class _Plan:
-    """A plan handle, its device and its workspace."""
+    """A plan handle, its device and its workspace (of kinds that have one)."""
 
-    def __init__(self, kind: str, shape, device, workspace):
+    def __init__(self, kind: str, shape, device, workspace, *more):
         self._h = None
-        L = lib()
+        L = self._lib()
         self._destroy = getattr(L, f"respec_{kind}_destroy")
         h = ctypes.c_void_p()
-        status = getattr(L, f"respec_{kind}_create")(ctypes.byref(shape), ctypes.byref(h))
+        status = getattr(L, f"respec_{kind}_create")(ctypes.byref(shape), *more, ctypes.byref(h))
         if status != OK:
             raise VerifyError(status, f"respec_{kind}_create")
         self._h, self.shape = h, shape
@@ -95,8 +117,11 @@ class _Plan:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.dtype = _TORCH[shape.dtype]
         self._index = self.device.index if self.device.type == "cuda" else -1
-        self.workspace_bytes = int(getattr(L, f"respec_{kind}_workspace_bytes")(h))
         self._streams = None   # streams that torch's allocator knows the plan's own workspace to be used on
+        size = getattr(L, f"respec_{kind}_workspace_bytes", None)
+        if size is None:
+            return
+        self.workspace_bytes = int(size(h))
         if workspace is None:
             if self._index >= 0:
                 self._streams = {torch._C._cuda_getCurrentRawStream(self._index)}
@@ -107,6 +132,10 @@ class _Plan:
                 raise ValueError(f"the workspace holds {self.workspace_bytes} bytes on {self.device}")
             self.workspace_ptr = workspace.data_ptr()
         self._ws_buf = workspace
+
+    @staticmethod
+    def _lib() -> ctypes.CDLL:
+        return lib()
 
     def close(self):
         if self._h:
@@ -166,6 +195,14 @@ class _Plan:
             raise VerifyError(status, name)
 
 
+def _scale(scale) -> float:
+    """The scores' scale as float32; 0: the default."""
+    scale_f = 0.0 if scale is None else ctypes.c_float(scale).value
+    if scale is not None and not scale_f > 0:
+        raise ValueError("scale: a positive number expected, in float32, too")
+    return scale_f
+
+
 class ChunkPlan(_Plan):
     """A respec_chunk plan plus its device workspace.
 
@@ -214,13 +251,61 @@ class ChunkPlan(_Plan):
         dims = (q.shape[0], s.n_q_heads, s.head_dim)
         qp, q_st = self._rows(q, "q", self.dtype, dims)
         op, o_st = self._rows(out, "out", self.dtype, dims)
-        scale_f = 0.0 if scale is None else ctypes.c_float(scale).value
-        if scale is not None and not scale_f > 0:
-            raise ValueError("scale: a positive number expected, in float32, too")
+        scale_f = _scale(scale)
         b = self._batch(k_pages, v_pages, page_table, new_off, kv_len, dims[0], max_new_in_batch, max_kv_len_in_batch,
                         status)
         a = AttnArgs(b, qp, q_st[0], q_st[1], op, o_st[0], o_st[1], scale_f)
         self._call(lib().respec_chunk_attn, "respec_chunk_attn", (ctypes.byref(a), self.workspace_ptr), stream)
+
+
+    def _batch_q8(self, k_pages, v_pages, k_scale, v_scale, page_table, new_off, kv_len, total_new, max_new, max_kv_len, status):
+        s, i32 = self.shape, torch.int32
+        n_pages, _, page, _ = k_pages.shape
+        batch, width = page_table.shape
+        dims = (n_pages, s.n_kv_heads, page, s.head_dim)
+        k, st = self._rows(k_pages, "k_pages", _E4M3, dims)
+        v, v_st = self._rows(v_pages, "v_pages", _E4M3, dims)
+        blocks = k_scale.shape[-1] if k_scale.dim() == 3 else 0
+        if blocks < 1 or page % blocks:
+            raise ValueError(f"k_scale: [pages][heads][blocks of a page] expected, {page} rows a page in whole blocks; got "
+                             f"{tuple(k_scale.shape)}")
+        ks, s_st = self._rows(k_scale, "k_scale", _E8M0, dims[:2] + (blocks,))
+        vs, vs_st = self._rows(v_scale, "v_scale", _E8M0, dims[:2] + (blocks,))
+        if st != v_st or s_st != vs_st:
+            raise ValueError("k_pages and v_pages, or their scales, are laid out differently")
+        table, t_st = self._rows(page_table, "page_table", i32, (batch, width))
+        return Q8Batch(batch, total_new, max_new, max_kv_len, self._flat(new_off, "new_off", i32, (batch + 1,)),
+                       self._flat(kv_len, "kv_len", i32, (batch,)),
+                       Q8Cache(k, v, ks, vs, n_pages, page, page // blocks, st[0], st[1], st[2], s_st[0], s_st[1], table, width,
+                               t_st[0]),
+                       None if status is None else self._flat(status, "status", i32, (batch,)))
+
+    def append_q8(self, k_new, v_new, k_pages, v_pages, k_scale, v_scale, page_table, new_off, kv_len, *, max_new_in_batch,
+                  status=None, max_kv_len_in_batch=None, stream=None) -> None:
+        """Enqueue respec_chunk_append_q8: rows ``k_new``, ``v_new`` [T][Hkv][D] of the new tokens into the e4m3 values
+        ``k_pages``, ``v_pages`` [pages][Hkv][page][D] with their blocks' scales ``k_scale``, ``v_scale``
+        [pages][Hkv][blocks of a page] (float8_e8m0fnu)."""
+        s = self.shape
+        dims = (k_new.shape[0], s.n_kv_heads, s.head_dim)
+        k, k_st = self._rows(k_new, "k_new", self.dtype, dims)
+        v, v_st = self._rows(v_new, "v_new", self.dtype, dims)
+        b = self._batch_q8(k_pages, v_pages, k_scale, v_scale, page_table, new_off, kv_len, dims[0], max_new_in_batch,
+                           s.max_kv_len if max_kv_len_in_batch is None else max_kv_len_in_batch, status)
+        a = Q8AppendArgs(b, k, v, k_st[0], k_st[1], v_st[0], v_st[1])
+        self._call(lib().respec_chunk_append_q8, "respec_chunk_append_q8", (ctypes.byref(a),), stream)
+
+    def attend_q8(self, q, k_pages, v_pages, k_scale, v_scale, page_table, new_off, kv_len, out, *, max_new_in_batch,
+                  max_kv_len_in_batch, scale=None, status=None, stream=None) -> None:
+        """Enqueue respec_chunk_attn_q8: ``attend`` over the 8-bit cache that ``append_q8`` fills."""
+        s = self.shape
+        dims = (q.shape[0], s.n_q_heads, s.head_dim)
+        qp, q_st = self._rows(q, "q", self.dtype, dims)
+        op, o_st = self._rows(out, "out", self.dtype, dims)
+        scale_f = _scale(scale)
+        b = self._batch_q8(k_pages, v_pages, k_scale, v_scale, page_table, new_off, kv_len, dims[0], max_new_in_batch,
+                           max_kv_len_in_batch, status)
+        a = Q8AttnArgs(b, qp, q_st[0], q_st[1], op, o_st[0], o_st[1], scale_f)
+        self._call(lib().respec_chunk_attn_q8, "respec_chunk_attn_q8", (ctypes.byref(a), self.workspace_ptr), stream)
 
 
 # outputs of a scoring call: type, and whether they hold the top alternatives' columns

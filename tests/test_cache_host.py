@@ -1,0 +1,330 @@
+"""The C ABI of include/respec_cache.h on the host: exports, structs, plans, refusals, and the 64-bit definitions.
+
+No call here reaches the GPU (see test_prompt_host.py).
+"""
+import ctypes
+import math
+import os
+import re
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import cache_cases as cc  # noqa: E402
+from test_prompt_host import BATCH_REFUSALS, CAPACITY, DTYPE, FAKE, NULL, OK, PARAM, ROOT, SHAPE, WORKSPACE, _chunk_shape, _create, p  # noqa: E402,F401
+
+
+@pytest.fixture(scope="module")
+def lib(p):  # noqa: F811
+    from paper_2511_01282_amd import cache
+    cache.lib()
+    return cache
+
+
+def test_library_exports_every_declared_function(lib):
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "respec_cache.h")).read(), flags=re.S)
+    assert set(re.findall(r"\b(respec_[a-z0-9_]+)\s*\(", text)) == set(lib.EXPORTS)
+    for name in lib.EXPORTS:
+        assert hasattr(lib.lib(), name), name
+
+
+def test_structs_match_the_header(lib, p, tmp_path):  # noqa: F811
+    import shutil
+    import subprocess
+    cc_ = shutil.which("gcc")
+    if not cc_:
+        pytest.skip("no C compiler")
+    names = {"respec_rotary_shape": lib.RotaryShape, "respec_rotary_args": lib.RotaryArgs, "respec_q8_cache": p.Q8Cache,
+             "respec_q8_batch": p.Q8Batch, "respec_q8_append_args": p.Q8AppendArgs, "respec_q8_attn_args": p.Q8AttnArgs,
+             "respec_cache_keep_args": lib.KeepArgs, "respec_page_plane": lib.PagePlane, "respec_cache_copy_args": lib.CopyArgs}
+    lines, want = [], []
+    for c, s in names.items():
+        lines.append(f'printf("%zu\\n", sizeof({c}));')
+        lines += [f'printf("%zu\\n", offsetof({c}, {f[0]}));' for f in s._fields_]
+        want.append(ctypes.sizeof(s))
+        want += [getattr(s, f[0]).offset for f in s._fields_]
+    src = tmp_path / "s.c"
+    src.write_text('#include <stdio.h>\n#include "respec_cache.h"\nint main(void) {\n%s\nreturn 0;}\n' % "\n".join(lines))
+    exe = str(tmp_path / "s")
+    subprocess.check_call([cc_, "-I", os.path.join(ROOT, "include"), str(src), "-o", exe])
+    assert [int(x) for x in subprocess.check_output([exe]).split()] == want
+
+
+# ---------------------------------------------------------------------------
+# rotary positions
+# ---------------------------------------------------------------------------
+
+def _rotary(lib, w=None, **over):
+    d = dict(n_q_heads=8, n_kv_heads=2, head_dim=64, rotary_dim=64, layout=0, dtype=1, max_tokens=100, amplitude=0.0)
+    d.update(over)
+    w = (ctypes.c_double * 64)(*([0.5] * 64 if w is None else w))
+    h = ctypes.c_void_p()
+    return lib.lib().respec_rotary_create(ctypes.byref(lib.RotaryShape(**d)), w, ctypes.byref(h)), h
+
+
+@pytest.mark.parametrize("over,status", [
+    ({}, OK), ({"dtype": 2}, DTYPE), ({"head_dim": 96}, SHAPE), ({"rotary_dim": 0}, SHAPE), ({"rotary_dim": 24}, SHAPE),
+    ({"rotary_dim": 80}, SHAPE), ({"rotary_dim": 16}, OK), ({"head_dim": 128, "rotary_dim": 112}, OK), ({"n_q_heads": 0}, SHAPE),
+    ({"n_kv_heads": 257}, SHAPE), ({"n_q_heads": 7}, OK), ({"layout": 2}, PARAM), ({"layout": 1}, OK), ({"max_tokens": 0}, SHAPE),
+    ({"max_tokens": (1 << 24) + 1}, SHAPE), ({"amplitude": -1.0}, PARAM), ({"amplitude": math.inf}, PARAM),
+    ({"amplitude": math.nan}, PARAM), ({"w": [-1.0]}, PARAM), ({"w": [math.nan]}, PARAM), ({"w": [math.inf]}, PARAM),
+    ({"w": [0.0]}, OK), ({"w": [1e9]}, OK),
+])
+def test_rotary_create(lib, over, status):
+    st, h = _rotary(lib, **over)
+    assert st == status and bool(h.value) == (status == OK)
+    lib.lib().respec_rotary_destroy(h)
+
+
+def test_rotary_create_without_arguments(lib):
+    L, h, s, w = lib.lib(), ctypes.c_void_p(), lib.RotaryShape(8, 2, 64, 64, 0, 1, 9, 1.0), (ctypes.c_double * 32)()
+    assert L.respec_rotary_create(None, w, ctypes.byref(h)) == NULL
+    assert L.respec_rotary_create(ctypes.byref(s), None, ctypes.byref(h)) == NULL
+    assert L.respec_rotary_create(ctypes.byref(s), w, None) == NULL
+    L.respec_rotary_destroy(None)
+
+
+@pytest.mark.parametrize("over,status", [
+    ({"tokens": -1}, SHAPE), ({"tokens": 101}, CAPACITY), ({"tokens": 0}, OK), ({"q": None, "q_out": None, "k": None, "k_out": None}, OK),
+    ({"q": None}, NULL), ({"q_out": None}, NULL), ({"k": None}, NULL), ({"k_out": None}, NULL), ({"q": FAKE + 8}, SHAPE),
+    ({"k_out": FAKE + 4}, SHAPE), ({"q_token_stride": 4}, SHAPE), ({"q_head_stride": -64}, SHAPE), ({"q_out_head_stride": 68}, SHAPE),
+    ({"k_token_stride": 1}, SHAPE), ({"k_out_token_stride": -8}, SHAPE), ({"positions": FAKE, "seq_status": FAKE}, PARAM),
+    ({"batch": -1}, SHAPE), ({"batch": 65536}, SHAPE), ({"new_off": None}, NULL), ({"kv_len": None}, NULL),
+    ({"batch": 0, "new_off": None, "kv_len": None}, OK),
+])
+def test_rotary_refusals(lib, over, status):
+    st, h = _rotary(lib)
+    assert st == OK
+    d = dict(tokens=5, positions=None, batch=2, new_off=FAKE, kv_len=FAKE)
+    for x, n in (("q", 8), ("q_out", 8), ("k", 2), ("k_out", 2)):
+        d.update({x: FAKE, x + "_token_stride": n * 64, x + "_head_stride": 64})
+    d.update(over)
+    a = lib.RotaryArgs(**d)
+    assert lib.lib().respec_rotary(h, ctypes.byref(a), None) == status
+    assert lib.lib().respec_rotary(None, ctypes.byref(a), None) == NULL
+    assert lib.lib().respec_rotary(h, None, None) == NULL
+    lib.lib().respec_rotary_destroy(h)
+
+
+def test_frequencies(lib):
+    w = lib.frequencies(64, 500000.0)
+    assert w[0] == 1.0 and w[1] == 500000.0 ** (-1 / 32) and len(w) == 32
+    assert lib.frequencies(64, 500000.0, scaling="linear", factor=4) == [x / 4 for x in w]
+    kw = dict(factor=8.0, original_len=8192)
+    b = lib.frequencies(64, 500000.0, scaling="bands", **kw)
+    for x, y in zip(w, b):
+        turns = 8192 * x / (2 * math.pi)
+        assert y == pytest.approx(x if turns >= 4 else x / 8 if turns <= 1 else x * (turns - 1) / 3 + x / 8 * (4 - turns) / 3, rel=1e-12)
+    r = lib.frequencies(64, 10000.0, scaling="ramp", factor=4.0, original_len=4096)
+    w = lib.frequencies(64)
+    ratio = [y / x for x, y in zip(w, r)]
+    assert ratio[0] == 1.0 and ratio[-1] == 0.25 and all(a >= b for a, b in zip(ratio, ratio[1:]))
+    # the first pair that turns under 32 times in 4096 positions is not kept whole, the last one that turns once not divided whole
+    assert ratio[sum(4096 * x / (2 * math.pi) >= 32 for x in w) + 1] < 1.0 and ratio[sum(4096 * x / (2 * math.pi) >= 1 for x in w) - 1] > 0.25
+    assert lib.ramp_amplitude(4.0) == 0.1 * math.log(4) + 1
+    for bad in (dict(scaling="other"), dict(scaling="linear", factor=0.5), dict(scaling="bands", factor=2.0),
+                dict(scaling="bands", low=4.0, high=4.0, **kw), dict(scaling="ramp", fast=1.0, slow=1.0, **kw)):
+        with pytest.raises(ValueError):
+            lib.frequencies(64, **bad)
+
+
+def test_rotary_binding_refusals(lib):
+    bf, i32 = torch.bfloat16, torch.int32
+    new = dict(n_q_heads=4, n_kv_heads=2, head_dim=64, dtype=1, device="cpu")
+    for bad in (dict(frequencies=[1.0] * 31), dict(amplitude=0.0), dict(amplitude=math.nan), dict(rotary_dim=16, frequencies=[1.0] * 32)):
+        with pytest.raises(ValueError):
+            lib.RotaryPlan(**new, **bad)
+    plan = lib.RotaryPlan(**new)
+    good = dict(q=torch.zeros(3, 4, 64, dtype=bf), k=torch.zeros(3, 2, 64, dtype=bf), positions=torch.zeros(3, dtype=i32))
+    good.update(q_out=good["q"], k_out=good["k"])
+    two = dict(new_off=torch.zeros(2, dtype=i32), kv_len=torch.zeros(1, dtype=i32))
+    for bad in (dict(q=None), dict(q=None, q_out=None, k=None, k_out=None), dict(k=torch.zeros(2, 2, 64, dtype=bf)),
+                dict(k=torch.zeros(2, 2, 64, dtype=bf), k_out=torch.zeros(2, 2, 64, dtype=bf)),
+                dict(q=torch.zeros(3, 4, 64)), dict(q=torch.zeros(3, 4, 32, dtype=bf)), dict(positions=None),
+                dict(positions=torch.zeros(3, dtype=torch.int64)), dict(positions=torch.zeros(4, dtype=i32)), two,
+                dict(status=torch.zeros(1, dtype=i32)), dict(positions=None, new_off=two["new_off"]),
+                dict(positions=None, new_off=torch.zeros(3, dtype=i32), kv_len=two["kv_len"]),
+                dict(q_out=good["q"].view(3, 2, 2, 64).transpose(1, 2).reshape(3, 4, 64)[:, :, ::1].view(3, 4, 64).transpose(0, 1)),
+                dict(k_out=good["k"].to("meta"))):
+        with pytest.raises(ValueError):
+            plan.rotate(**dict(good, **bad))
+    plan.close()
+    with pytest.raises(ValueError):
+        plan.rotate(**good)
+
+
+# ---------------------------------------------------------------------------
+# the 8-bit cache
+# ---------------------------------------------------------------------------
+
+def _batch(p, **over):  # noqa: F811
+    cache = dict(k=FAKE, v=FAKE, k_scale=FAKE, v_scale=FAKE, n_pages=9, page_size=32, scale_block=16, page_stride=2 * 32 * 64,
+                 head_stride=32 * 64, row_stride=64, scale_page_stride=4, scale_head_stride=2, page_table=FAKE, table_width=5,
+                 table_stride=5)
+    d = dict(batch=2, total_new=10, max_new_in_batch=8, max_kv_len_in_batch=40, new_off=FAKE, kv_len=FAKE, seq_status=None)
+    cache.update({k: v for k, v in over.items() if k in cache})
+    d.update({k: v for k, v in over.items() if k in d})
+    return p.Q8Batch(cache=p.Q8Cache(**cache), **d)
+
+
+@pytest.mark.parametrize("over,status", BATCH_REFUSALS + [
+    ({"batch": 0, "k": None, "k_scale": None}, OK), ({"total_new": 0, "max_new_in_batch": 0}, OK), ({"k_scale": None}, NULL),
+    ({"v_scale": None}, NULL), ({"scale_block": 0}, SHAPE), ({"scale_block": 8}, SHAPE), ({"scale_block": 24}, SHAPE),
+    ({"scale_block": 256}, SHAPE), ({"scale_block": 64}, SHAPE), ({"page_size": 24}, SHAPE), ({"page_size": 48, "scale_block": 32}, SHAPE),
+    ({"scale_page_stride": -1}, SHAPE), ({"scale_head_stride": -2}, SHAPE), ({"row_stride": 72}, SHAPE), ({"head_stride": 8}, SHAPE),
+])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_q8_batch_refusals(p, over, status, dtype):  # noqa: F811
+    st, h = _create(p, "chunk", _chunk_shape(p, dtype=dtype))
+    assert st == OK
+    ap = p.Q8AppendArgs(_batch(p, **over), FAKE, FAKE, 128, 64, 128, 64)
+    at = p.Q8AttnArgs(_batch(p, **over), FAKE, 512, 64, FAKE, 512, 64, 0.0)
+    assert p.lib().respec_chunk_append_q8(h, ctypes.byref(ap), None) == status
+    assert p.lib().respec_chunk_attn_q8(h, ctypes.byref(at), FAKE, None) == status
+    p.lib().respec_chunk_destroy(h)
+
+
+@pytest.mark.parametrize("over,status", [
+    ({"k_new": None}, NULL), ({"v_new": None}, NULL), ({"k_new": FAKE + 4}, SHAPE), ({"v_new": FAKE + 4}, SHAPE),
+    ({"k_token_stride": 130}, SHAPE), ({"k_head_stride": -8}, SHAPE), ({"v_token_stride": 4}, SHAPE), ({"v_head_stride": 1}, SHAPE)])
+def test_q8_append_refusals(p, over, status):  # noqa: F811
+    _, h = _create(p, "chunk", _chunk_shape(p))
+    d = dict(k_new=FAKE, v_new=FAKE, k_token_stride=128, k_head_stride=64, v_token_stride=128, v_head_stride=64)
+    a = p.Q8AppendArgs(b=_batch(p), **dict(d, **over))
+    assert p.lib().respec_chunk_append_q8(h, ctypes.byref(a), None) == status
+    assert p.lib().respec_chunk_append_q8(None, ctypes.byref(a), None) == NULL
+    assert p.lib().respec_chunk_append_q8(h, None, None) == NULL
+    p.lib().respec_chunk_destroy(h)
+
+
+@pytest.mark.parametrize("over,status", [
+    ({"q": None}, NULL), ({"out": None}, NULL), ({"q": FAKE + 8}, SHAPE), ({"out": FAKE + 8}, SHAPE), ({"q_token_stride": 4}, SHAPE),
+    ({"q_head_stride": -8}, SHAPE), ({"out_token_stride": 2}, SHAPE), ({"scale": -1.0}, PARAM), ({"scale": math.nan}, PARAM),
+    ({"scale": math.inf}, PARAM)])
+def test_q8_attn_refusals(p, over, status):  # noqa: F811
+    _, h = _create(p, "chunk", _chunk_shape(p))
+    d = dict(q=FAKE, q_token_stride=512, q_head_stride=64, out=FAKE, out_token_stride=512, out_head_stride=64, scale=0.0)
+    a = p.Q8AttnArgs(b=_batch(p), **dict(d, **over))
+    f = p.lib().respec_chunk_attn_q8
+    assert f(h, ctypes.byref(a), FAKE, None) == status
+    assert f(h, ctypes.byref(a), None, None) == WORKSPACE and f(h, ctypes.byref(a), FAKE + 16, None) == WORKSPACE
+    assert f(None, ctypes.byref(a), FAKE, None) == NULL and f(h, None, FAKE, None) == NULL
+    p.lib().respec_chunk_destroy(h)
+
+
+def test_q8_launches_of_too_many_threads(p):  # noqa: F811
+    _, h = _create(p, "chunk", _chunk_shape(p, n_q_heads=256, n_kv_heads=256, max_batch=65535, max_new=65535))
+    b = _batch(p, batch=65535, total_new=65535, max_new_in_batch=1, max_kv_len_in_batch=0, seq_status=FAKE)
+    assert p.lib().respec_chunk_append_q8(h, ctypes.byref(p.Q8AppendArgs(_batch(
+        p, batch=65535, total_new=65535, max_new_in_batch=1, max_kv_len_in_batch=0, scale_block=128, page_size=128), FAKE, FAKE, 0, 0, 0, 0)), None) == SHAPE
+    assert p.lib().respec_chunk_attn_q8(h, ctypes.byref(p.Q8AttnArgs(b, FAKE, 0, 0, FAKE, 0, 0, 0.0)), FAKE, None) == SHAPE
+    p.lib().respec_chunk_destroy(h)
+
+
+def test_q8_binding_refusals(p):  # noqa: F811
+    plan = p.ChunkPlan(n_q_heads=4, n_kv_heads=2, head_dim=64, dtype=1, max_batch=2, max_new=8, max_kv_len=64, device="cpu")
+    bf, i32 = torch.bfloat16, torch.int32
+    pages = torch.zeros(5, 2, 32, 64, dtype=torch.uint8).view(cc.E4M3)
+    scale = torch.zeros(5, 2, 2, dtype=torch.uint8).view(cc.E8M0)
+    cache = dict(k_pages=pages, v_pages=pages, k_scale=scale, v_scale=scale, page_table=torch.zeros(1, 4, dtype=i32),
+                 new_off=torch.zeros(2, dtype=i32), kv_len=torch.zeros(1, dtype=i32))
+    rows, q = torch.zeros(3, 2, 64, dtype=bf), torch.zeros(3, 4, 64, dtype=bf)
+    bad = [dict(k_pages=pages.view(torch.uint8)), dict(v_pages=pages.view(torch.uint8).to(bf)), dict(k_scale=scale.view(torch.uint8)),
+           dict(k_scale=torch.zeros(5, 2, 3, dtype=torch.uint8).view(cc.E8M0)), dict(k_scale=scale[:, :, 0]), dict(v_scale=scale[:4]),
+           dict(v_scale=torch.zeros(5, 2, 1, dtype=torch.uint8).view(cc.E8M0)), dict(k_scale=scale[:, :1]),
+           dict(v_pages=pages.view(torch.uint8).view(5, 32, 2, 64).transpose(1, 2).view(cc.E4M3)),
+           dict(v_scale=torch.zeros(5, 2, 4, dtype=torch.uint8)[:, :, :2].view(cc.E8M0)), dict(kv_len=torch.zeros(2, dtype=i32)),
+           dict(page_table=torch.zeros(1, 4, dtype=torch.int64)), dict(status=torch.zeros(2, dtype=i32))]
+    for b in bad:
+        with pytest.raises(ValueError):
+            plan.append_q8(rows, rows, **dict(cache, **b), max_new_in_batch=3)
+        with pytest.raises(ValueError):
+            plan.attend_q8(q, out=q, **dict(cache, **b), max_new_in_batch=3, max_kv_len_in_batch=9)
+    for scale_ in (0.0, -1.0, 1e-50, math.nan):
+        with pytest.raises(ValueError):
+            plan.attend_q8(q, out=q, **cache, max_new_in_batch=3, max_kv_len_in_batch=9, scale=scale_)
+    with pytest.raises(ValueError):
+        plan.append_q8(q, rows, **cache, max_new_in_batch=3)
+
+
+def test_definition_of_the_scale():
+    """power() is the least exponent, and a block's largest value keeps its precision."""
+    for top, k in ((448.0, 0), (448.0001, 1), (449.0, 1), (224.0, -1), (1.0, -8), (1.75, -8), (1.76, -7), (0.0, -126), (1e-45, -126),
+                   (3.3e38, 120), (2.0 ** 127 * 1.75, 119)):
+        assert cc.power(top) == k, top
+    x = torch.tensor([448.0, 17.0, 19.0, 2.0 ** -9, 2.0 ** -10, 3 * 2.0 ** -10, -0.3, math.nan, math.inf], dtype=cc.F64)
+    got = cc.codes(x, 0).view(cc.E4M3).to(cc.F64)
+    assert got[:7].tolist() == [448.0, 16.0, 20.0, 2.0 ** -9, 0.0, 2.0 ** -8, -0.3125] and bool(got[7:].isnan().all())
+
+
+# ---------------------------------------------------------------------------
+# rows kept, pages copied
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("over,status", [
+    ({"dtype": 2}, DTYPE), ({"batch": -1}, SHAPE), ({"batch": 65536}, SHAPE), ({"batch": 0, "kv_len": None}, OK), ({"n_layers": 0}, SHAPE),
+    ({"n_layers": 65536}, SHAPE), ({"n_kv_heads": 0}, SHAPE), ({"n_kv_heads": 257}, SHAPE), ({"head_dim": 80}, SHAPE),
+    ({"path_width": 0}, SHAPE), ({"path_width": 66}, SHAPE), ({"path_stride": 5}, SHAPE), ({"layer_stride": -8}, SHAPE),
+    ({"layer_stride": 4}, SHAPE), ({"kv_len": None}, NULL), ({"path": None}, NULL), ({"acc_len": None}, NULL),
+    ({"kv_len_out": FAKE}, SHAPE), ({"kv_len_out": FAKE + 4}, SHAPE), ({"k": None}, NULL), ({"v": None}, NULL), ({"page_table": None}, NULL),
+    ({"n_pages": 0}, SHAPE), ({"page_size": 0}, SHAPE), ({"table_width": 0}, SHAPE), ({"table_stride": 4}, SHAPE),
+    ({"page_stride": 4}, SHAPE), ({"head_stride": -8}, SHAPE), ({"row_stride": 12}, SHAPE), ({"row_stride": (1 << 24) + 8}, SHAPE),
+    ({"k": FAKE + 8}, SHAPE), ({"v": FAKE + 2}, SHAPE),
+    ({"batch": 65535, "n_layers": 65535, "table_stride": 5, "path_stride": 6}, SHAPE),
+])
+def test_keep_refusals(lib, p, over, status):  # noqa: F811
+    cache = dict(k=FAKE, v=FAKE, n_pages=9, page_size=16, page_stride=2 * 16 * 64, head_stride=16 * 64, row_stride=64,
+                 page_table=FAKE, table_width=5, table_stride=5)
+    d = dict(batch=2, n_layers=3, n_kv_heads=2, head_dim=64, dtype=1, layer_stride=9 * 2048, kv_len=FAKE, path=FAKE + 64, path_width=6,
+             path_stride=6, acc_len=FAKE + 4096, kv_len_out=FAKE + 8192, seq_status=None)
+    cache.update({k: v for k, v in over.items() if k in cache})
+    d.update({k: v for k, v in over.items() if k in d})
+    a = lib.KeepArgs(cache=p.PagedCache(**cache), **d)
+    assert lib.lib().respec_cache_keep(ctypes.byref(a), None) == status
+    assert lib.lib().respec_cache_keep(None, None) == NULL
+
+
+@pytest.mark.parametrize("over,plane,status", [
+    ({"pairs": -1}, {}, SHAPE), ({"pairs": 65536}, {}, SHAPE), ({"pairs": 0, "src": None}, {}, OK), ({"src": None}, {}, NULL),
+    ({"dst": None}, {}, NULL), ({"n_pages": 0}, {}, SHAPE), ({"n_planes": 0}, {}, SHAPE), ({"n_planes": 9}, {}, SHAPE),
+    ({"planes": None}, {}, NULL), ({}, {"base": None}, NULL), ({}, {"n_layers": 0}, SHAPE), ({}, {"n_layers": 65536}, SHAPE),
+    ({}, {"heads": 0}, SHAPE), ({}, {"rows": 0}, SHAPE), ({}, {"row_bytes": 0}, SHAPE), ({}, {"row_bytes": 1 << 31}, SHAPE),
+    ({}, {"heads": 1 << 15, "rows": 1 << 16, "row_bytes": 1}, SHAPE), ({}, {"heads": 1 << 14, "rows": 1 << 14, "row_bytes": 8}, SHAPE),
+    ({}, {"page_stride": -1}, SHAPE), ({}, {"layer_stride": -1}, SHAPE), ({}, {"head_stride": -1}, SHAPE), ({}, {"row_stride": -1}, SHAPE),
+    ({}, {"n_layers": 65535, "rows": 1 << 20}, SHAPE), ({"pairs": 65535}, {"n_layers": 300}, SHAPE),
+])
+def test_copy_refusals(lib, over, plane, status):
+    d = dict(base=FAKE, page_stride=4096, n_layers=2, layer_stride=1 << 20, heads=2, head_stride=2048, rows=16, row_stride=128, row_bytes=128)
+    planes = (lib.PagePlane * 1)(lib.PagePlane(**dict(d, **plane)))
+    a = dict(pairs=3, src=FAKE, dst=FAKE, n_pages=9, n_planes=1, planes=ctypes.addressof(planes), status=None)
+    a = lib.CopyArgs(**dict(a, **over))
+    assert lib.lib().respec_cache_copy(ctypes.byref(a), None) == status
+    assert lib.lib().respec_cache_copy(None, None) == NULL
+
+
+def test_layers_binding_refusals(lib):
+    bf, i32, u8 = torch.bfloat16, torch.int32, torch.uint8
+    k = torch.zeros(3, 5, 2, 16, 64, dtype=bf)
+    codes, scale = torch.zeros(3, 5, 2, 16, 64, dtype=u8).view(cc.E4M3), torch.zeros(3, 5, 2, 1, dtype=u8).view(cc.E8M0)
+    for bad in ((k, k[:, :4]), (k, k.float()), (k.half(), k.half()), (k, k, scale), (codes, codes), (k, k, scale, scale), (k[0, 0], k[0, 0]),
+                (codes, codes, scale, scale[:, :, :1]), (codes, codes, scale.view(u8), scale.view(u8)), (k, k[0]), (k[:0], k[:0]),
+                (k.transpose(3, 4), k.transpose(3, 4)), (codes, codes, scale[0], scale[0]), (k, k.to("meta")),
+                (codes, codes, scale, torch.zeros(3, 5, 2, 2, dtype=u8).view(cc.E8M0))):
+        with pytest.raises(ValueError):
+            lib.CacheLayers(*bad)
+    layers = lib.CacheLayers(k, k)
+    good = dict(page_table=torch.zeros(2, 3, dtype=i32), kv_len=torch.zeros(2, dtype=i32), path=torch.zeros(2, 6, dtype=i32),
+                acc_len=torch.zeros(2, dtype=i32), kv_len_out=torch.zeros(2, dtype=i32))
+    for bad in (dict(kv_len=torch.zeros(3, dtype=i32)), dict(path=torch.zeros(3, 6, dtype=i32)), dict(path=torch.zeros(12, dtype=i32)),
+                dict(acc_len=torch.zeros(2, dtype=torch.int64)), dict(page_table=torch.zeros(3, 3, dtype=i32)),
+                dict(path=torch.zeros(6, 2, dtype=i32).t()), dict(status=torch.zeros(1, dtype=i32))):
+        with pytest.raises(ValueError):
+            layers.keep_rows(**dict(good, **bad))
+    with pytest.raises(ValueError):   # K and V laid out differently; 8-bit values
+        lib.CacheLayers(k, torch.zeros(3, 5, 16, 2, 64, dtype=bf).transpose(2, 3)).keep_rows(**good)
+    with pytest.raises(ValueError):
+        lib.CacheLayers(codes, codes, scale, scale).keep_rows(**good)
+    for bad in ((torch.zeros(2, dtype=i32), torch.zeros(3, dtype=i32)), (torch.zeros(2), torch.zeros(2, dtype=i32))):
+        with pytest.raises(ValueError):
+            layers.copy_pages(*bad)

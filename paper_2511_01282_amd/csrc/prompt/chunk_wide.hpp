@@ -42,8 +42,9 @@ struct WideShape {
 };
 
 // Q8: the cache holds e4m3 values with a scale per block.  A wave brings its rows of a pass, 16 that share a page and a
-// scale, through registers: they are requested as a pass begins, and become bf16, which holds them exactly, on the way
-// into LDS at its end.  So each value is converted once for all 256 rows, and what follows is the same.
+// scale, through registers, and they become bf16, which holds them exactly, on the way into LDS.  So each value is converted
+// once for all 256 rows, and what follows is the same.  K is on its way during the first half of a pass and V during the
+// second, for want of registers (both during all of it spilled 76 and took 561 us for 512 tokens over 16384 rows, 32 heads on 8).
 template <int D, bool Q8>
 __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, unsigned char* smem) {
   using G = WideShape<D, Q8>;
@@ -92,26 +93,41 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
   // units that this wave requests something of end here (it asks for rows of the last tile, no further ones)
   const int n_units = ((hi_row - lo + kWideTile - 1) / kWideTile - 1 - w_tile + kPass - 1) / kPass;
   int unit = -1;
-  // (Q8: a wave's window of 64 units, a lane for each, and the unit that is on its way)
+  // (Q8: a wave's window of 64 units, a lane for each; the unit that is on its way)
   static_assert(!Q8 || kRows == 16, "16 rows share a page and a scale");
   Q8Window window;
   Q8Rows<D> q8;
-  int coming = -1;  // its tile; none: -1
-  auto commit = [&]() __attribute__((always_inline)) {
-    if (coming < 0) return;
-    unsigned char* to = smem + (coming % S) * G::kSlot;
-    q8.to_lds(to, to + G::kHalf, w_row, lane);
+  int coming = -1, entry = 0;  // its first tile (none: -1), its lane of the window
+  int64_t q8_off = 0;
+  auto here = [&]() __attribute__((always_inline)) {  // the lane, for what is worked out again at each use (held along, it spills)
+    int at = lane;
+    asm volatile("" : "+v"(at));
+    return at;
+  };
+  auto q8_begin = [&](int u) __attribute__((always_inline)) {  // K of unit u is requested
+    const int t = kPass * u + 1 + w_tile, t0 = min(lo + t * kWideTile + w_row, (hi_row - 1) & ~15);
     coming = -1;
+    if (u >= n_units) return;
+    entry = (u + 1) & 63;
+    if (entry == 0) window.fill(a, it, lo + (kPass * (u + lane) + 1 + w_tile) * kWideTile + w_row, hi_row);
+    if (t < 0) return;
+    coming = t;
+    q8_off = offset_in(a.b, __builtin_amdgcn_readlane(window.id, entry), (uint32_t)t0) + (int64_t)it.g * a.b.head_stride;
+    q8.fetch(a.b.k + q8_off, a.b.row_stride, here());
+  };
+  auto q8_middle = [&]() __attribute__((always_inline)) {  // ... is in LDS, V is requested
+    if (coming < 0) return;
+    q8.template to_lds<true>(smem + (coming % S) * G::kSlot, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.k, entry)), here());
+    q8.fetch(a.b.v + q8_off, a.b.row_stride, here());
+  };
+  auto q8_end = [&]() __attribute__((always_inline)) {
+    if (coming < 0) return;
+    q8.template to_lds<false>(smem + (coming % S) * G::kSlot + G::kHalf, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.v, entry)), here());
   };
   auto request = [&]() __attribute__((always_inline)) {
     const int u = unit++, t = kPass * u + 1 + w_tile, t0 = lo + t * kWideTile + w_row;
     if constexpr (Q8) {
-      commit();
-      if (u >= n_units) return;
-      if (((u + 1) & 63) == 0) window.fill(a, it, lo + (kPass * (u + lane) + 1 + w_tile) * kWideTile + w_row, hi_row);
-      if (t < 0) return;
-      q8.fetch(a, it.g, window, (u + 1) & 63, min(t0, (hi_row - 1) & ~15), lane);
-      coming = t;
+      q8_begin(u);
       return;
     }
     if (t < 0 || u >= n_units) return;
@@ -127,7 +143,7 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
   // slots that are filled next have arrived (their products stand before this, but nothing else keeps them there).
   auto landed = [&](int u) __attribute__((always_inline)) {
     if constexpr (Q8) {
-      commit();
+      q8_end();
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       return;
     }
@@ -139,13 +155,24 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
   };
   static_assert(G::kAhead <= 3, "landed() tells two newer units apart");
 #pragma unroll 1
-  for (int u = -1; u < G::kAhead; ++u) request();
+  for (int u = -1; u < G::kAhead; ++u) {
+    request();
+    if constexpr (Q8) {
+      q8_middle();
+      if (u < 0) q8_end();
+    }
+  }
 
   Rows<D> r[1];
   r[0].init();
   f32x16 s[2];
   u32x4 p[2], kf[KS], vf[DB][2];
-  auto slot = [&](int t) __attribute__((always_inline)) { return smem + (t % S) * G::kSlot; };
+  // (Q8: a slot's place as a number of its own.  As part of every fragment's address, kept up to date per fragment, it spills.)
+  auto slot = [&](int t) __attribute__((always_inline)) {
+    int at = (t % S) * G::kSlot;
+    if constexpr (Q8) asm("" : "+s"(at));
+    return smem + at;
+  };
   landed(0);
   if (my_tiles > 0) {
     read_k<D>(slot(0), lane, kf);
@@ -186,6 +213,7 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
     for (int u = 0; u < kPass; u += 2) {
       tile(masked_c, I0{}, t + u);
       tile(masked_c, I1{}, t + u + 1);
+      if (Q8 && u == 0) q8_middle();
     }
   };
   // (every wave passes np barriers; a tile takes the next one's scores, too)
@@ -206,6 +234,7 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
       using Yes = std::integral_constant<bool, true>;
       if (t < my_tiles) tile(Yes{}, I0{}, t);
       if (t + 1 < my_tiles) tile(Yes{}, I1{}, t + 1);
+      if (Q8 && u == 0) q8_middle();
     }
   }
   // the requests past the last pass land before the workgroup's LDS is released

@@ -238,7 +238,7 @@ respec_status attend(const respec_chunk_plan* plan, const respec_chunk_attn_args
     // Calls of at most 64 query rows per KV head have the few-row kernel, of one or two groups of 32; others have
     // 256-row blocks, and sequences of up to 32 rows among them the few-row kernel's way in the same launch.
     const bool wide = rows > 64, mixed = wide && a.b.batch > 1;
-    a.few_rows = !wide ? (rows <= 32 ? 32 : 64) : mixed ? 32 : 0;
+    a.few_rows = !wide ? (q8 && rows <= 16 ? 16 : rows <= 32 ? 32 : 64) : mixed ? 32 : 0;
     a.few = !wide || mixed ? geometry(a.b, a.few_rows, seqs, limit, 128, 128, 1,
                                       s.head_dim == 128 ? Pace{0.02, 6} : Pace{0.01, 6}, rb, held)
                            : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};

@@ -6,13 +6,13 @@ namespace respec {
 namespace {
 
 template <int D, int GR>
-__global__ __launch_bounds__(kAttnFewThreads, 1) void q8_attn_few_kernel(ChunkAttnArgs a) {
+__global__ __launch_bounds__(kAttnFewThreads, GR <= 2 ? 2 : 1) void q8_attn_few_kernel(ChunkAttnArgs a) {
   extern __shared__ __align__(1024) unsigned char smem[];
   if ((int)blockIdx.x >= a.few.items) {
     report_status<kAttnFewThreads>(a.b, (int)blockIdx.x - a.few.items, true);
     return;
   }
-  q8_few_rows_item<D, GR, false>(a, (int)blockIdx.x, smem);
+  q8_few_rows_item<D, GR>(a, (int)blockIdx.x, smem);
 }
 
 // MIXED: as chunk_attn_wide_kernel's.
@@ -27,7 +27,7 @@ __global__ __launch_bounds__(kAttnWideThreads, 1) void q8_attn_wide_kernel(Chunk
   x -= a.wide.items;
   if constexpr (MIXED) {
     if (x < a.few.items) {
-      if (threadIdx.x < 256) q8_few_rows_item<D, 1, D == 128>(a, x, smem);
+      if (threadIdx.x < 256) q8_few_rows_item<D, 2>(a, x, smem);
       return;
     }
     x -= a.few.items;
@@ -59,7 +59,7 @@ hipError_t go_wide(bool launch, const ChunkAttnArgs& a, bool status, hipStream_t
 template <int D>
 hipError_t set_limits() {
   const ChunkAttnArgs none{};
-  for (hipError_t e : {go_few<D, 1>(false, none, false, nullptr), go_few<D, 2>(false, none, false, nullptr),
+  for (hipError_t e : {go_few<D, 1>(false, none, false, nullptr), go_few<D, 2>(false, none, false, nullptr), go_few<D, 4>(false, none, false, nullptr),
                        go_wide<D, false>(false, none, false, nullptr), go_wide<D, true>(false, none, false, nullptr)})
     if (e != hipSuccess) return e;
   return hipSuccess;
@@ -68,8 +68,9 @@ hipError_t set_limits() {
 }  // namespace
 
 hipError_t launch_q8_attn_few(int head_dim, const ChunkAttnArgs& a, bool status, hipStream_t s) {
-  if (a.few.rows_per_wg == 32) return head_dim == 128 ? go_few<128, 1>(true, a, status, s) : go_few<64, 1>(true, a, status, s);
-  if (a.few.rows_per_wg == 64) return head_dim == 128 ? go_few<128, 2>(true, a, status, s) : go_few<64, 2>(true, a, status, s);
+  if (a.few.rows_per_wg == 16) return head_dim == 128 ? go_few<128, 1>(true, a, status, s) : go_few<64, 1>(true, a, status, s);
+  if (a.few.rows_per_wg == 32) return head_dim == 128 ? go_few<128, 2>(true, a, status, s) : go_few<64, 2>(true, a, status, s);
+  if (a.few.rows_per_wg == 64) return head_dim == 128 ? go_few<128, 4>(true, a, status, s) : go_few<64, 4>(true, a, status, s);
   return hipErrorInvalidValue;
 }
 hipError_t launch_q8_attn_wide(int head_dim, const ChunkAttnArgs& a, bool mixed, bool status, hipStream_t s) {

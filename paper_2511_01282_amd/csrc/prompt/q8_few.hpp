@@ -5,43 +5,42 @@
 // operands.
 #pragma once
 
-#include "chunk_few.hpp"
 #include "q8_tile.hpp"
 
 namespace respec {
 
+constexpr int kQ8Tile = 32;
+
 template <int D>
 struct Q8FewShape {
-  static constexpr int S = D == 128 ? 4 : 8;  // ring slots of a wave
-  static constexpr int kHalf = kFewTile * D;  // bytes of a K or V tile
+  static constexpr int S = D == 128 ? 2 : 4;  // ring slots of a wave
+  static constexpr int kHalf = kQ8Tile * D;   // bytes of a K or V tile
   static constexpr int kSlot = 2 * kHalf;
   static constexpr int kWave = S * kSlot;
   static constexpr int kMl = 4 * kWave;
   static constexpr int kLds = kMl + 4 * 64 * 8;
-  static_assert(kLds <= 163840 - 1024, "LDS of a CU, less report_status()'s");
+  static_assert(D * 64 <= kWave, "the waves hand their O over through their rings");
+  static_assert(kLds <= 163840 / 2 - 1024, "two workgroups to a CU");
 };
 
-// Waits until at most n tiles of R requests each are under way (n from 0 to 7).
+// Waits until at most n tiles of R requests each are under way (n from 0 to 3).
 template <int R>
 __device__ __forceinline__ void wait_tiles(int n) {
   switch (n) {
     case 0: asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); break;
     case 1: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R) : "memory"); break;
     case 2: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * R) : "memory"); break;
-    case 3: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * R) : "memory"); break;
-    case 4: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * R) : "memory"); break;
-    case 5: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(5 * R) : "memory"); break;
-    case 6: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(6 * R) : "memory"); break;
-    default: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(7 * R) : "memory"); break;
+    default: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * R) : "memory"); break;
   }
 }
 
-// Item x, by four waves (256 threads); GR groups of 32 query rows.
-template <int D, int GR, bool LEAN>
+// Item x, by four waves (256 threads); GR groups of 16 query rows.
+template <int D, int GR>
 __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, unsigned char* smem) {
   using G = Q8FewShape<D>;
-  constexpr int KS = D / 16, DB = D / 32, S = G::S;
+  constexpr int KS = D / 32, CB = D / 16, S = G::S;
   constexpr int NR = D / 64, RPI = 1024 / D, CPR = D / 16;  // requests of 16 rows, rows of a request, chunks of a row
+  static_assert(S <= 4, "wait_tiles()");
   const ChunkGeom& ge = a.few;
   const Item it = find_item(a.b, ge, 1, a.few_rows, x);
   const ChunkSeq& sq = it.seq;
@@ -52,10 +51,10 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
   if (lo >= limit) return;
   const bool whole = limit <= ge.split_rows;
   const int hi_row = whole ? limit : min(limit, lo + ge.split_rows);
-  const int nt = (hi_row - lo + kFewTile - 1) / kFewTile;
+  const int nt = (hi_row - lo + kQ8Tile - 1) / kQ8Tile;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r32 = lane & 31, hi = lane >> 5;
+  const int r16 = lane & 15, g4 = lane >> 4;
   const uint32_t lds0 =
       (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char*)smem + (uint32_t)(wave * G::kWave);
   const unsigned char* ring = smem + wave * G::kWave;
@@ -64,16 +63,16 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
   int64_t tok[GR], head[GR];
   int end[GR];
   u32x4 qf[GR][KS];
-  Rows<D> r[GR];
+  Rows16<D> r[GR];
 #pragma unroll
   for (int g = 0; g < GR; ++g) {
-    const int row = min(g * 32 + r32, rows - 1), i = (int)div_by((uint32_t)row, a.group);
+    const int row = min(g * 16 + r16, rows - 1), i = (int)div_by((uint32_t)row, a.group);
     tok[g] = sq.t0 + i;
     head[g] = (int64_t)it.g * a.b.group + (row - i * a.b.group);
     end[g] = min(sq.L + i + 1, hi_row);
     const char* q = a.q + tok[g] * a.q_tok + head[g] * a.q_head;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[g][ks] = ld16(q + (4 * (ks / 2) + 2 * hi + ks % 2) * 16);  // (as read_k8 orders them)
+    for (int ks = 0; ks < KS; ++ks) qf[g][ks] = ld16(q + (2 * (4 * (ks / 2) + g4) + ks % 2) * 16);  // (as read_k8 orders them)
     r[g].init();
   }
   const int unmasked = min(sq.L + 1, hi_row);  // rows that every query row sees
@@ -81,13 +80,14 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
   // ---- tiles: pages and scales of 64 of the wave's at a time, a lane for each; DMA of their rows, 16 at a time ----
   const char* kb = a.b.k + (int64_t)it.g * a.b.head_stride;
   const char* vb = a.b.v + (int64_t)it.g * a.b.head_stride;
-  uint32_t k_off[NR], v_off[NR];
+  uint32_t k_off[NR], v_off[2][NR];
 #pragma unroll
   for (int q = 0; q < NR; ++q) {
     const int rr = q * RPI + lane / CPR, pos = lane % CPR;
     const uint32_t row = (uint32_t)rr * a.b.row_stride + 1024u * (NR - 1 - q);
     k_off[q] = row + (uint32_t)((pos ^ k8_chunk<D>(rr)) * 16);
-    v_off[q] = row + (uint32_t)((pos ^ v8_chunk<D>(rr)) * 16);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) v_off[h][q] = row + (uint32_t)((pos ^ v8_chunk<D>(16 * h + rr)) * 16);
   }
   int32_t ids[2];
   uint32_t scales[2] = {0u, 0u};  // of 64 tiles each, by turns: bytes K, K, V, V of a tile's two halves
@@ -96,7 +96,7 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       Q8Window w;
-      w.fill(a, it, lo + ((base + lane) * 4 + wave) * kFewTile + h * 16, hi_row);
+      w.fill(a, it, lo + ((base + lane) * 4 + wave) * kQ8Tile + h * 16, hi_row);
       ids[h] = w.id;
       bytes |= (w.k | w.v << 16) << (8 * h);
     }
@@ -109,11 +109,11 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
     const uint32_t dst = lds0 + (uint32_t)((produced % S) * G::kSlot);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint32_t t0 = (uint32_t)min(lo + (produced * 4 + wave) * kFewTile + h * 16, (hi_row - 1) & ~15);
+      const uint32_t t0 = (uint32_t)min(lo + (produced * 4 + wave) * kQ8Tile + h * 16, (hi_row - 1) & ~15);
       const int64_t off = offset_in(a.b, __builtin_amdgcn_readlane(ids[h], produced & 63), t0) - 1024 * (NR - 1);
       const uint32_t to = dst + (uint32_t)(h * 16 * D);
       dma_rows<NR>(to, (uint64_t)(kb + off), k_off);
-      dma_rows<NR>(to + G::kHalf, (uint64_t)(vb + off), v_off);
+      dma_rows<NR>(to + G::kHalf, (uint64_t)(vb + off), v_off[h]);
     }
     ++produced;
   };
@@ -123,10 +123,7 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
 #pragma unroll
   for (int g = 0; g < GR; ++g)
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      if constexpr (GR > 1) asm volatile("" : "+a"(qf[g][ks]));
-      else asm volatile("" : "+v"(qf[g][ks]));
-    }
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[g][ks]));
   asm volatile("" : "+v"(scales[0]));
   for (int t = 0; t < min(my_nt, S); ++t) produce();
 
@@ -134,43 +131,90 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
   for (int j = 0; j < my_nt; ++j) {
     wait_tiles<4 * NR>(produced - 1 - j);
     const unsigned char* t = ring + (j % S) * G::kSlot;
-    const int key0 = lo + (j * 4 + wave) * kFewTile;
+    const int key0 = lo + (j * 4 + wave) * kQ8Tile;
     const uint32_t word = (uint32_t)__builtin_amdgcn_readlane((int)(j & 64 ? scales[1] : scales[0]), j & 63);
     const float v0 = q8_scale((word >> 16) & 0xFF), v1 = q8_scale(word >> 24);
-    u32x4 kf[KS], vf[DB][2], p[GR][2];
-    int at = lane;
-    if constexpr (LEAN) asm("" : "+v"(at));
-    read_k8<D>(t, at, q8_scale((at & 16 ? word >> 8 : word) & 0xFF), kf);
-    read_v8<D>(t + G::kHalf, at, v0, v1, vf);
-    f32x16 s[GR];
+    u32x4 kf[KS], vf[CB], p[GR];
+    f32x4 s[GR][2];
 #pragma unroll
-    for (int g = 0; g < GR; ++g) {
-      s[g] = f32x16{};
+    for (int h = 0; h < 2; ++h) {
+      read_k8<D>(t, lane, h, q8_scale((word >> (8 * h)) & 0xFF), kf);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s[g] = mma32(kf[ks], qf[g][ks], s[g]);
+      for (int g = 0; g < GR; ++g) {
+        s[g][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s[g][h] = mma16(kf[ks], qf[g][ks], s[g][h]);
+      }
     }
-    if (key0 + kFewTile <= unmasked) {
+    read_v8<D>(t + G::kHalf, lane, v0, v1, vf);
+    if (key0 + kQ8Tile <= unmasked) {
 #pragma unroll
-      for (int g = 0; g < GR; ++g) settle(r[g], s[g], a.scale_log2, p[g], weights(s[g], a.scale_log2, r[g].m, p[g]));
+      for (int g = 0; g < GR; ++g) settle16(r[g], s[g], a.scale_log2, p[g], weights16(s[g], a.scale_log2, r[g].m, p[g]));
     } else {
 #pragma unroll
       for (int g = 0; g < GR; ++g) {
-        mask_scores(s[g], key0, end[g], at);
-        settle(r[g], s[g], a.scale_log2, p[g], weights(s[g], a.scale_log2, r[g].m, p[g]));
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[g][h][i] = key0 + 16 * h + 4 * g4 + i < end[g] ? s[g][h][i] : kNegInf;
+        settle16(r[g], s[g], a.scale_log2, p[g], weights16(s[g], a.scale_log2, r[g].m, p[g]));
       }
-      if (take_out_not_finite<D>(vf)) add_not_finite8<D, GR>(r, t + G::kHalf, v0, v1, key0, end, at);
+      if (take_out_not_finite16<D>(vf)) add_not_finite16<D, GR>(r, t + G::kHalf, v0, v1, key0, end, lane);
     }
 #pragma unroll
-    for (int k2 = 0; k2 < 2; ++k2)
+    for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int g = 0; g < GR; ++g) r[g].o[db] = mma32(vf[db][k2], p[g][k2], r[g].o[db]);
+      for (int g = 0; g < GR; ++g) r[g].o[cb] = mma16(vf[cb], p[g], r[g].o[cb]);
     // this wave's reads of the slot are done before it is filled again
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (produced < my_nt) produce();
   }
-  join_waves<D, GR, G::kWave>(a, r, smem, reinterpret_cast<float2*>(smem + G::kMl), whole, it.split, tok, head, rows, wave, lane);
+
+  // ---- O = sum_w 2^(m_w - M) O_w, l likewise: every wave writes its own, and joins a quarter of the columns ----
+  float2* ml = reinterpret_cast<float2*>(smem + G::kMl);
+#pragma unroll
+  for (int g = 0; g < GR; ++g) {
+    if (g > 0) __syncthreads();
+    f32x4* to = reinterpret_cast<f32x4*>(smem + wave * G::kWave) + lane;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) to[cb * 64] = r[g].o[cb];
+    ml[wave * 64 + lane] = make_float2(r[g].m, r[g].l);
+    __syncthreads();
+    float M = kNoRef, w[4], l = 0.f;
+#pragma unroll
+    for (int w_ = 0; w_ < 4; ++w_) M = fmaxf(M, ml[w_ * 64 + lane].x);
+#pragma unroll
+    for (int w_ = 0; w_ < 4; ++w_) {
+      w[w_] = __builtin_amdgcn_exp2f(ml[w_ * 64 + lane].x - M);
+      l += w[w_] * ml[w_ * 64 + lane].y;
+    }
+    l += xchg<4>(l);
+    l += xchg<5>(l);
+    const bool mine = g * 16 + r16 < rows;
+    const int64_t pr = ((int64_t)it.split * a.b.total_new + tok[g]) * ((int64_t)a.b.n_kv_heads * a.b.group) + head[g];
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int c = 0; c < CB / 4; ++c) {
+      const int cb = wave * (CB / 4) + c, col = 16 * cb + 4 * g4;
+      f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w_ = 0; w_ < 4; ++w_) v += (reinterpret_cast<const f32x4*>(smem + w_ * G::kWave) + lane)[cb * 64] * w[w_];
+      if (!mine) continue;
+      if (whole) {
+        u32x2 y;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * e] * inv, v[2 * e + 1] * inv}, bf16x2));
+        *reinterpret_cast<u32x2*>(a.out + tok[g] * a.o_tok + head[g] * a.o_head + col * 2) = y;
+      } else {
+        *reinterpret_cast<f32x4*>(a.part_o + pr * D + col) = v;
+      }
+    }
+    if (!whole && mine && wave == 0 && g4 == 0) {
+      a.part_m[pr] = M;
+      a.part_l[pr] = l;
+    }
+  }
 }
 
 }  // namespace respec

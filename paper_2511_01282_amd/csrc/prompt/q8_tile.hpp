@@ -26,100 +26,164 @@ struct Q8Window {
   }
 };
 
-// 16 rows of K and V on their way through a wave's registers into tiles of bf16 (as chunk_tile.hpp's).
+// 16 rows of K or V on their way through a wave's registers into a tile of bf16 (as chunk_tile.hpp's).
 template <int D>
 struct Q8Rows {
   static constexpr int PPR = D / 16, N = D / 64;  // 16-byte pieces per row, of a lane
-  u32x4 k[N], v[N];
-  float k_scale, v_scale;
-  __device__ __forceinline__ void fetch(const ChunkAttnArgs& a, int g, const Q8Window& w, int entry, int r0, int lane) {
-    const int32_t id = __builtin_amdgcn_readlane(w.id, entry);
-    k_scale = q8_scale((uint32_t)__builtin_amdgcn_readlane((int)w.k, entry));
-    v_scale = q8_scale((uint32_t)__builtin_amdgcn_readlane((int)w.v, entry));
-    const int64_t off = offset_in(a.b, id, (uint32_t)r0) + (int64_t)g * a.b.head_stride;
+  u32x4 x[N];
+  // Rows at `rows` (this head's), `stride` bytes apart.
+  __device__ __forceinline__ void fetch(const char* rows, uint32_t stride, int lane) {
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const int p = u * 64 + lane;
-      const uint32_t in = (uint32_t)(p / PPR) * a.b.row_stride + (uint32_t)(p % PPR * 16);
-      k[u] = ld16(a.b.k + off + in);
-      v[u] = ld16(a.b.v + off + in);
+      x[u] = ld16(rows + ((uint32_t)(p / PPR) * stride + (uint32_t)(p % PPR * 16)));
     }
   }
-  __device__ __forceinline__ void to_lds(unsigned char* k_tile, unsigned char* v_tile, int row0, int lane) const {
+  // Into a tile from its row `row0` on.
+  template <bool K>
+  __device__ __forceinline__ void to_lds(unsigned char* tile, int row0, float scale, int lane) const {
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      const int p = u * 64 + lane, r = row0 + p / PPR, c = 2 * (p % PPR);
+      const int p = u * 64 + lane, r = row0 + p / PPR, c = 2 * (p % PPR), permuted = K ? k_chunk<D>(r) : v_chunk<D>(r);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        *reinterpret_cast<u32x4*>(k_tile + r * D * 2 + ((c + h) ^ k_chunk<D>(r)) * 16) = q8_bf16(u32x2{k[u][2 * h], k[u][2 * h + 1]}, k_scale);
-        *reinterpret_cast<u32x4*>(v_tile + r * D * 2 + ((c + h) ^ v_chunk<D>(r)) * 16) = q8_bf16(u32x2{v[u][2 * h], v[u][2 * h + 1]}, v_scale);
-      }
+      for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<u32x4*>(tile + r * D * 2 + ((c + h) ^ permuted) * 16) = q8_bf16(u32x2{x[u][2 * h], x[u][2 * h + 1]}, scale);
     }
   }
 };
 
-// Tiles of 32 rows of D codes, their 16-byte chunks permuted inside the row: reads of 16 rows (K), or of two chunks of 8 rows
-// (V), touch every bank once.
+// Tiles of 32 rows of D codes for products of 16 query rows, v_mfma_f32_16x16x32_bf16.  S^T = K Q^T of 16 keys leaves, in lane l,
+// the scores of query row l % 16 with keys 4 (l / 16) .. + 3; those of both halves of a tile are the B operand of O^T += V^T P^T
+// as they stand, if V's A operand takes its keys in the same order.
+//
+// The rows' 16-byte chunks are permuted inside the row (by the DMA's source addresses): the 16 rows that a quarter of a K read
+// takes, and the 16 that half of a transposing V read does, touch every bank once.
 template <int D>
 __device__ __forceinline__ int k8_chunk(int r) {
   return D == 128 ? ((r >> 1) & 7) : ((r >> 2) & 3);
 }
 template <int D>
 __device__ __forceinline__ int v8_chunk(int r) {
-  return D == 128 ? (r & 2) + ((r & 8) >> 1) : ((r & 8) >> 2);
+  return D == 128 ? ((r >> 1) & 3) + ((r & 16) >> 2) : ((r >> 2) & 1) + ((r & 16) >> 3);
 }
 
-// K fragments of 32 keys (A operand: lane l holds key l & 31, elements 32 (ks / 2) + 16 (l / 32) + 8 (ks % 2) ..).
+__device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) { return mma_k64(bf16_t{}, a, b, c); }
+
+// K fragments of 16 keys (A operand): lane l holds key l % 16, for step 2 j + e the elements 16 (4 j + l / 16) + 8 e .. + 7.
 template <int D>
-__device__ __forceinline__ void read_k8(const unsigned char* tile, int lane, float scale, u32x4 (&kf)[D / 16]) {
-  const int r32 = lane & 31, hi = lane >> 5;
+__device__ __forceinline__ void read_k8(const unsigned char* tile, int lane, int half, float scale, u32x4 (&kf)[D / 32]) {
+  const int r = 16 * half + (lane & 15), g = lane >> 4;
 #pragma unroll
-  for (int kk = 0; kk < D / 32; ++kk) {
-    const u32x4 x = *reinterpret_cast<const u32x4*>(tile + r32 * D + (((2 * kk + hi) ^ k8_chunk<D>(r32)) << 4));
-    kf[2 * kk] = q8_bf16(u32x2{x.x, x.y}, scale);
-    kf[2 * kk + 1] = q8_bf16(u32x2{x.z, x.w}, scale);
+  for (int j = 0; j < D / 64; ++j) {
+    const u32x4 x = *reinterpret_cast<const u32x4*>(tile + r * D + (((4 * j + g) ^ k8_chunk<D>(r)) << 4));
+    kf[2 * j] = q8_bf16(u32x2{x.x, x.y}, scale);
+    kf[2 * j + 1] = q8_bf16(u32x2{x.z, x.w}, scale);
   }
 }
 
-// V^T fragments of 32 keys as read_v's, by transposing reads: lane j of a 16-lane group addresses columns 8 (j % 2) .. of row
-// j / 2 of eight and receives column j of them.
+// V^T fragments of 32 keys (A operand): lane l holds column 16 cb + l % 16 of keys 4 (l / 16) .. + 3 and 16 further, by transposing
+// reads: lane j of a 16-lane group addresses columns 8 (j % 2) .. of row j / 2 of eight and receives column j of them.
 template <int D>
-__device__ __forceinline__ void read_v8(const unsigned char* tile, int lane, float s0, float s1, u32x4 (&vf)[D / 32][2]) {
+__device__ __forceinline__ void read_v8(const unsigned char* tile, int lane, float s0, float s1, u32x4 (&vf)[D / 16]) {
   typedef int i32x2 __attribute__((ext_vector_type(2)));
   typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
-  const int lr = lane & 15, dh = (lane >> 4) & 1, hi = lane >> 5, i = lr >> 1;
-  const int r = 4 * hi + i + (i & 4);  // rows 4 hi .. + 3 and 8 + 4 hi .. + 3 (and 16 further: the same permutation)
+  const int j = lane & 15, i = j >> 1, r = 4 * (lane >> 4) + (i & 3) + 4 * (i & 4);
+  const unsigned char* row = tile + r * D + (j & 1) * 8;
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int k2 = 0; k2 < 2; ++k2) {
-      const unsigned char* p = tile + (16 * k2 + r) * D + (((2 * db + dh) ^ v8_chunk<D>(r)) << 4) + (lr & 1) * 8;
-      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)p));
-      vf[db][k2] = q8_bf16(x, k2 ? s1 : s0);
-    }
+  for (int cb = 0; cb < D / 16; ++cb) {
+    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(row + ((cb ^ v8_chunk<D>(r)) << 4))));
+    const u32x4 lo = q8_bf16(x, s0), hi = q8_bf16(x, s1);
+    vf[cb] = u32x4{lo.x, lo.y, hi.z, hi.w};
+  }
 }
 
-// add_not_finite() over a tile of codes.
+// 16 query rows of a wave (lane l: row l % 16; its four lanes hold a quarter of the keys and columns each).
+template <int D>
+struct Rows16 {
+  f32x4 o[D / 16];  // columns 16 cb + 4 (l / 16) .. + 3
+  float m, l;       // as Rows'
+  float limit;
+
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int cb = 0; cb < D / 16; ++cb) o[cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = kNoRef;
+    l = 0.f;
+    limit = kSumLimit16;
+  }
+  static constexpr float kSumLimit16 = 2048.f;  // 8 weights of at most 2^8
+};
+
+// weights() and settle() of a tile's 8 scores per lane.
+template <bool FAR = false>
+__device__ __forceinline__ float weights16(const f32x4 (&s)[2], float scale_log2, float m, u32x4& p) {
+  const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+  float sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float p0 = __builtin_amdgcn_exp2f(less_ref<FAR>(s[w / 2][2 * (w % 2)], scale_log2, m));
+    const float p1 = __builtin_amdgcn_exp2f(less_ref<FAR>(s[w / 2][2 * (w % 2) + 1], scale_log2, m));
+    const bf16x2 h = __builtin_convertvector(f32x2{p0, p1}, bf16x2);
+    sum = __builtin_amdgcn_fdot2_f32_bf16(h, ones, sum, false);
+    p[w] = __builtin_bit_cast(uint32_t, h);
+  }
+  return sum;
+}
+template <int D>
+__device__ __forceinline__ void settle16(Rows16<D>& r, const f32x4 (&s)[2], float scale_log2, u32x4& p, float sum) {
+  if (__any(sum > r.limit)) {
+    float x = max_of(s[0][0], s[1][0]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) x = max_of(x, max_of(s[0][i], s[1][i]));
+    x = max_of(x, xchg<4>(x));
+    const float top = max_of(x, xchg<5>(x)) * scale_log2;
+    const float to = top > r.m + kRefMargin ? top : r.m;
+    const float alpha = __builtin_amdgcn_exp2f(r.m - to);
+    r.m = to;
+    r.limit = fabsf(to) > kFarRef && to != kNoRef ? -1.f : Rows16<D>::kSumLimit16;
+    r.l *= alpha;
+#pragma unroll
+    for (int cb = 0; cb < D / 16; ++cb) r.o[cb] *= alpha;
+    sum = weights16<true>(s, scale_log2, to, p);
+  }
+  r.l += sum;
+}
+
+// Values that are not finite, in tiles that some row does not see whole: see take_out_not_finite() and add_not_finite().
+template <int D>
+__device__ __forceinline__ bool take_out_not_finite16(u32x4 (&vf)[D / 16]) {
+  u16x2 top = {0, 0};
+#pragma unroll
+  for (int cb = 0; cb < D / 16; ++cb)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vf[cb][w] & 0x7FFF7FFFu));
+  if (!__any(top[0] >= 0x7F80 || top[1] >= 0x7F80)) return false;
+#pragma unroll
+  for (int cb = 0; cb < D / 16; ++cb)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t x = vf[cb][w];
+      vf[cb][w] = ((x & 0x7F80u) == 0x7F80u ? 0u : x & 0xFFFFu) | ((x & 0x7F800000u) == 0x7F800000u ? 0u : x & 0xFFFF0000u);
+    }
+  return true;
+}
 template <int D, int G>
-__device__ __forceinline__ void add_not_finite8(Rows<D> (&rows)[G], const unsigned char* v_tile, float s0, float s1, int key0,
-                                                const int (&end)[G], int lane) {
+__device__ __forceinline__ void add_not_finite16(Rows16<D> (&rows)[G], const unsigned char* v_tile, float s0, float s1, int key0,
+                                                 const int (&end)[G], int lane) {
 #pragma unroll 1
   for (int key = 0; key < 32; ++key)
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
+    for (int cb = 0; cb < D / 16; ++cb) {
+      const uint32_t x = *reinterpret_cast<const uint32_t*>(v_tile + key * D + ((cb ^ v8_chunk<D>(key)) << 4) + 4 * (lane >> 4));
+      const u32x4 y = q8_bf16(u32x2{x, 0u}, key < 16 ? s0 : s1);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int col = 32 * db + 8 * q + 4 * (lane >> 5);
-        const uint32_t x = *reinterpret_cast<const uint32_t*>(v_tile + key * D + (((col >> 4) ^ v8_chunk<D>(key)) << 4) + (col & 15));
-        const u32x4 y = q8_bf16(u32x2{x, 0u}, key < 16 ? s0 : s1);
+      for (int e = 0; e < 4; ++e) {
+        const float v = bf16_to_f32((uint16_t)(y[e / 2] >> (16 * (e % 2))));
+        const bool odd = !(fabsf(v) < __builtin_huge_valf());
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float v = bf16_to_f32((uint16_t)(y[e / 2] >> (16 * (e % 2))));
-          const bool odd = !(fabsf(v) < __builtin_huge_valf());
-#pragma unroll
-          for (int g = 0; g < G; ++g) rows[g].o[db][4 * q + e] += odd && key0 + key < end[g] ? v : 0.f;
-        }
+        for (int g = 0; g < G; ++g) rows[g].o[cb][e] += odd && key0 + key < end[g] ? v : 0.f;
       }
+    }
 }
 
 }  // namespace respec

@@ -99,11 +99,7 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
   Q8Rows<D> q8;
   int coming = -1, entry = 0;  // its first tile (none: -1), its lane of the window
   int64_t q8_off = 0;
-  auto here = [&]() __attribute__((always_inline)) {  // the lane, for what is worked out again at each use (held along, it spills)
-    int at = lane;
-    asm volatile("" : "+v"(at));
-    return at;
-  };
+  const uint32_t q8_from = Q8Rows<D>::from(a.b.row_stride, lane), q8_k = Q8Rows<D>::template to<true>(lane), q8_v = Q8Rows<D>::template to<false>(lane);
   auto q8_begin = [&](int u) __attribute__((always_inline)) {  // K of unit u is requested
     const int t = kPass * u + 1 + w_tile, t0 = min(lo + t * kWideTile + w_row, (hi_row - 1) & ~15);
     coming = -1;
@@ -113,16 +109,18 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
     if (t < 0) return;
     coming = t;
     q8_off = offset_in(a.b, __builtin_amdgcn_readlane(window.id, entry), (uint32_t)t0) + (int64_t)it.g * a.b.head_stride;
-    q8.fetch(a.b.k + q8_off, a.b.row_stride, here());
+    q8.fetch(a.b.k + q8_off, a.b.row_stride, q8_from);
   };
   auto q8_middle = [&]() __attribute__((always_inline)) {  // ... is in LDS, V is requested
     if (coming < 0) return;
-    q8.template to_lds<true>(smem + (coming % S) * G::kSlot, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.k, entry)), here());
-    q8.fetch(a.b.v + q8_off, a.b.row_stride, here());
+    q8.template to_lds<true>(smem + (coming % S) * G::kSlot, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.k, entry)), q8_k);
+    q8.fetch(a.b.v + q8_off, a.b.row_stride, q8_from);
   };
   auto q8_end = [&]() __attribute__((always_inline)) {
     if (coming < 0) return;
-    q8.template to_lds<false>(smem + (coming % S) * G::kSlot + G::kHalf, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.v, entry)), here());
+    const int valid = hi_row - (lo + coming * kWideTile + w_row);  // rows that some token sees
+    if (valid < kRows) q8.clear_from(valid, lane);
+    q8.template to_lds<false>(smem + (coming % S) * G::kSlot + G::kHalf, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.v, entry)), q8_v);
   };
   auto request = [&]() __attribute__((always_inline)) {
     const int u = unit++, t = kPass * u + 1 + w_tile, t0 = lo + t * kWideTile + w_row;

@@ -23,15 +23,13 @@ struct Q8FewShape {
   static_assert(kLds <= 163840 / 2 - 1024, "two workgroups to a CU");
 };
 
-// Waits until at most n tiles of R requests each are under way (n from 0 to 3).
-template <int R>
+// Waits until at most n tiles of R requests each are under way, n < S.
+template <int R, int S>
 __device__ __forceinline__ void wait_tiles(int n) {
-  switch (n) {
-    case 0: asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); break;
-    case 1: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R) : "memory"); break;
-    case 2: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * R) : "memory"); break;
-    default: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * R) : "memory"); break;
-  }
+  if (S > 3 && n == 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * R) : "memory");
+  else if (S > 2 && n == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * R) : "memory");
+  else if (S > 1 && n == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R) : "memory");
+  else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
 // Item x, by four waves (256 threads); GR groups of 16 query rows.
@@ -89,15 +87,18 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
 #pragma unroll
     for (int h = 0; h < 2; ++h) v_off[h][q] = row + (uint32_t)((pos ^ v8_chunk<D>(16 * h + rr)) * 16);
   }
-  int32_t ids[2];
+  uint32_t at_lo[2], at_hi[2];    // where a half's rows lie in this head of the cache (64 bits, for dma_rows)
   uint32_t scales[2] = {0u, 0u};  // of 64 tiles each, by turns: bytes K, K, V, V of a tile's two halves
   auto fill = [&](int base) {
     uint32_t bytes = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       Q8Window w;
-      w.fill(a, it, lo + ((base + lane) * 4 + wave) * kQ8Tile + h * 16, hi_row);
-      ids[h] = w.id;
+      const int r0 = lo + ((base + lane) * 4 + wave) * kQ8Tile + h * 16;
+      w.fill(a, it, r0, hi_row);
+      const uint64_t off = (uint64_t)(offset_in(a.b, w.id, (uint32_t)min(r0, (hi_row - 1) & ~15)) - 1024 * (NR - 1));
+      at_lo[h] = (uint32_t)off;
+      at_hi[h] = (uint32_t)(off >> 32);
       bytes |= (w.k | w.v << 16) << (8 * h);
     }
     if (base & 64) scales[1] = bytes;
@@ -109,8 +110,8 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
     const uint32_t dst = lds0 + (uint32_t)((produced % S) * G::kSlot);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint32_t t0 = (uint32_t)min(lo + (produced * 4 + wave) * kQ8Tile + h * 16, (hi_row - 1) & ~15);
-      const int64_t off = offset_in(a.b, __builtin_amdgcn_readlane(ids[h], produced & 63), t0) - 1024 * (NR - 1);
+      const int i = produced & 63;
+      const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_hi[h], i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)at_lo[h], i);
       const uint32_t to = dst + (uint32_t)(h * 16 * D);
       dma_rows<NR>(to, (uint64_t)(kb + off), k_off);
       dma_rows<NR>(to + G::kHalf, (uint64_t)(vb + off), v_off[h]);
@@ -129,24 +130,31 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
 
 #pragma unroll 1
   for (int j = 0; j < my_nt; ++j) {
-    wait_tiles<4 * NR>(produced - 1 - j);
+    wait_tiles<4 * NR, S>(produced - 1 - j);
     const unsigned char* t = ring + (j % S) * G::kSlot;
     const int key0 = lo + (j * 4 + wave) * kQ8Tile;
     const uint32_t word = (uint32_t)__builtin_amdgcn_readlane((int)(j & 64 ? scales[1] : scales[0]), j & 63);
     const float v0 = q8_scale((word >> 16) & 0xFF), v1 = q8_scale(word >> 24);
-    u32x4 kf[KS], vf[CB], p[GR];
+    u32x4 vf[CB], p[GR];
     f32x4 s[GR][2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      read_k8<D>(t, lane, h, q8_scale((word >> (8 * h)) & 0xFF), kf);
+    for (int g = 0; g < GR; ++g) s[g][0] = s[g][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // (neighbouring products are of different sums, the halves' of one group or the groups' of one half: one that waits for the
+    // product before it costs more)
+    constexpr int HH = GR == 1 ? 2 : 1;
 #pragma unroll
-      for (int g = 0; g < GR; ++g) {
-        s[g][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int h0 = 0; h0 < 2; h0 += HH) {
+      u32x4 kf[HH][KS];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s[g][h] = mma16(kf[ks], qf[g][ks], s[g][h]);
-      }
+      for (int h = 0; h < HH; ++h) read_k8<D>(t, lane, h0 + h, q8_scale((word >> (8 * (h0 + h))) & 0xFF), kf[h]);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int g = 0; g < GR; ++g)
+#pragma unroll
+          for (int h = 0; h < HH; ++h) s[g][h0 + h] = mma16(kf[h][ks], qf[g][ks], s[g][h0 + h]);
     }
-    read_v8<D>(t + G::kHalf, lane, v0, v1, vf);
+    read_v8<D>(t + G::kHalf, lane, v0, v1, hi_row - key0, vf);
     if (key0 + kQ8Tile <= unmasked) {
 #pragma unroll
       for (int g = 0; g < GR; ++g) settle16(r[g], s[g], a.scale_log2, p[g], weights16(s[g], a.scale_log2, r[g].m, p[g]));

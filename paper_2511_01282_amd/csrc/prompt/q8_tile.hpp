@@ -1,8 +1,9 @@
 // Tiles of an 8-bit paged cache (see q8.hpp), for the bf16 attention kernels (gfx950).
 //
 // Sixteen rows from a multiple of 16 lie in one page and share a scale (scale blocks are multiples of 16 rows, pages of
-// blocks), so a wave's rows come 16 at a time from one address, whole also where the sequence ends inside them (what
-// is behind the end is masked).  bf16 holds e4m3 values times a power of two exactly.
+// blocks), so a wave's rows come 16 at a time from one address, whole also where the sequence ends inside them: keys
+// behind the end are masked in the scores, and their values, which a reused page may well hold NaNs in, count as zeros.
+// bf16 holds e4m3 values times a power of two exactly.
 #pragma once
 
 #include "chunk_tile.hpp"
@@ -31,24 +32,36 @@ template <int D>
 struct Q8Rows {
   static constexpr int PPR = D / 16, N = D / 64;  // 16-byte pieces per row, of a lane
   u32x4 x[N];
-  // Rows at `rows` (this head's), `stride` bytes apart.
-  __device__ __forceinline__ void fetch(const char* rows, uint32_t stride, int lane) {
-#pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const int p = u * 64 + lane;
-      x[u] = ld16(rows + ((uint32_t)(p / PPR) * stride + (uint32_t)(p % PPR * 16)));
-    }
-  }
-  // Into a tile from its row `row0` on.
+  // A lane's places: in memory, from the first row on, and in a tile of bf16 (its first 16 bytes of 32), row 0 on.
+  static __device__ __forceinline__ uint32_t from(uint32_t stride, int lane) { return (uint32_t)(lane / PPR) * stride + (uint32_t)(lane % PPR * 16); }
   template <bool K>
-  __device__ __forceinline__ void to_lds(unsigned char* tile, int row0, float scale, int lane) const {
+  static __device__ __forceinline__ uint32_t to(int lane) {
+    const int r = lane / PPR, c = 2 * (lane % PPR);
+    return (uint32_t)(r * D * 2 + ((c ^ (K ? k_chunk<D>(r) : v_chunk<D>(r))) << 4));
+  }
+  // Rows at `rows` (this head's), `stride` bytes apart.
+  __device__ __forceinline__ void fetch(const char* rows, uint32_t stride, uint32_t from) {
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const int p = u * 64 + lane, r = row0 + p / PPR, c = 2 * (p % PPR), permuted = K ? k_chunk<D>(r) : v_chunk<D>(r);
+    for (int u = 0; u < N; ++u) x[u] = ld16(rows + u * 8 * (uint64_t)stride + from);
+  }
+  // Rows from `valid` on become zeros.
+  __device__ __forceinline__ void clear_from(int valid, int lane) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        *reinterpret_cast<u32x4*>(tile + r * D * 2 + ((c + h) ^ permuted) * 16) = q8_bf16(u32x2{x[u][2 * h], x[u][2 * h + 1]}, scale);
-    }
+    for (int u = 0; u < N; ++u)
+      if ((u * 64 + lane) / PPR >= valid) x[u] = u32x4{0u, 0u, 0u, 0u};
+  }
+  // Into a tile at its row `row0`, 0 or 16: chunk c + 1 is c's neighbour (c is even), and 8 rows further the permutation has
+  // its bit of 8 changed (K's of 128 columns) or is the same.
+  template <bool K>
+  __device__ __forceinline__ void to_lds(unsigned char* tile, int row0, float scale, uint32_t to) const {
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)tile + (uint32_t)(row0 * D * 2) + to;
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t here = (at ^ (uint32_t)(16 * h + (K ? 128 * u : 0))) + (uint32_t)(u * 8 * D * 2);
+        *(__attribute__((address_space(3))) u32x4*)(uintptr_t)here = q8_bf16(u32x2{x[u][2 * h], x[u][2 * h + 1]}, scale);
+      }
   }
 };
 
@@ -83,16 +96,30 @@ __device__ __forceinline__ void read_k8(const unsigned char* tile, int lane, int
 
 // V^T fragments of 32 keys (A operand): lane l holds column 16 cb + l % 16 of keys 4 (l / 16) .. + 3 and 16 further, by transposing
 // reads: lane j of a 16-lane group addresses columns 8 (j % 2) .. of row j / 2 of eight and receives column j of them.
+// Keys from `valid` on count as zeros.
 template <int D>
-__device__ __forceinline__ void read_v8(const unsigned char* tile, int lane, float s0, float s1, u32x4 (&vf)[D / 16]) {
+__device__ __forceinline__ void read_v8(const unsigned char* tile, int lane, float s0, float s1, int valid, u32x4 (&vf)[D / 16]) {
   typedef int i32x2 __attribute__((ext_vector_type(2)));
   typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
   const int j = lane & 15, i = j >> 1, r = 4 * (lane >> 4) + (i & 3) + 4 * (i & 4);
   const unsigned char* row = tile + r * D + (j & 1) * 8;
+  u32x2 x[D / 16];
+#pragma unroll
+  for (int cb = 0; cb < D / 16; ++cb)
+    x[cb] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(row + ((cb ^ v8_chunk<D>(r)) << 4))));
+  if (valid < 32) {  // (uniform)
+    u32x2 mask;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int keys = valid - 16 * h - 4 * (lane >> 4);  // of these four
+      mask[h] = keys >= 4 ? ~0u : keys <= 0 ? 0u : (1u << (8 * keys)) - 1;
+    }
+#pragma unroll
+    for (int cb = 0; cb < D / 16; ++cb) x[cb] &= mask;
+  }
 #pragma unroll
   for (int cb = 0; cb < D / 16; ++cb) {
-    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(row + ((cb ^ v8_chunk<D>(r)) << 4))));
-    const u32x4 lo = q8_bf16(x, s0), hi = q8_bf16(x, s1);
+    const u32x4 lo = q8_bf16(x[cb], s0), hi = q8_bf16(x[cb], s1);
     vf[cb] = u32x4{lo.x, lo.y, hi.z, hi.w};
   }
 }

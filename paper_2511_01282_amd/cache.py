@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 
 import torch
 
@@ -48,6 +49,11 @@ class CopyArgs(ctypes.Structure):
     _fields_ = [("pairs", _I32), ("src", _P), ("dst", _P), ("n_pages", _I32), ("n_planes", _I32), ("planes", _P),
                 ("status", _P)]
 
+
+# the same as one call packs them (native alignment; ctypes takes twice as long to fill such structures)
+_ROTARY = struct.Struct("@iPiPP" "PqqPqq" "PqqPqq" "P")
+_KEEP = struct.Struct("@iiiii" "PPiiqqqPiq" "qPPiqPPP")
+_COPY = struct.Struct("@iPPiiPP")
 
 _READY = False
 
@@ -131,7 +137,7 @@ class RotaryPlan(_Plan):
         if x is None or y is None:
             if x is not None or y is not None:
                 raise ValueError(f"{name} and {name}_out: both or neither expected")
-            return None, (None, 0, 0, None, 0, 0)
+            return None, (0, 0, 0, 0, 0, 0)
         dims = (x.shape[0], heads, self.shape.head_dim)
         xp, st = self._rows(x, name, self.dtype, dims)
         yp, y_st = self._rows(y, name + "_out", self.dtype, dims)
@@ -152,15 +158,15 @@ class RotaryPlan(_Plan):
         if positions is not None:
             if new_off is not None or kv_len is not None or status is not None:
                 raise ValueError("positions, or new_off and kv_len (and their status), expected")
-            a = RotaryArgs(tokens, self._flat(positions, "positions", i32, (tokens,)), 0, None, None, *qs, *ks, None)
+            a = _ROTARY.pack(tokens, self._flat(positions, "positions", i32, (tokens,)), 0, 0, 0, *qs, *ks, 0)
         else:
             if new_off is None or kv_len is None:
                 raise ValueError("positions, or new_off and kv_len, expected")
             batch = kv_len.shape[0]
-            a = RotaryArgs(tokens, None, batch, self._flat(new_off, "new_off", i32, (batch + 1,)),
-                           self._flat(kv_len, "kv_len", i32, (batch,)), *qs, *ks,
-                           None if status is None else self._flat(status, "status", i32, (batch,)))
-        self._call(lib().respec_rotary, "respec_rotary", (ctypes.byref(a),), stream)
+            a = _ROTARY.pack(tokens, 0, batch, self._flat(new_off, "new_off", i32, (batch + 1,)),
+                             self._flat(kv_len, "kv_len", i32, (batch,)), *qs, *ks,
+                             0 if status is None else self._flat(status, "status", i32, (batch,)))
+        self._call(lib().respec_rotary, "respec_rotary", (a,), stream)
 
 
 class CacheLayers:
@@ -211,7 +217,8 @@ class CacheLayers:
         self.n_pages = shape[1]
 
     def _flat(self, t, name, shape):
-        if t.shape != shape or t.dtype != torch.int32 or t.device != self.device or (t.stride(-1) != 1 and shape[-1] > 1):
+        if t.shape != shape or t.dtype is not torch.int32 or t.get_device() != self._index or (t.stride(-1) != 1 and shape[-1] > 1) or (
+                self._index < 0 and t.device != self.device):
             raise ValueError(f"{name}: {torch.int32} {tuple(shape)} on {self.device}, the last dimension contiguous, expected; got "
                              f"{t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
         return t.data_ptr()
@@ -224,10 +231,10 @@ class CacheLayers:
         else:
             raw = stream.cuda_stream
         if torch.cuda.current_device() == self._index:
-            status = fn(ctypes.byref(args), raw)
+            status = fn(args, raw)
         else:
             with torch.cuda.device(self.device):
-                status = fn(ctypes.byref(args), raw)
+                status = fn(args, raw)
         if status != OK:
             raise VerifyError(status, name)
 
@@ -242,17 +249,17 @@ class CacheLayers:
             raise ValueError(f"path: [sequences][nodes] expected; got {tuple(path.shape)}")
         table = self._flat(page_table, "page_table", (batch, width))
         steps = path.shape[1]
-        a = KeepArgs(batch, *self._keep, PagedCache(*self._cache, table, width, page_table.stride(0)), self._layer,
-                     self._flat(kv_len, "kv_len", (batch,)), self._flat(path, "path", (batch, steps)), steps, path.stride(0),
-                     self._flat(acc_len, "acc_len", (batch,)),
-                     None if kv_len_out is None else self._flat(kv_len_out, "kv_len_out", (batch,)),
-                     None if status is None else self._flat(status, "status", (batch,)))
+        a = _KEEP.pack(batch, *self._keep, *self._cache, table, width, page_table.stride(0), self._layer,
+                       self._flat(kv_len, "kv_len", (batch,)), self._flat(path, "path", (batch, steps)), steps, path.stride(0),
+                       self._flat(acc_len, "acc_len", (batch,)),
+                       0 if kv_len_out is None else self._flat(kv_len_out, "kv_len_out", (batch,)),
+                       0 if status is None else self._flat(status, "status", (batch,)))
         self._call(lib().respec_cache_keep, "respec_cache_keep", a, stream)
 
     def copy_pages(self, src, dst, *, status=None, stream=None) -> None:
         """Enqueue respec_cache_copy: page ``dst[i]`` becomes a copy of page ``src[i]`` (-1: none), values and scales, in every
         layer."""
         pairs = (src.shape[0],)
-        a = CopyArgs(pairs[0], self._flat(src, "src", pairs), self._flat(dst, "dst", pairs), self.n_pages, self._n,
-                     ctypes.addressof(self._pages), None if status is None else self._flat(status, "status", pairs))
+        a = _COPY.pack(pairs[0], self._flat(src, "src", pairs), self._flat(dst, "dst", pairs), self.n_pages, self._n,
+                       ctypes.addressof(self._pages), 0 if status is None else self._flat(status, "status", pairs))
         self._call(lib().respec_cache_copy, "respec_cache_copy", a, stream)

@@ -8,6 +8,7 @@ the last dimension is contiguous.
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
@@ -66,6 +67,12 @@ class Q8AppendArgs(ctypes.Structure):
 
 class Q8AttnArgs(ctypes.Structure):
     _fields_ = [("b", Q8Batch), *AttnArgs._fields_[1:]]
+
+
+# the same as one call packs them (native alignment; ctypes takes twice as long to fill such structures)
+_Q8_BATCH = "iiiiPP" "PPPPiiiqqqqqPiq" "P"
+_Q8_APPEND = struct.Struct("@" + _Q8_BATCH + "PPqqqq")
+_Q8_ATTN = struct.Struct("@" + _Q8_BATCH + "PqqPqqf0P")
 
 
 class ScoreShape(ctypes.Structure):
@@ -153,14 +160,12 @@ class _Plan:
                          f"offsets, lengths, tokens and results), expected; got {t.dtype} {tuple(t.shape)}, strides "
                          f"{t.stride()}, on {t.device}")
 
-    def _here(self, t):
-        return t.get_device() == self._index and (self._index >= 0 or t.device == self.device)
-
     def _rows(self, t, name, dtype, shape):
         """Address and strides of a tensor of rows: the last dimension contiguous (where it has more than one), strides
         of dimensions of one element 0."""
         st = t.stride()
-        if t.shape != shape or t.dtype != dtype or not self._here(t) or (st[-1] != 1 and shape[-1] > 1):
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != self._index or (st[-1] != 1 and shape[-1] > 1) or (
+                self._index < 0 and t.device != self.device):
             self._refuse(t, name, dtype, shape)
         if 1 in shape:
             st = [0 if n == 1 else s for n, s in zip(shape, st)]
@@ -168,7 +173,8 @@ class _Plan:
 
     def _flat(self, t, name, dtype, shape):
         """Address of a contiguous tensor."""
-        if t.shape != shape or t.dtype != dtype or not self._here(t) or not t.is_contiguous():
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != self._index or not t.is_contiguous() or (
+                self._index < 0 and t.device != self.device):
             self._refuse(t, name, dtype, shape)
         return t.data_ptr()
 
@@ -259,26 +265,28 @@ class ChunkPlan(_Plan):
 
 
     def _batch_q8(self, k_pages, v_pages, k_scale, v_scale, page_table, new_off, kv_len, total_new, max_new, max_kv_len, status):
-        s, i32 = self.shape, torch.int32
+        """The fields of a respec_q8_batch."""
+        s, i32, rows = self.shape, torch.int32, self._rows
         n_pages, _, page, _ = k_pages.shape
         batch, width = page_table.shape
-        dims = (n_pages, s.n_kv_heads, page, s.head_dim)
-        k, st = self._rows(k_pages, "k_pages", _E4M3, dims)
-        v, v_st = self._rows(v_pages, "v_pages", _E4M3, dims)
+        heads = s.n_kv_heads
+        dims = (n_pages, heads, page, s.head_dim)
+        k, st = rows(k_pages, "k_pages", _E4M3, dims)
+        v, v_st = rows(v_pages, "v_pages", _E4M3, dims)
         blocks = k_scale.shape[-1] if k_scale.dim() == 3 else 0
         if blocks < 1 or page % blocks:
             raise ValueError(f"k_scale: [pages][heads][blocks of a page] expected, {page} rows a page in whole blocks; got "
                              f"{tuple(k_scale.shape)}")
-        ks, s_st = self._rows(k_scale, "k_scale", _E8M0, dims[:2] + (blocks,))
-        vs, vs_st = self._rows(v_scale, "v_scale", _E8M0, dims[:2] + (blocks,))
-        if st != v_st or s_st != vs_st:
+        dims = (n_pages, heads, blocks)
+        ks, s_st = rows(k_scale, "k_scale", _E8M0, dims)
+        vs, vs_st = rows(v_scale, "v_scale", _E8M0, dims)
+        # (the last dimension is contiguous, or of one element)
+        if st[:3] != v_st[:3] or s_st[:2] != vs_st[:2]:
             raise ValueError("k_pages and v_pages, or their scales, are laid out differently")
-        table, t_st = self._rows(page_table, "page_table", i32, (batch, width))
-        return Q8Batch(batch, total_new, max_new, max_kv_len, self._flat(new_off, "new_off", i32, (batch + 1,)),
-                       self._flat(kv_len, "kv_len", i32, (batch,)),
-                       Q8Cache(k, v, ks, vs, n_pages, page, page // blocks, st[0], st[1], st[2], s_st[0], s_st[1], table, width,
-                               t_st[0]),
-                       None if status is None else self._flat(status, "status", i32, (batch,)))
+        table, t_st = rows(page_table, "page_table", i32, (batch, width))
+        return (batch, total_new, max_new, max_kv_len, self._flat(new_off, "new_off", i32, (batch + 1,)),
+                self._flat(kv_len, "kv_len", i32, (batch,)), k, v, ks, vs, n_pages, page, page // blocks, st[0], st[1], st[2], s_st[0],
+                s_st[1], table, width, t_st[0], 0 if status is None else self._flat(status, "status", i32, (batch,)))
 
     def append_q8(self, k_new, v_new, k_pages, v_pages, k_scale, v_scale, page_table, new_off, kv_len, *, max_new_in_batch,
                   status=None, max_kv_len_in_batch=None, stream=None) -> None:
@@ -291,8 +299,8 @@ class ChunkPlan(_Plan):
         v, v_st = self._rows(v_new, "v_new", self.dtype, dims)
         b = self._batch_q8(k_pages, v_pages, k_scale, v_scale, page_table, new_off, kv_len, dims[0], max_new_in_batch,
                            s.max_kv_len if max_kv_len_in_batch is None else max_kv_len_in_batch, status)
-        a = Q8AppendArgs(b, k, v, k_st[0], k_st[1], v_st[0], v_st[1])
-        self._call(lib().respec_chunk_append_q8, "respec_chunk_append_q8", (ctypes.byref(a),), stream)
+        a = _Q8_APPEND.pack(*b, k, v, k_st[0], k_st[1], v_st[0], v_st[1])
+        self._call(lib().respec_chunk_append_q8, "respec_chunk_append_q8", (a,), stream)
 
     def attend_q8(self, q, k_pages, v_pages, k_scale, v_scale, page_table, new_off, kv_len, out, *, max_new_in_batch,
                   max_kv_len_in_batch, scale=None, status=None, stream=None) -> None:
@@ -304,8 +312,8 @@ class ChunkPlan(_Plan):
         scale_f = _scale(scale)
         b = self._batch_q8(k_pages, v_pages, k_scale, v_scale, page_table, new_off, kv_len, dims[0], max_new_in_batch,
                            max_kv_len_in_batch, status)
-        a = Q8AttnArgs(b, qp, q_st[0], q_st[1], op, o_st[0], o_st[1], scale_f)
-        self._call(lib().respec_chunk_attn_q8, "respec_chunk_attn_q8", (ctypes.byref(a), self.workspace_ptr), stream)
+        a = _Q8_ATTN.pack(*b, qp, q_st[0], q_st[1], op, o_st[0], o_st[1], scale_f)
+        self._call(lib().respec_chunk_attn_q8, "respec_chunk_attn_q8", (a, self.workspace_ptr), stream)
 
 
 # outputs of a scoring call: type, and whether they hold the top alternatives' columns

@@ -51,6 +51,23 @@ def test_structs_match_the_header(lib, p, tmp_path):  # noqa: F811
     assert [int(x) for x in subprocess.check_output([exe]).split()] == want
 
 
+def test_packed_arguments_match_the_structs(lib, p):  # noqa: F811
+    """What the binding packs in one call lies as the structures' fields do."""
+    def flat(s, at=0):
+        for name, kind in s._fields_:
+            off = at + getattr(s, name).offset
+            yield from flat(kind, off) if issubclass(kind, ctypes.Structure) else [(off, kind)]
+
+    for packed, s in ((p._Q8_APPEND, p.Q8AppendArgs), (p._Q8_ATTN, p.Q8AttnArgs), (lib._ROTARY, lib.RotaryArgs), (lib._KEEP, lib.KeepArgs),
+                      (lib._COPY, lib.CopyArgs)):
+        fields = list(flat(s))
+        values = [float(i + 1) if kind is ctypes.c_float else i + 1 for i, (_, kind) in enumerate(fields)]
+        raw = packed.pack(*values)
+        assert packed.size == ctypes.sizeof(s)
+        for (off, kind), v in zip(fields, values):
+            assert kind.from_buffer_copy(raw, off).value == v, s
+
+
 # ---------------------------------------------------------------------------
 # rotary positions
 # ---------------------------------------------------------------------------

@@ -47,7 +47,7 @@ typedef struct {
 
 /* Row t of q and k (one head's D columns) at position p: with w_i = frequency[i],
  *   y_a = amplitude (x_a cos(p w_i) - x_b sin(p w_i)),  y_b = amplitude (x_b cos(p w_i) + x_a sin(p w_i))
- * for pair i = (a, b); columns from rotary_dim on are copied.  Angles are within 2^-32 of
+ * for pair i = (a, b); columns from rotary_dim on are copied.  Angles are within 2^-31 of
  * a turn at every position; cosines, sines and products are float32, rounded once.
  * Positions are given one per token, or as a chunk batch's: token i of sequence b
  * stands at kv_len[b] + i.  A token at a negative position, one of no sequence and those of a
@@ -73,7 +73,7 @@ typedef struct {
 
 typedef struct respec_rotary_plan respec_rotary_plan;
 
-/* frequency: HOST array of rotary_dim / 2 doubles, radians per position, finite and >= 0 (copied). */
+/* frequency: HOST array of rotary_dim / 2 doubles, radians per position, 0 .. 2 pi (copied). */
 respec_status respec_rotary_create(const respec_rotary_shape* shape, const double* frequency, respec_rotary_plan** out);
 void respec_rotary_destroy(respec_rotary_plan* plan);
 respec_status respec_rotary(const respec_rotary_plan* plan, const respec_rotary_args* args, void* stream);
@@ -141,7 +141,8 @@ typedef struct {
  * a <= 448 2^k:  the scale is 2^k or, where rows of the sequence stand in the block already
  * (from its first row to kv_len - 1), the larger of that and the scale that they have; these
  * rows' values are rounded again if their scale grows.  A new value x becomes x 2^-k
- * rounded to nearest even; a NaN or an infinity becomes a NaN.  Rows of the block behind the new
+ * rounded to nearest even; a NaN or an infinity becomes a NaN.  (A value within 2^-5 of 2^128 of
+ * its size may round to 2^128, which attention takes for an infinity.)  Rows of the block behind the new
  * ones keep their bytes.
  * A block belongs to one sequence while it is written: what the rows of a block hold that two
  * sequences of the call write is unspecified (share whole blocks, copy a partly filled page

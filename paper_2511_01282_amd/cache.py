@@ -107,6 +107,9 @@ def frequencies(rotary_dim, base=10000.0, *, scaling=None, factor=1.0, original_
     return [x * k + x / factor * (1 - k) for x, k in zip(w, keep)]
 
 
+_frequencies = frequencies
+
+
 def ramp_amplitude(factor) -> float:
     """What the ramp's scaling multiplies cosines and sines by."""
     return 0.1 * math.log(factor) + 1.0
@@ -119,7 +122,7 @@ class RotaryPlan(_Plan):
                  amplitude=1.0, max_tokens=1 << 24, device="cuda"):
         rotary_dim = head_dim if rotary_dim is None else rotary_dim
         if frequencies is None:
-            frequencies = globals()["frequencies"](max(rotary_dim, 1), base)
+            frequencies = _frequencies(max(rotary_dim, 1), base)
         if len(frequencies) != rotary_dim // 2:
             raise ValueError(f"frequencies: one for each of {rotary_dim // 2} pairs expected, got {len(frequencies)}")
         if not amplitude > 0:

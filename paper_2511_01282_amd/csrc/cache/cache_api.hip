@@ -28,7 +28,9 @@ bool stride_ok(int64_t s, int es) { return s >= 0 && s < kMaxStride && s * es % 
 // A dispatch counts its threads in 32 bits (and its workgroups of the second and third dimension in 16).
 bool launchable(long long workgroups, int threads) { return workgroups >= 0 && workgroups < (1ll << 32) / threads; }
 
-// 2^64 times the fraction of a turn that w radians are.
+constexpr double kTurn = 6.283185307179586;  // 2 pi, rounded down
+// 2^64 times the fraction of a turn that w radians are, to 2^-63 of w and half a unit: under 2^-62, so that 2^31 positions further the
+// angle is within 2^-31 of a turn.
 uint64_t turns_of(double w) {
   const long double turns = fmodl((long double)w / (2 * 3.141592653589793238462643383279502884L), 1.0L);
   const long double scaled = roundl(ldexpl(turns, 64));
@@ -52,7 +54,7 @@ respec_status respec_rotary_create(const respec_rotary_shape* shape, const doubl
   if (s.layout != RESPEC_ROTARY_HALF && s.layout != RESPEC_ROTARY_INTERLEAVED) return RESPEC_ERR_PARAM;
   if (!(s.amplitude >= 0.f) || isinf(s.amplitude)) return RESPEC_ERR_PARAM;
   for (int i = 0; i < s.rotary_dim / 2; ++i)
-    if (!(frequency[i] >= 0.0) || isinf(frequency[i])) return RESPEC_ERR_PARAM;
+    if (!(frequency[i] >= 0.0) || frequency[i] > kTurn) return RESPEC_ERR_PARAM;
   respec_rotary_plan* p = new (std::nothrow) respec_rotary_plan();
   if (!p) return RESPEC_ERR_CAPACITY;
   p->s = s;

@@ -4,7 +4,7 @@
 // amplitude.  Every row is read and written once, and memory bounds it if the angles cost little:
 //
 // Angles.  w_i is held in turns per position, as a 64-bit fraction; p w_i mod 1 turn is then the low word of an integer
-// product, exact at any position, where a float's product would be off by p 2^-24.  Its upper 32 bits split into a quadrant and
+// product, within 2^-31 at any position, where a float's product would be off by p 2^-24.  Its upper 32 bits split into a quadrant and
 // a rest of at most an eighth of a turn either way, whose sine and cosine are Taylor's polynomials up to x^9 and x^10 (what is
 // left out is below 2^-25).
 //

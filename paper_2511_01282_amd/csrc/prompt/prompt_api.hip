@@ -110,9 +110,10 @@ Q8Scales device_scales(const respec_q8_cache& c) {
 }
 
 // How long an attention kernel takes over one cache row of a block, with all the workgroups of a CU that the pace was
-// taken with, and to start a workgroup (us).
+// taken with, to start a workgroup, and to launch the merge (us); and how much of the work that longest sequences would be a batch
+// is taken to be.
 struct Pace {
-  double row, start;
+  double row, start, merge = 4, share = 0.5;
 };
 
 // Splits of the sequences: the number n (of a coarser choice upwards; at most `held`, each of `least` cache rows or
@@ -124,7 +125,6 @@ struct Pace {
 // workgroup's true pace 13.1 us, with four workgroups' for any 13.9, where calls of a few rows were split in vain.
 ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long long limit, int unit, int least,
                    int per_cu, Pace pace, int row_bytes, long long held) {
-  constexpr double kShare = 0.5;
   ChunkGeom g{rows_per_wg, 1, INT_MAX, 0, fast_div(INT_MAX)};
   const long long items = blocks * b.n_kv_heads;
   double best = 0;
@@ -134,9 +134,9 @@ ChunkGeom geometry(const ChunkBatch& b, int rows_per_wg, long long blocks, long 
     if (rows == rows_before) continue;
     rows_before = rows;
     const double wgs = (double)items * ceil_div(limit, std::max(rows, 1ll)) / (kCUs * per_cu);
-    const double rounds = b.batch == 1 ? ceil(wgs) : std::max(1.0, wgs * kShare) + 0.5;
+    const double rounds = b.batch == 1 ? ceil(wgs) : std::max(1.0, wgs * pace.share) + 0.5;
     const double joined = 1e-6 * n * b.total_new * b.n_kv_heads * b.group * row_bytes * 2 / 4.5;
-    const double merge = n == 1 ? 0 : 4 + joined * (b.batch == 1 ? 1 : kShare);
+    const double merge = n == 1 ? 0 : pace.merge + joined * (b.batch == 1 ? 1 : pace.share);
     const double crowd = std::min(1.0, ceil(wgs * per_cu) / per_cu);  // workgroups of a CU, of the per_cu that set the pace
     const double t = rounds * (rows * pace.row * crowd + pace.start) + merge;
     if (n == 1 || t < best) {
@@ -235,13 +235,19 @@ respec_status attend(const respec_chunk_plan* plan, const respec_chunk_attn_args
     if (!launchable(a.wide.items + reports, kAttnF32Threads)) return RESPEC_ERR_SHAPE;
     e = launch_chunk_attn_f32(s.head_dim, q8 != nullptr, a, status, stm);
   } else {
-    // Calls of at most 64 query rows per KV head have the few-row kernel, of one or two groups of 32; others have
-    // 256-row blocks, and sequences of up to 32 rows among them the few-row kernel's way in the same launch.
+    // Calls of at most 64 query rows per KV head have the few-row kernel, of one or two groups of 32 (over an 8-bit cache: of one,
+    // two or four of 16); others have 256-row blocks, and sequences of up to 32 rows among them the few-row kernel's way in the same launch.
     const bool wide = rows > 64, mixed = wide && a.b.batch > 1;
     a.few_rows = !wide ? (q8 && rows <= 16 ? 16 : rows <= 32 ? 32 : 64) : mixed ? 32 : 0;
-    a.few = !wide || mixed ? geometry(a.b, a.few_rows, seqs, limit, 128, 128, 1,
-                                      s.head_dim == 128 ? Pace{0.02, 6} : Pace{0.01, 6}, rb, held)
-                           : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
+    // Few rows over an 8-bit cache: up to 32 rows, two workgroups to a CU, 33-64 rows one.  (25 batches of decoding tokens and short
+    // chunks, over the best of eleven splits each: 1.02 times its time, with the other cache's paces 1.08.)
+    if (q8 && !wide)
+      a.few = a.few_rows <= 32 ? geometry(a.b, a.few_rows, seqs, limit, 128, 512, 2, Pace{0.005, 4, 6, 0.4}, rb, held)
+                               : geometry(a.b, a.few_rows, seqs, limit, 128, 256, 1, Pace{0.0142, 5, 6, 0.4}, rb, held);
+    else
+      a.few = !wide || mixed ? geometry(a.b, a.few_rows, seqs, limit, 128, 128, 1,
+                                        s.head_dim == 128 ? Pace{0.02, 6} : Pace{0.01, 6}, rb, held)
+                             : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
     a.wide = wide ? geometry(a.b, 256, blocks(256), limit, 128, 256, 1, s.head_dim == 128 ? Pace{0.032, 6} : Pace{0.018, 6}, rb, held)
                   : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
     if (!launchable((long long)a.few.items + a.wide.items + reports, wide ? kAttnWideThreads : kAttnFewThreads)) return RESPEC_ERR_SHAPE;

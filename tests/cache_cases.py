@@ -1,6 +1,7 @@
 """The operators of include/respec_cache.h in 64 bits, and batches for them; everything is evaluated on the host."""
 import math
 from dataclasses import dataclass
+from fractions import Fraction
 
 import torch
 
@@ -15,18 +16,27 @@ NAN_CODE = 0x7F
 # rotary positions
 # ---------------------------------------------------------------------------
 
+_TURN = 2 * Fraction(31415926535897932384626433832795028841971693993751, 10 ** 49)
+
+
+def angle(p, w):
+    """p w, less whole turns: exact but for pi's 50 digits and the float."""
+    a = Fraction(p) * Fraction(w)
+    return float(a - round(a / _TURN) * _TURN)
+
+
 def rotary(x, pos, w, rotary_dim, half, amplitude=1.0):
     """(rows, tolerance) of x [T][H][D] at positions [T] (ints) for frequencies w (floats).
 
     With e = 2^-24 a cosine or sine is off by: its argument, at most pi / 4 and rounded twice, 1.57 e; three
-    roundings of its polynomial, 3 e; what the polynomial leaves out, e / 2; the angle itself, 2^-32 of a turn, under e / 10;
+    roundings of its polynomial, 3 e; what the polynomial leaves out, e / 2; the angle itself, 2^-31 of a turn, e / 20;
     the amplitude's product, e.  A product and the sum round by e each of their size.  In all under 2^-20 (16 e) of
     amplitude (|x_a| + |x_b|), and the result's rounding.
     """
     u = torch.finfo(x.dtype).eps / 2
     y = x.to(F64)
-    angle = torch.tensor([[math.remainder(p * f, 2 * math.pi) if p * f < 2 ** 52 else math.nan for f in w] for p in pos], dtype=F64)
-    c, s = angle.cos()[:, None] * amplitude, angle.sin()[:, None] * amplitude
+    turned = torch.tensor([[angle(p, f) for f in w] for p in pos], dtype=F64)
+    c, s = turned.cos()[:, None] * amplitude, turned.sin()[:, None] * amplitude
     r = rotary_dim
     a, b = (y[..., :r // 2], y[..., r // 2:r]) if half else (y[..., :r:2], y[..., 1:r:2])
     pair = (a * c - b * s, b * c + a * s)

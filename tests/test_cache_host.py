@@ -86,7 +86,7 @@ def _rotary(lib, w=None, **over):
     ({"n_kv_heads": 257}, SHAPE), ({"n_q_heads": 7}, OK), ({"layout": 2}, PARAM), ({"layout": 1}, OK), ({"max_tokens": 0}, SHAPE),
     ({"max_tokens": (1 << 24) + 1}, SHAPE), ({"amplitude": -1.0}, PARAM), ({"amplitude": math.inf}, PARAM),
     ({"amplitude": math.nan}, PARAM), ({"w": [-1.0]}, PARAM), ({"w": [math.nan]}, PARAM), ({"w": [math.inf]}, PARAM),
-    ({"w": [0.0]}, OK), ({"w": [1e9]}, OK),
+    ({"w": [0.0]}, OK), ({"w": [2 * math.pi]}, OK), ({"w": [6.2831853071795872]}, PARAM), ({"w": [1e9]}, PARAM),
 ])
 def test_rotary_create(lib, over, status):
     st, h = _rotary(lib, **over)

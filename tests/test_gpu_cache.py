@@ -640,6 +640,34 @@ def test_keep_rows_past_32_bits(lib):
     assert int((k != 0).sum()) == 2 * 8 * 128
 
 
+def test_captured_keep_replays(lib):
+    """Captured once, replayed on other caches' contents, lengths and paths (failed sequences among them), eager work in between."""
+    rng = random.Random(11)
+    nodes, page, batch = 20, 16, 5
+    shape = (3, 40, 2, page, 64)
+    k, v = (torch.zeros(shape, dtype=BF, device="cuda") for _ in range(2))
+    table = torch.arange(40, dtype=I32, device="cuda").view(batch, 8)
+    lens, path, acc, out, st = _ints([0] * batch), _ints([[0] * nodes] * batch), _ints([0] * batch), _ints([0] * batch), _ints([0] * batch)
+    layers = lib[2].CacheLayers(k, v)
+    layers.keep_rows(table, lens, path, acc, out, status=st)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layers.keep_rows(table, lens, path, acc, out, status=st)
+    for _ in range(4):
+        accs = [rng.choice([-1, 0, 5, nodes - 1, nodes]) for _ in range(batch)]   # (the last: one more than the path holds)
+        paths = [[0] + sorted(rng.sample(range(1, nodes), min(max(a, 0), nodes - 1))) for a in accs]
+        ls = [rng.randrange(8 * page - nodes) for _ in range(batch)]
+        for t, x in ((lens, ls), (acc, accs), (path, [p + [-1] * (nodes - len(p)) for p in paths])):
+            t.copy_(torch.tensor(x, dtype=I32))
+        kc, vc = k.normal_().cpu(), v.normal_().cpu()
+        graph.replay()
+        torch.cuda.synchronize()
+        kept = [p if 0 <= a < nodes else [] for p, a in zip(paths, accs)]
+        assert st.tolist() == [5 if a == nodes else 0 for a in accs] and out.tolist() == [l + len(p) for l, p in zip(ls, kept)]
+        assert torch.equal(k.cpu(), _kept(kc, ls, kept, table.tolist(), page)) and torch.equal(v.cpu(), _kept(vc, ls, kept, table.tolist(), page))
+
+
 def test_verification_then_kept_rows(lib):
     """Verification steps whose accepted rows are kept in the cache, and nothing else of their trees: the next step's attention is
     that over a cache of the accepted tokens alone."""

@@ -117,7 +117,9 @@ respec_status respec_rotary(const respec_rotary_plan* plan, const respec_rotary_
   memcpy(a.turns, plan->turns, sizeof a.turns);
   const int units = s.head_dim * es / 32;
   a.turned = s.rotary_dim * es / 32;
-  // Four heads to a thread where that still leaves each CU a workgroup or so; the angles are half of a thread's work otherwise.
+  // Four heads to a thread where that still leaves each CU a workgroup: the angles are half of a thread's work otherwise.  (32 + 8 heads
+  // of 128, bf16, one and four heads: 512 tokens 9.2 and 9.2 us, 2048 12.3 and 11.4, 4096 18.9 and 16.9, 8192 38.1 and 38.8; 28 + 4: 512
+  // 8.5 and 9.2, 4096 16.1 and 14.4.)
   const long long items = (long long)a.tokens * a.heads * units;
   const int r = items >= 4ll * kRotaryThreads * 256 ? 4 : 1;
   a.stride = fast_div((uint32_t)ceil_div(a.heads, r));

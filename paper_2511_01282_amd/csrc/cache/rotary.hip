@@ -11,6 +11,9 @@
 // A unit of work is 32 bytes of a row that hold 16 / (bytes per element) whole pairs: two 16-byte pieces, rotary_dim / 2
 // columns apart (half) or side by side (interleaved).  A thread takes one unit's place in up to R heads of one token, so the
 // angles are taken once for R units, while the loads of these are under way.
+//
+// 8192 tokens of 32 + 8 heads of 128, bf16 (168 MB): 34 to 37 us, 4.5 to 4.9 TB/s, as a large copy; the vector instructions stand
+// behind it.  65 nodes of 28 + 4 heads: 4.2 us, which is a launch.
 #include "cache.hpp"
 
 namespace respec {

@@ -31,63 +31,6 @@ struct FewShape {
   static_assert(kLds <= 163840, "LDS of a CU");
 };
 
-// O = sum_w 2^(m_w - M) O_w, l likewise: each of the four waves writes its own to LDS (its `WAVE` bytes), joins a quarter of the
-// columns and stores them.  ml: 4 * 64 float2 of LDS.
-template <int D, int GR, int WAVE>
-__device__ __forceinline__ void join_waves(const ChunkAttnArgs& a, Rows<D> (&r)[GR], unsigned char* smem, float2* ml, bool whole,
-                                           int split, const int64_t (&tok)[GR], const int64_t (&head)[GR], int rows, int wave,
-                                           int lane) {
-  constexpr int DB = D / 32;
-  static_assert(D * 64 * 2 <= WAVE, "a wave's O");
-  const int r32 = lane & 31, hi = lane >> 5;
-#pragma unroll
-  for (int g = 0; g < GR; ++g) {
-    if (g > 0) __syncthreads();
-    f32x4* to = reinterpret_cast<f32x4*>(smem + wave * WAVE) + lane;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        to[(db * 4 + q) * 64] = f32x4{r[g].o[db][4 * q], r[g].o[db][4 * q + 1], r[g].o[db][4 * q + 2], r[g].o[db][4 * q + 3]};
-    ml[wave * 64 + lane] = make_float2(r[g].m, r[g].l);
-    __syncthreads();
-    float M = kNoRef, w[4], l = 0.f;
-#pragma unroll
-    for (int w_ = 0; w_ < 4; ++w_) M = fmaxf(M, ml[w_ * 64 + lane].x);
-#pragma unroll
-    for (int w_ = 0; w_ < 4; ++w_) {
-      w[w_] = __builtin_amdgcn_exp2f(ml[w_ * 64 + lane].x - M);
-      l += w[w_] * ml[w_ * 64 + lane].y;
-    }
-    l += xchg<5>(l);
-    const bool mine = g * 32 + r32 < rows;
-    const int64_t pr = ((int64_t)split * a.b.total_new + tok[g]) * ((int64_t)a.b.n_kv_heads * a.b.group) + head[g];
-    const float inv = 1.f / l;
-#pragma unroll
-    for (int c = 0; c < DB; ++c) {  // (4 DB blocks of 8 columns, DB per wave)
-      const int blk = wave * DB + c;
-      f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w_ = 0; w_ < 4; ++w_) v += (reinterpret_cast<const f32x4*>(smem + w_ * WAVE) + lane)[blk * 64] * w[w_];
-      const int col = 32 * (blk / 4) + 8 * (blk % 4) + 4 * hi;
-      if (!mine) continue;
-      if (whole) {
-        u32x2 y;
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * e] * inv, v[2 * e + 1] * inv}, bf16x2));
-        *reinterpret_cast<u32x2*>(a.out + tok[g] * a.o_tok + head[g] * a.o_head + col * 2) = y;
-      } else {
-        *reinterpret_cast<f32x4*>(a.part_o + pr * D + col) = v;
-      }
-    }
-    if (!whole && mine && wave == 0 && hi == 0) {
-      a.part_m[pr] = M;
-      a.part_l[pr] = l;
-    }
-  }
-}
-
 // Item x, by four waves (256 threads); GR groups of 32 query rows.  LEAN, for waves of at most 256 registers: what depends
 // on the lane alone is worked out in every tile (`at`); held along, as the compiler would have it, it spills.
 template <int D, int GR, bool LEAN>
@@ -208,7 +151,54 @@ __device__ __forceinline__ void few_rows_item(const ChunkAttnArgs& a, int x, uns
     if (produced < my_nt) produce();
   }
 
-  join_waves<D, GR, G::kWave>(a, r, smem, reinterpret_cast<float2*>(smem + G::kMl), whole, it.split, tok, head, rows, wave, lane);
+  // ---- O = sum_w 2^(m_w - M) O_w, l likewise: every wave writes its own, and joins a quarter of the columns ----
+  float2* ml = reinterpret_cast<float2*>(smem + G::kMl);
+#pragma unroll
+  for (int g = 0; g < GR; ++g) {
+    if (g > 0) __syncthreads();
+    f32x4* to = reinterpret_cast<f32x4*>(smem + wave * G::kWave) + lane;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        to[(db * 4 + q) * 64] = f32x4{r[g].o[db][4 * q], r[g].o[db][4 * q + 1], r[g].o[db][4 * q + 2], r[g].o[db][4 * q + 3]};
+    ml[wave * 64 + lane] = make_float2(r[g].m, r[g].l);
+    __syncthreads();
+    float M = kNoRef, w[4], l = 0.f;
+#pragma unroll
+    for (int w_ = 0; w_ < 4; ++w_) M = fmaxf(M, ml[w_ * 64 + lane].x);
+#pragma unroll
+    for (int w_ = 0; w_ < 4; ++w_) {
+      w[w_] = __builtin_amdgcn_exp2f(ml[w_ * 64 + lane].x - M);
+      l += w[w_] * ml[w_ * 64 + lane].y;
+    }
+    l += xchg<5>(l);
+    const bool mine = g * 32 + r32 < rows;
+    const int64_t pr = ((int64_t)it.split * a.b.total_new + tok[g]) * ((int64_t)a.b.n_kv_heads * a.b.group) + head[g];
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int c = 0; c < DB; ++c) {  // (4 DB blocks of 8 columns, DB per wave)
+      const int blk = wave * DB + c;
+      f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w_ = 0; w_ < 4; ++w_) v += (reinterpret_cast<const f32x4*>(smem + w_ * G::kWave) + lane)[blk * 64] * w[w_];
+      const int col = 32 * (blk / 4) + 8 * (blk % 4) + 4 * hi;
+      if (!mine) continue;
+      if (whole) {
+        u32x2 y;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * e] * inv, v[2 * e + 1] * inv}, bf16x2));
+        *reinterpret_cast<u32x2*>(a.out + tok[g] * a.o_tok + head[g] * a.o_head + col * 2) = y;
+      } else {
+        *reinterpret_cast<f32x4*>(a.part_o + pr * D + col) = v;
+      }
+    }
+    if (!whole && mine && wave == 0 && hi == 0) {
+      a.part_m[pr] = M;
+      a.part_l[pr] = l;
+    }
+  }
 }
 
 }  // namespace respec

@@ -1,9 +1,9 @@
 // Causal attention of long chunks over a paged cache, bf16: 256 query rows per workgroup.
 //
 // Eight waves, two per SIMD, own 32 query rows each and walk over the same cache rows, tile by tile of 32.
-// Tiles go round an LDS ring by DMA, four of them per pass and barrier.
+// Tiles go round an LDS ring by DMA (or, of an 8-bit cache, through registers), four of them per pass and barrier.
 //
-// 8192 tokens, 32 heads of 128 (0.55 TFLOP): 511 to 556 us with the card's temperature, 0.99 to 1.08 PFLOP/s, where a large
+// Over a bf16 cache, 8192 tokens, 32 heads of 128 (0.55 TFLOP): 511 to 556 us with the card's temperature, 0.99 to 1.08 PFLOP/s, where a large
 // bf16 matrix product reaches 1.22.  The matrix cores are busy half of the cycles, at 1.96 GHz; matrix and vector
 // instructions of a SIMD's two waves hardly overlap (512 and some 480 cycles of the 1010 that a wave's tile takes), and the
 // waves wait 30% of their time.  Part of that is the queries': they are first used inside the loops, so the compiler counts
@@ -44,7 +44,10 @@ struct WideShape {
 // Q8: the cache holds e4m3 values with a scale per block.  A wave brings its rows of a pass, 16 that share a page and a
 // scale, through registers, and they become bf16, which holds them exactly, on the way into LDS.  So each value is converted
 // once for all 256 rows, and what follows is the same.  K is on its way during the first half of a pass and V during the
-// second, for want of registers (both during all of it spilled 76 and took 561 us for 512 tokens over 16384 rows, 32 heads on 8).
+// second, for want of registers: both during all of it spilled 76, and 512 tokens over 16384 rows, 32 heads on 8 of 128, took 561 us.
+// Like this 140 to 150 (0.93 to 1.0 PFLOP/s), and 10 for the merge; 8192 tokens, 32 heads, 540 to 562 us, as over the bf16 cache.
+// V's writes meet banks twice, 17% of the LDS cycles.  The queries waited for ahead of the loops: no change (562 us of
+// 8192 tokens).  Waves at a higher priority in their products: 160 instead of 155 us (512 tokens).
 template <int D, bool Q8>
 __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, unsigned char* smem) {
   using G = WideShape<D, Q8>;

@@ -240,7 +240,9 @@ respec_status attend(const respec_chunk_plan* plan, const respec_chunk_attn_args
     const bool wide = rows > 64, mixed = wide && a.b.batch > 1;
     a.few_rows = !wide ? (q8 && rows <= 16 ? 16 : rows <= 32 ? 32 : 64) : mixed ? 32 : 0;
     // Few rows over an 8-bit cache: up to 32 rows, two workgroups to a CU, 33-64 rows one.  (25 batches of decoding tokens and short
-    // chunks, over the best of eleven splits each: 1.02 times its time, with the other cache's paces 1.08.)
+    // chunks, over the best of eleven splits each: 1.02 times its time, with the other cache's paces 1.08; 13 more with heads of
+    // 64: 1.04.)  Long chunks have the other cache's paces (44 calls, over the best of thirteen splits each: 1.04; paces fitted to
+    // these calls 1.03).
     if (q8 && !wide)
       a.few = a.few_rows <= 32 ? geometry(a.b, a.few_rows, seqs, limit, 128, 512, 2, Pace{0.005, 4, 6, 0.4}, rb, held)
                                : geometry(a.b, a.few_rows, seqs, limit, 128, 256, 1, Pace{0.0142, 5, 6, 0.4}, rb, held);

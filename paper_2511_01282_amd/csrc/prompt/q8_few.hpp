@@ -2,7 +2,21 @@
 //
 // As chunk_few.hpp's: four waves own all the query rows and every fourth tile of 32 cache rows each, with rings of their own
 // in LDS, filled by DMA as the codes lie in memory.  The codes become bf16, exactly, on the way from LDS into the products'
-// operands.
+// operands.  The cache's bytes bound it, if the matrix and vector work on them hides behind their arrival:
+//
+// * Groups of 16 query rows: a conversion costs the same for any number of rows, products and softmax less the fewer
+//   rows there are (32 tokens over 300-16000 rows, 32 heads on 8 of 128: groups of 32 136 us, of 16 74 then).
+// * Two workgroups to a CU with two slots of 32 rows per wave: three with slots of half a tile 86 us, one with four slots 83,
+//   two 73.  Slots given back between K's and V's products: 81.  Heads of 64 columns with four slots: 64 tokens over 200-3000 rows
+//   23.8 us, with two, and so up to four workgroups to a CU, 22.0.
+// * Pages and scales of 64 tiles are looked up at once, a lane each; keys behind the sequence's end are cleared
+//   before they are converted, so that what a reused page holds there never takes the slow way of values that are not finite
+//   (40 us for such a tile).  With both, 60 us.
+// * Sequences' lines of tiles dealt evenly over the workgroups: 62 us.  The longest splits first: 61, and 64 tokens over 200-3000 rows 38
+//   instead of 33.
+//
+// The 32 tokens: 268 MB in 53 to 56 us (4.8 to 5.1 TB/s; batches of equal lengths 5.2 to 5.4), and 5 for the merge.  One token
+// over 32767 rows, 28 heads on 4: 33.6 MB in 10.1 to 11.5 us.
 #pragma once
 
 #include "q8_tile.hpp"
@@ -13,7 +27,7 @@ constexpr int kQ8Tile = 32;
 
 template <int D>
 struct Q8FewShape {
-  static constexpr int S = D == 128 ? 2 : 4;  // ring slots of a wave
+  static constexpr int S = 2;                 // ring slots of a wave
   static constexpr int kHalf = kQ8Tile * D;   // bytes of a K or V tile
   static constexpr int kSlot = 2 * kHalf;
   static constexpr int kWave = S * kSlot;
@@ -23,12 +37,10 @@ struct Q8FewShape {
   static_assert(kLds <= 163840 / 2 - 1024, "two workgroups to a CU");
 };
 
-// Waits until at most n tiles of R requests each are under way, n < S.
-template <int R, int S>
+// Waits until at most n tiles of R requests each are under way, n < 2.
+template <int R>
 __device__ __forceinline__ void wait_tiles(int n) {
-  if (S > 3 && n == 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * R) : "memory");
-  else if (S > 2 && n == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * R) : "memory");
-  else if (S > 1 && n == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R) : "memory");
+  if (n == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R) : "memory");
   else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
@@ -38,7 +50,7 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
   using G = Q8FewShape<D>;
   constexpr int KS = D / 32, CB = D / 16, S = G::S;
   constexpr int NR = D / 64, RPI = 1024 / D, CPR = D / 16;  // requests of 16 rows, rows of a request, chunks of a row
-  static_assert(S <= 4, "wait_tiles()");
+  static_assert(S == 2, "wait_tiles()");
   const ChunkGeom& ge = a.few;
   const Item it = find_item(a.b, ge, 1, a.few_rows, x);
   const ChunkSeq& sq = it.seq;
@@ -130,7 +142,7 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
 
 #pragma unroll 1
   for (int j = 0; j < my_nt; ++j) {
-    wait_tiles<4 * NR, S>(produced - 1 - j);
+    wait_tiles<4 * NR>(produced - 1 - j);
     const unsigned char* t = ring + (j % S) * G::kSlot;
     const int key0 = lo + (j * 4 + wave) * kQ8Tile;
     const uint32_t word = (uint32_t)__builtin_amdgcn_readlane((int)(j & 64 ? scales[1] : scales[0]), j & 63);

@@ -3,17 +3,14 @@
 // Eight waves, two per SIMD, own 32 query rows each and walk over the same cache rows, tile by tile of 32.
 // Tiles go round an LDS ring by DMA (or, of an 8-bit cache, through registers), four of them per pass and barrier.
 //
-// Over a bf16 cache, 8192 tokens, 32 heads of 128 (0.55 TFLOP): 511 to 556 us with the card's temperature, 0.99 to 1.08 PFLOP/s, where a large
-// bf16 matrix product reaches 1.22.  The matrix cores are busy half of the cycles, at 1.96 GHz; matrix and vector
-// instructions of a SIMD's two waves hardly overlap (512 and some 480 cycles of the 1010 that a wave's tile takes), and the
-// waves wait 30% of their time.  Part of that is the queries': they are first used inside the loops, so the compiler counts
-// their loads as under way at each loop's head and waits for them there.  It does not know of the DMA, and these waits
-// (vmcnt(7) .. vmcnt(0) before the first score products of a pass, and of every masked tile) are for the unit just
-// requested as well: it lands beside that tile, not beside the whole pass.
-// With those waits in place: four waves of 64 rows, with the tiles' fragments read half as often, took a tenth more clocks and
-// the same time (537 to 545 us, the clock at 2.2 GHz), and chunks 3-5% longer; two tiles per pass and three passes requested
-// ahead at D = 128, 558 against 546 us.
-// 512 tokens over 16384 rows, 32 heads on 8: 134 to 150 us and 10 us for the merge of the splits.
+// Over a bf16 cache, 8192 tokens, 32 heads of 128 (0.55 TFLOP): 511 to 556 us with the card's temperature, 0.99 to 1.08
+// PFLOP/s, where a large bf16 matrix product reaches 1.22.  The matrix cores are busy half of the cycles, at 1.96 GHz; matrix
+// and vector instructions of a SIMD's two waves hardly overlap (512 and some 480 cycles of the 1010 that a wave's tile takes),
+// and the waves wait 30% of their time.  (Forms that leave one kind of work out, the weights' exponentials or the tiles' reads, took
+// 9 to 14% less each; none of them bounds it alone.)  Four waves of 64 rows, with the tiles' fragments read half as often, took
+// a tenth more clocks and the same time (537 to 545 us, the clock at 2.2 GHz), and chunks 3-5% longer; two tiles per pass and
+// three passes requested ahead at D = 128, 558 against 546 us.
+// 512 tokens over 16384 rows, 32 heads on 8: 134 to 150 us, and 10 us for the merge of the splits.
 #pragma once
 
 #include <type_traits>
@@ -43,11 +40,11 @@ struct WideShape {
 
 // Q8: the cache holds e4m3 values with a scale per block.  A wave brings its rows of a pass, 16 that share a page and a
 // scale, through registers, and they become bf16, which holds them exactly, on the way into LDS.  So each value is converted
-// once for all 256 rows, and what follows is the same.  K is on its way during the first half of a pass and V during the
+// once for all 256 rows, and what follows is the same.  D = 128: K is on its way during the first half of a pass and V during the
 // second, for want of registers: both during all of it spilled 76, and 512 tokens over 16384 rows, 32 heads on 8 of 128, took 561 us.
-// Like this 140 to 150 (0.93 to 1.0 PFLOP/s), and 10 for the merge; 8192 tokens, 32 heads, 540 to 562 us, as over the bf16 cache.
-// V's writes meet banks twice, 17% of the LDS cycles.  The queries waited for ahead of the loops: no change (562 us of
-// 8192 tokens).  Waves at a higher priority in their products: 160 instead of 155 us (512 tokens).
+// Like this 148 to 158 with the card's temperature, the merge's 10 among them; 8192 tokens, 32 heads, 540 to 562 us, as over the bf16 cache.
+// V's writes meet banks twice, 17% of the LDS cycles.  Waves at a higher priority in their products: 160 instead of 155 us
+// (512 tokens).  Values left as they are in LDS after the first passes, which is wrong, 138 of 152: what the conversion costs.
 template <int D, bool Q8>
 __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, unsigned char* smem) {
   using G = WideShape<D, Q8>;
@@ -98,8 +95,10 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
   int unit = -1;
   // (Q8: a wave's window of 64 units, a lane for each; the unit that is on its way)
   static_assert(!Q8 || kRows == 16, "16 rows share a page and a scale");
+  constexpr bool kBoth = D == 64;  // K and V are requested together
   Q8Window window;
-  Q8Rows<D> q8;
+  Q8Rows<D> q8[kBoth ? 2 : 1];
+  auto &k8 = q8[0], &v8 = q8[kBoth];
   int coming = -1, entry = 0;  // its first tile (none: -1), its lane of the window
   int64_t q8_off = 0;
   const uint32_t q8_from = Q8Rows<D>::from(a.b.row_stride, lane), q8_k = Q8Rows<D>::template to<true>(lane), q8_v = Q8Rows<D>::template to<false>(lane);
@@ -112,18 +111,19 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
     if (t < 0) return;
     coming = t;
     q8_off = offset_in(a.b, __builtin_amdgcn_readlane(window.id, entry), (uint32_t)t0) + (int64_t)it.g * a.b.head_stride;
-    q8.fetch(a.b.k + q8_off, a.b.row_stride, q8_from);
+    k8.fetch(a.b.k + q8_off, a.b.row_stride, q8_from);
+    if constexpr (kBoth) v8.fetch(a.b.v + q8_off, a.b.row_stride, q8_from);
   };
   auto q8_middle = [&]() __attribute__((always_inline)) {  // ... is in LDS, V is requested
     if (coming < 0) return;
-    q8.template to_lds<true>(smem + (coming % S) * G::kSlot, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.k, entry)), q8_k);
-    q8.fetch(a.b.v + q8_off, a.b.row_stride, q8_from);
+    k8.template to_lds<true>(smem + (coming % S) * G::kSlot, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.k, entry)), q8_k);
+    if constexpr (!kBoth) v8.fetch(a.b.v + q8_off, a.b.row_stride, q8_from);
   };
   auto q8_end = [&]() __attribute__((always_inline)) {
     if (coming < 0) return;
     const int valid = hi_row - (lo + coming * kWideTile + w_row);  // rows that some token sees
-    if (valid < kRows) q8.clear_from(valid, lane);
-    q8.template to_lds<false>(smem + (coming % S) * G::kSlot + G::kHalf, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.v, entry)), q8_v);
+    if (valid < kRows) v8.clear_from(valid, lane);
+    v8.template to_lds<false>(smem + (coming % S) * G::kSlot + G::kHalf, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.v, entry)), q8_v);
   };
   auto request = [&]() __attribute__((always_inline)) {
     const int u = unit++, t = kPass * u + 1 + w_tile, t0 = lo + t * kWideTile + w_row;
@@ -155,6 +155,10 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
   static_assert(G::kAhead <= 3, "landed() tells two newer units apart");
+  // The queries have arrived here: first used inside the loops, they would be waited for at each loop's head, and with them the
+  // unit just requested, of which the compiler does not know (8192 tokens, bf16 cache: 543 us; like this 533).
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
 #pragma unroll 1
   for (int u = -1; u < G::kAhead; ++u) {
     request();
@@ -182,12 +186,23 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
     for (int ks = 0; ks < KS; ++ks) s[0] = mma32(kf[ks], qf[ks], s[0]);
     mask_scores(s[0], lo, end[0], lane);
   }
-  // Tile t, whose scores are s[t % 2]: the next tile's scores, this one's weights, O += V^T P.
+  auto take_in = [&]() __attribute__((always_inline)) {  // O += V^T P
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) r[0].o[db] = mma32(vf[db][k2], p[k2], r[0].o[db]);
+  };
+  // Tile t, whose scores are s[t % 2]: the next tile's scores, this one's weights, O += V^T P.  Where no row is masked, O is that
+  // of the tile before: its products, and the next tile's scores', then stand between two of settle()'s branches with nothing
+  // that they wait for (16384 rows, 512 tokens, 32 heads on 8 of 64: 100.5 and, like this, 97.2 us; bf16 94.5 and 92.5; of 128
+  // 152 and 152, bf16 148.5 and 147).  Orders of products and vector instructions that were asked for one by one took up
+  // to 4% more at 64 columns and up to 1% less at 128.
   auto tile = [&](auto masked_c, auto u_c, int t) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked_c)::value;
     constexpr int U = decltype(u_c)::value;
     const unsigned char* v_tile = slot(t) + G::kHalf;
     const int key0 = lo + t * kWideTile;
+    if constexpr (!MASKED) take_in();
     read_k<D>(slot(t + 1), lane, kf);
     s[1 - U] = f32x16{};
 #pragma unroll
@@ -197,11 +212,8 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
     if constexpr (MASKED) odd = take_out_not_finite<D>(vf);
     const float sum = weights(s[U], a.scale_log2, r[0].m, p);
     settle(r[0], s[U], a.scale_log2, p, sum);
-#pragma unroll
-    for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-      for (int db = 0; db < DB; ++db) r[0].o[db] = mma32(vf[db][k2], p[k2], r[0].o[db]);
     if constexpr (MASKED) {
+      take_in();
       if (odd) add_not_finite<D, 1>(r, v_tile, key0, end, lane);
       mask_scores(s[1 - U], key0 + kWideTile, end[0], lane);
     }
@@ -219,12 +231,16 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
   };
   // (every wave passes np barriers; a tile takes the next one's scores, too)
   int j = 0;
+  p[0] = p[1] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int db = 0; db < DB; ++db) vf[db][0] = vf[db][1] = p[0];
 #pragma unroll 1
   for (; kPass * j + kPass + 1 <= unmasked; ++j) {
     if (j > 0) landed(j);
     request();
     pass(std::integral_constant<bool, false>{}, j);
   }
+  if (j > 0) take_in();
 #pragma unroll 1
   for (; j < np; ++j) {
     if (j > 0) landed(j);

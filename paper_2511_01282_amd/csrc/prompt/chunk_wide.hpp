@@ -93,6 +93,11 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
   // units that this wave requests something of end here (it asks for rows of the last tile, no further ones)
   const int n_units = ((hi_row - lo + kWideTile - 1) / kWideTile - 1 - w_tile + kPass - 1) / kPass;
   int unit = -1;
+  // Offset of the ring slot that this wave's rows of the next unit go into, and of the one that they went into last.  (Slots are
+  // counted on, not divided for, and a unit's place is looked up with its page: scalar instructions stand in a wave's line with the
+  // others.  12 chunks of 1-700 tokens over 33-9000 rows, 8-bit cache, 64 columns: 61 and, so, 58 us; 2 prompts of 3000 tokens 116.5
+  // and 110, bf16 105 and 102.7.)
+  int into_next = (S + 1 - kPass + w_tile) % S * G::kSlot, into = 0;
   // (Q8: a wave's window of 64 units, a lane for each; the unit that is on its way)
   static_assert(!Q8 || kRows == 16, "16 rows share a page and a scale");
   constexpr bool kBoth = D == 64;  // K and V are requested together
@@ -100,39 +105,41 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
   Q8Rows<D> q8[kBoth ? 2 : 1];
   auto &k8 = q8[0], &v8 = q8[kBoth];
   int coming = -1, entry = 0;  // its first tile (none: -1), its lane of the window
-  int64_t q8_off = 0;
+  uint64_t q8_off = 0;
   const uint32_t q8_from = Q8Rows<D>::from(a.b.row_stride, lane), q8_k = Q8Rows<D>::template to<true>(lane), q8_v = Q8Rows<D>::template to<false>(lane);
   auto q8_begin = [&](int u) __attribute__((always_inline)) {  // K of unit u is requested
-    const int t = kPass * u + 1 + w_tile, t0 = min(lo + t * kWideTile + w_row, (hi_row - 1) & ~15);
+    const int t = kPass * u + 1 + w_tile;
     coming = -1;
     if (u >= n_units) return;
     entry = (u + 1) & 63;
     if (entry == 0) window.fill(a, it, lo + (kPass * (u + lane) + 1 + w_tile) * kWideTile + w_row, hi_row);
     if (t < 0) return;
     coming = t;
-    q8_off = offset_in(a.b, __builtin_amdgcn_readlane(window.id, entry), (uint32_t)t0) + (int64_t)it.g * a.b.head_stride;
+    q8_off = window.offset(entry) + (uint64_t)((int64_t)it.g * a.b.head_stride);
     k8.fetch(a.b.k + q8_off, a.b.row_stride, q8_from);
     if constexpr (kBoth) v8.fetch(a.b.v + q8_off, a.b.row_stride, q8_from);
   };
   auto q8_middle = [&]() __attribute__((always_inline)) {  // ... is in LDS, V is requested
     if (coming < 0) return;
-    k8.template to_lds<true>(smem + (coming % S) * G::kSlot, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.k, entry)), q8_k);
+    k8.template to_lds<true>(smem + into, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.scales, entry) & 0xFF), q8_k);
     if constexpr (!kBoth) v8.fetch(a.b.v + q8_off, a.b.row_stride, q8_from);
   };
   auto q8_end = [&]() __attribute__((always_inline)) {
     if (coming < 0) return;
     const int valid = hi_row - (lo + coming * kWideTile + w_row);  // rows that some token sees
     if (valid < kRows) v8.clear_from(valid, lane);
-    v8.template to_lds<false>(smem + (coming % S) * G::kSlot + G::kHalf, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.v, entry)), q8_v);
+    v8.template to_lds<false>(smem + into + G::kHalf, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.scales, entry) >> 16), q8_v);
   };
   auto request = [&]() __attribute__((always_inline)) {
     const int u = unit++, t = kPass * u + 1 + w_tile, t0 = lo + t * kWideTile + w_row;
+    into = into_next;
+    into_next += kPass * G::kSlot - (into_next >= (S - kPass) * G::kSlot ? S * G::kSlot : 0);
     if constexpr (Q8) {
       q8_begin(u);
       return;
     }
     if (t < 0 || u >= n_units) return;
-    const uint32_t dst = lds0 + (uint32_t)((t % S) * G::kSlot + w_row * D * 2);
+    const uint32_t dst = lds0 + (uint32_t)(into + w_row * D * 2);
     const uint32_t pa = div_by((uint32_t)min(t0, hi_row - 1), a.b.page);
     ids.need(pa, div_by((uint32_t)min(t0 + kRows - 1, hi_row - 1), a.b.page), lane);
     if (in_page && t0 + kRows <= hi_row)
@@ -172,15 +179,10 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
   r[0].init();
   f32x16 s[2];
   u32x4 p[2], kf[KS], vf[DB][2];
-  // (Q8: a slot's place as a number of its own.  As part of every fragment's address, kept up to date per fragment, it spills.)
-  auto slot = [&](int t) __attribute__((always_inline)) {
-    int at = (t % S) * G::kSlot;
-    if constexpr (Q8) asm("" : "+s"(at));
-    return smem + at;
-  };
+  int slot = 0;  // offset of the slot of the tile at hand
   landed(0);
   if (my_tiles > 0) {
-    read_k<D>(slot(0), lane, kf);
+    read_k<D>(smem, lane, kf);
     s[0] = f32x16{};
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) s[0] = mma32(kf[ks], qf[ks], s[0]);
@@ -200,10 +202,11 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
   auto tile = [&](auto masked_c, auto u_c, int t) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked_c)::value;
     constexpr int U = decltype(u_c)::value;
-    const unsigned char* v_tile = slot(t) + G::kHalf;
+    const unsigned char* v_tile = smem + slot + G::kHalf;
+    slot = slot == (S - 1) * G::kSlot ? 0 : slot + G::kSlot;
     const int key0 = lo + t * kWideTile;
     if constexpr (!MASKED) take_in();
-    read_k<D>(slot(t + 1), lane, kf);
+    read_k<D>(smem + slot, lane, kf);
     s[1 - U] = f32x16{};
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) s[1 - U] = mma32(kf[ks], qf[ks], s[1 - U]);

@@ -88,8 +88,8 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
   const int unmasked = min(sq.L + 1, hi_row);  // rows that every query row sees
 
   // ---- tiles: pages and scales of 64 of the wave's at a time, a lane for each; DMA of their rows, 16 at a time ----
-  const char* kb = a.b.k + (int64_t)it.g * a.b.head_stride;
-  const char* vb = a.b.v + (int64_t)it.g * a.b.head_stride;
+  const char* kb = a.b.k + (int64_t)it.g * a.b.head_stride - 1024 * (NR - 1);
+  const char* vb = a.b.v + (int64_t)it.g * a.b.head_stride - 1024 * (NR - 1);
   uint32_t k_off[NR], v_off[2][NR];
 #pragma unroll
   for (int q = 0; q < NR; ++q) {
@@ -99,20 +99,12 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
 #pragma unroll
     for (int h = 0; h < 2; ++h) v_off[h][q] = row + (uint32_t)((pos ^ v8_chunk<D>(16 * h + rr)) * 16);
   }
-  uint32_t at_lo[2], at_hi[2];    // where a half's rows lie in this head of the cache (64 bits, for dma_rows)
+  Q8Window window[2];             // of a tile's halves
   uint32_t scales[2] = {0u, 0u};  // of 64 tiles each, by turns: bytes K, K, V, V of a tile's two halves
   auto fill = [&](int base) {
-    uint32_t bytes = 0;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      Q8Window w;
-      const int r0 = lo + ((base + lane) * 4 + wave) * kQ8Tile + h * 16;
-      w.fill(a, it, r0, hi_row);
-      const uint64_t off = (uint64_t)(offset_in(a.b, w.id, (uint32_t)min(r0, (hi_row - 1) & ~15)) - 1024 * (NR - 1));
-      at_lo[h] = (uint32_t)off;
-      at_hi[h] = (uint32_t)(off >> 32);
-      bytes |= (w.k | w.v << 16) << (8 * h);
-    }
+    for (int h = 0; h < 2; ++h) window[h].fill(a, it, lo + ((base + lane) * 4 + wave) * kQ8Tile + h * 16, hi_row);
+    const uint32_t bytes = window[0].scales | window[1].scales << 8;
     if (base & 64) scales[1] = bytes;
     else scales[0] = bytes;
   };
@@ -122,8 +114,7 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
     const uint32_t dst = lds0 + (uint32_t)((produced % S) * G::kSlot);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int i = produced & 63;
-      const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_hi[h], i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)at_lo[h], i);
+      const uint64_t off = window[h].offset(produced & 63);
       const uint32_t to = dst + (uint32_t)(h * 16 * D);
       dma_rows<NR>(to, (uint64_t)(kb + off), k_off);
       dma_rows<NR>(to + G::kHalf, (uint64_t)(vb + off), v_off[h]);

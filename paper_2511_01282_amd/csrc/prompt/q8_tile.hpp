@@ -13,17 +13,22 @@ namespace respec {
 
 __device__ __forceinline__ float q8_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// Page ids and scales of 16 rows each, a lane for each: rows r0 .. r0 + 15 of the sequence (r0 a multiple of 16, from the
+// Places and scales of 16 rows each, a lane for each: rows r0 .. r0 + 15 of the sequence (r0 a multiple of 16, from the
 // sequence's end on its last 16 instead).
 struct Q8Window {
-  int32_t id;
-  uint32_t k, v;  // exponent bytes
+  uint32_t lo, hi;  // offset of the rows in a KV head of the cache (64 bits)
+  uint32_t scales;  // exponent bytes: K's, and from bit 16 on V's
   __device__ __forceinline__ void fill(const ChunkAttnArgs& a, const Item& it, int r0, int hi_row) {
     const uint32_t r = (uint32_t)max(0, min(r0, (hi_row - 1) & ~15));
-    id = a.b.table[(int64_t)it.b * a.b.table_stride + div_by(r, a.b.page)];
+    const int32_t id = a.b.table[(int64_t)it.b * a.b.table_stride + div_by(r, a.b.page)];
     const int64_t at = scale_offset(a, id, r, it.g);
-    k = a.q8.k[at];
-    v = a.q8.v[at];
+    scales = a.q8.k[at] | (uint32_t)a.q8.v[at] << 16;
+    const uint64_t off = (uint64_t)offset_in(a.b, id, r);
+    lo = (uint32_t)off;
+    hi = (uint32_t)(off >> 32);
+  }
+  __device__ __forceinline__ uint64_t offset(int l) const {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)lo, l);
   }
 };
 

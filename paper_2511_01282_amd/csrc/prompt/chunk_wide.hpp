@@ -40,7 +40,8 @@ struct WideShape {
 
 // Q8: the cache holds e4m3 values with a scale per block.  A wave brings its rows of a pass, 16 that share a page and a
 // scale, through registers, and they become bf16, which holds them exactly, on the way into LDS.  So each value is converted
-// once for all 256 rows, and what follows is the same.  D = 128: K is on its way during the first half of a pass and V during the
+// once for all 256 rows, and what follows is the same.  At 64 columns both are on their way during a whole pass (K written in its
+// middle: 1% more).  At 128 K is on its way during the first half of a pass and V during the
 // second, for want of registers: both during all of it spilled 76, and 512 tokens over 16384 rows, 32 heads on 8 of 128, took 561 us.
 // Like this 148 to 158 with the card's temperature, the merge's 10 among them; 8192 tokens, 32 heads, 540 to 562 us, as over the bf16 cache.
 // V's writes meet banks twice, 17% of the LDS cycles.  Waves at a higher priority in their products: 160 instead of 155 us
@@ -100,14 +101,14 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
   int into_next = (S + 1 - kPass + w_tile) % S * G::kSlot, into = 0;
   // (Q8: a wave's window of 64 units, a lane for each; the unit that is on its way)
   static_assert(!Q8 || kRows == 16, "16 rows share a page and a scale");
-  constexpr bool kBoth = D == 64;  // K and V are requested together
+  constexpr bool kBoth = D == 64;  // K and V are on their way together, during a whole pass
   Q8Window window;
   Q8Rows<D> q8[kBoth ? 2 : 1];
   auto &k8 = q8[0], &v8 = q8[kBoth];
   int coming = -1, entry = 0;  // its first tile (none: -1), its lane of the window
   uint64_t q8_off = 0;
   const uint32_t q8_from = Q8Rows<D>::from(a.b.row_stride, lane), q8_k = Q8Rows<D>::template to<true>(lane), q8_v = Q8Rows<D>::template to<false>(lane);
-  auto q8_begin = [&](int u) __attribute__((always_inline)) {  // K of unit u is requested
+  auto q8_begin = [&](int u) __attribute__((always_inline)) {  // K of unit u is requested (kBoth: and V)
     const int t = kPass * u + 1 + w_tile;
     coming = -1;
     if (u >= n_units) return;
@@ -119,16 +120,18 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
     k8.fetch(a.b.k + q8_off, a.b.row_stride, q8_from);
     if constexpr (kBoth) v8.fetch(a.b.v + q8_off, a.b.row_stride, q8_from);
   };
-  auto q8_middle = [&]() __attribute__((always_inline)) {  // ... is in LDS, V is requested
-    if (coming < 0) return;
-    k8.template to_lds<true>(smem + into, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.scales, entry) & 0xFF), q8_k);
-    if constexpr (!kBoth) v8.fetch(a.b.v + q8_off, a.b.row_stride, q8_from);
+  auto q8_scales = [&]() __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_readlane((int)window.scales, entry); };
+  auto q8_middle = [&]() __attribute__((always_inline)) {  // (not kBoth) K is in LDS, V is requested
+    if (kBoth || coming < 0) return;
+    k8.template to_lds<true>(smem + into, w_row, q8_scale(q8_scales() & 0xFF), q8_k);
+    v8.fetch(a.b.v + q8_off, a.b.row_stride, q8_from);
   };
-  auto q8_end = [&]() __attribute__((always_inline)) {
+  auto q8_end = [&]() __attribute__((always_inline)) {  // all of it is in LDS
     if (coming < 0) return;
+    if constexpr (kBoth) k8.template to_lds<true>(smem + into, w_row, q8_scale(q8_scales() & 0xFF), q8_k);
     const int valid = hi_row - (lo + coming * kWideTile + w_row);  // rows that some token sees
     if (valid < kRows) v8.clear_from(valid, lane);
-    v8.template to_lds<false>(smem + into + G::kHalf, w_row, q8_scale((uint32_t)__builtin_amdgcn_readlane((int)window.scales, entry) >> 16), q8_v);
+    v8.template to_lds<false>(smem + into + G::kHalf, w_row, q8_scale(q8_scales() >> 16), q8_v);
   };
   auto request = [&]() __attribute__((always_inline)) {
     const int u = unit++, t = kPass * u + 1 + w_tile, t0 = lo + t * kWideTile + w_row;

@@ -161,7 +161,9 @@ respec_status respec_chunk_attn_q8(const respec_chunk_plan* plan, const respec_q
  * kv_len[b] + i, for i = 0 .. acc_len[b] (path and acc_len as respec_verify_step leaves them: node
  * ids, ascending, the root's 0 first), and kv_len_out[b] = kv_len[b] + acc_len[b] + 1.
  * acc_len[b] = -1 (a step that failed for the sequence): nothing moves, kv_len_out[b] = kv_len[b].
- * A sequence with a non-zero status: nothing moves, kv_len_out[b] = kv_len[b]. */
+ * A sequence with a non-zero status: nothing moves, kv_len_out[b] = kv_len[b].
+ * kv_len_out and seq_status share no byte with kv_len, acc_len, the paths, the page table's rows or each other
+ * (RESPEC_ERR_SHAPE): they are written while other workgroups may still read. */
 typedef struct {
   int32_t batch;               /* 0 .. RESPEC_CHUNK_MAX_BATCH                                    */
   int32_t n_layers;            /* 1 .. 65535                                                     */
@@ -176,7 +178,7 @@ typedef struct {
   int32_t path_width;          /* 1 .. RESPEC_MAX_DEPTH + 1                                       */
   int64_t path_stride;         /* >= path_width (any value for one sequence)                     */
   const int32_t* acc_len;      /* [B] int32                                                      */
-  int32_t* kv_len_out;         /* [B], does not overlap kv_len; or NULL                           */
+  int32_t* kv_len_out;         /* [B] or NULL                                                    */
   int32_t* seq_status;         /* [B] or NULL: RESPEC_OK, RESPEC_ERR_TREE (acc_len below -1 or not below
                                   path_width; path not ascending from a node id >= 0),
                                   RESPEC_ERR_CAPACITY (kv_len negative, or more rows than the table's

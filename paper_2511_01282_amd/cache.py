@@ -243,8 +243,8 @@ class CacheLayers:
 
     def keep_rows(self, page_table, kv_len, path, acc_len, kv_len_out=None, *, status=None, stream=None) -> None:
         """Enqueue respec_cache_keep: the accepted rows of every sequence's verified tree (``path`` [B][width] and ``acc_len`` [B],
-        as a verification step leaves them) move behind its ``kv_len`` rows, in every layer, and ``kv_len_out`` becomes
-        its new length.  For caches of the step's types, float32 and bfloat16, K and V laid out alike."""
+        as a verification step leaves them) move behind its ``kv_len`` rows, in every layer, and ``kv_len_out`` (memory of
+        its own, not one of the call's other arrays) becomes its new length.  For caches of the step's types, float32 and bfloat16, K and V laid out alike."""
         if self._keep is None:
             raise ValueError("float32 or bfloat16 caches with heads of 64 or 128 columns, K and V laid out alike, expected")
         batch, width = page_table.shape

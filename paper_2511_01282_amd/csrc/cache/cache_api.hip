@@ -8,6 +8,7 @@
 #include <new>
 
 #include "../../../include/respec_cache.h"
+#include "../overlap.hpp"
 #include "cache.hpp"
 
 using namespace respec;
@@ -145,9 +146,17 @@ respec_status respec_cache_keep(const respec_cache_keep_args* args, void* stream
   if (x.path_width < 1 || x.path_width > kKeepMaxPath) return RESPEC_ERR_SHAPE;
   if (x.batch == 0) return RESPEC_OK;
   if (!c.k || !c.v || !c.page_table || !x.kv_len || !x.path || !x.acc_len) return RESPEC_ERR_NULL;
-  if (x.kv_len_out && x.kv_len_out < x.kv_len + x.batch && x.kv_len < x.kv_len_out + x.batch) return RESPEC_ERR_SHAPE;
   if (c.n_pages < 1 || c.page_size < 1 || c.table_width < 1) return RESPEC_ERR_SHAPE;
   if (x.batch > 1 && (c.table_stride < c.table_width || x.path_stride < x.path_width)) return RESPEC_ERR_SHAPE;
+  // A sequence's length and status are written by its first workgroup, while those of other layers may not have started.
+  const int64_t ints = 4ll * x.batch;
+  const __int128 path_step = x.batch > 1 ? (__int128)4 * x.path_stride : 0, table_step = x.batch > 1 ? (__int128)4 * c.table_stride : 0;
+  for (const int32_t* to : {x.kv_len_out, x.seq_status})
+    if (overlap(to, ints, x.kv_len, 1, 0, ints) || overlap(to, ints, x.acc_len, 1, 0, ints) ||
+        overlap(to, ints, x.path, x.batch, path_step, 4ll * x.path_width) ||
+        overlap(to, ints, c.page_table, x.batch, table_step, 4ll * c.table_width))
+      return RESPEC_ERR_SHAPE;
+  if (overlap(x.kv_len_out, ints, x.seq_status, 1, 0, ints)) return RESPEC_ERR_SHAPE;
   for (int64_t s : {c.page_stride, c.head_stride, c.row_stride, x.layer_stride})
     if (!stride_ok(s, es)) return RESPEC_ERR_SHAPE;
   if (c.row_stride > 1 << 24 || !aligned(c.k, 16) || !aligned(c.v, 16)) return RESPEC_ERR_SHAPE;

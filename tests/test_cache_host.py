@@ -345,3 +345,44 @@ def test_layers_binding_refusals(lib):
     for bad in ((torch.zeros(2, dtype=i32), torch.zeros(3, dtype=i32)), (torch.zeros(2), torch.zeros(2, dtype=i32))):
         with pytest.raises(ValueError):
             layers.copy_pages(*bad)
+
+
+def _keep_args(lib, p, **over):  # noqa: F811
+    """Two sequences, paths of 6 ids 10 apart, tables of 5 pages 9 apart; every array has a place of its own."""
+    cache = dict(k=FAKE, v=FAKE, n_pages=9, page_size=16, page_stride=2 * 16 * 64, head_stride=16 * 64, row_stride=64,
+                 page_table=FAKE + 0x1000, table_width=5, table_stride=9)
+    d = dict(batch=2, n_layers=3, n_kv_heads=2, head_dim=64, dtype=1, layer_stride=9 * 2048, kv_len=FAKE + 0x2000, path=FAKE + 0x3000,
+             path_width=6, path_stride=10, acc_len=FAKE + 0x4000, kv_len_out=FAKE + 0x5000, seq_status=FAKE + 0x6000)
+    cache.update({k: v for k, v in over.items() if k in cache})
+    d.update({k: v for k, v in over.items() if k in d})
+    return lib.KeepArgs(cache=p.PagedCache(**cache), **d)
+
+
+@pytest.mark.parametrize("written", ["kv_len_out", "seq_status"])
+@pytest.mark.parametrize("over", [
+    {"acc_len": 0}, {"acc_len": 4}, {"acc_len": -4}, {"kv_len": 0}, {"kv_len": 4}, {"path": 0}, {"path": -20}, {"path": -40},
+    {"path": -60}, {"path": 4}, {"page_table": 0}, {"page_table": -16}, {"page_table": -36}, {"page_table": -52}])
+def test_keep_writes_nothing_that_it_reads(lib, p, written, over):  # noqa: F811
+    """Lengths and statuses are written while other workgroups still read (name: its distance from the written array)."""
+    to = FAKE + 0x8000
+    a = _keep_args(lib, p, **{written: to}, **{name: to + by for name, by in over.items()})
+    assert lib.lib().respec_cache_keep(ctypes.byref(a), None) == SHAPE
+
+
+def test_keep_writes_lengths_and_statuses_apart(lib, p):  # noqa: F811
+    for by in (0, 4, -4):
+        a = _keep_args(lib, p, kv_len_out=FAKE + 0x6000 + by)
+        assert lib.lib().respec_cache_keep(ctypes.byref(a), None) == SHAPE
+
+
+def test_keep_binding_refuses_what_it_reads(lib):
+    """kv_len_out in acc_len's place, in kv_len's, and in the first path's."""
+    i32 = torch.int32
+    k = torch.zeros(3, 5, 2, 16, 64, dtype=torch.bfloat16)
+    layers = lib.CacheLayers(k, k)
+    lens, path, acc = torch.zeros(2, dtype=i32), torch.zeros(2, 6, dtype=i32), torch.zeros(2, dtype=i32)
+    seen = []
+    layers._call = lambda fn, name, args, stream: seen.append(fn(args, None))
+    for out in (acc, lens, path[0, 1:3]):
+        layers.keep_rows(torch.zeros(2, 3, dtype=i32), lens, path, acc, out)
+    assert seen == [SHAPE] * 3

@@ -640,6 +640,20 @@ def test_keep_rows_past_32_bits(lib):
     assert int((k != 0).sum()) == 2 * 8 * 128
 
 
+def test_keep_writes_in_gaps_of_what_it_reads(lib):
+    """New lengths and statuses in the gaps between the paths' rows and the page table's, as columns of one array of integers."""
+    rng = random.Random(5)
+    lens, acc, paths, table, k, v = _keep_case(rng, 3, 2, 2, 64, 16, BF)
+    wide = _ints([p + [-1] * (26 - len(p)) + [-9] * 3 for p in paths])
+    pages = _ints([t + [-9] * 3 for t in table])
+    path, out, st = wide[:, :26], wide[1, 26:], pages[0, len(table[0]):]
+    kg, vg = k.cuda(), v.cuda()
+    lib[2].CacheLayers(kg, vg).keep_rows(pages[:, :len(table[0])], _ints(lens), path, _ints(acc), out, status=st)
+    assert st.tolist() == [0] * 3 and out.tolist() == [l + len(p) for l, p in zip(lens, paths)]
+    assert torch.equal(kg.cpu(), _kept(k, lens, paths, table, 16)) and torch.equal(vg.cpu(), _kept(v, lens, paths, table, 16))
+    assert bool((wide[0, 26:] == -9).all()) and bool((wide[2, 26:] == -9).all()) and bool((pages[1:, len(table[0]):] == -9).all())
+
+
 def test_captured_keep_replays(lib):
     """Captured once, replayed on other caches' contents, lengths and paths (failed sequences among them), eager work in between."""
     rng = random.Random(11)

@@ -14,7 +14,8 @@
  * enqueue kernels on the caller's stream and can be captured, host checks that return
  * a status and launch nothing (RESPEC_ERR_SHAPE, too, for a launch of 2^32 threads or more),
  * errors in device data reported per sequence or pair (when the caller gives an
- * array for them) with no access outside the buffers described here. */
+ * array for them, which shares no byte with what the call reads: RESPEC_ERR_SHAPE)
+ * with no access outside the buffers described here. */
 #ifndef RESPEC_CACHE_H
 #define RESPEC_CACHE_H
 

@@ -100,7 +100,9 @@ typedef struct {
   int32_t* seq_status;         /* [B] or NULL: RESPEC_OK, RESPEC_ERR_SHAPE (new_off: decreasing,
                                   outside [0, total_new], or more than max_new_in_batch tokens),
                                   RESPEC_ERR_CAPACITY (kv_len outside [0, max_kv_len_in_batch], or
-                                  more rows than table_width pages hold), RESPEC_ERR_PAGE        */
+                                  more rows than table_width pages hold), RESPEC_ERR_PAGE.  Shares no
+                                  byte with new_off, kv_len and the page table's rows (the call:
+                                  RESPEC_ERR_SHAPE), which other workgroups may still read      */
 } respec_chunk_batch;
 
 /* Strides of the packed tensors are in elements and multiples of 16 bytes;

@@ -129,6 +129,10 @@ respec_status respec_rotary(const respec_rotary_plan* plan, const respec_rotary_
   a.status_wgs = reports;
   const long long wgs = reports + ceil_div(a.tokens, a.tok_per_wg), per_token = a.tok_per_wg > 1 ? 1 : ceil_div(slots, kRotaryThreads);
   if (!launchable(wgs * per_token, kRotaryThreads)) return RESPEC_ERR_SHAPE;
+  // (a status is written while workgroups of tokens still read offsets and lengths)
+  if (reports > 0 && (overlap(x.seq_status, 4ll * x.batch, x.new_off, 1, 0, 4ll * x.batch + 4) ||
+                      overlap(x.seq_status, 4ll * x.batch, x.kv_len, 1, 0, 4ll * x.batch)))
+    return RESPEC_ERR_SHAPE;
   return launch_rotary(es, s.head_dim, s.layout == RESPEC_ROTARY_HALF, r, (int)wgs, (int)per_token, a, static_cast<hipStream_t>(stream)) ==
                  hipSuccess
              ? RESPEC_OK
@@ -148,15 +152,6 @@ respec_status respec_cache_keep(const respec_cache_keep_args* args, void* stream
   if (!c.k || !c.v || !c.page_table || !x.kv_len || !x.path || !x.acc_len) return RESPEC_ERR_NULL;
   if (c.n_pages < 1 || c.page_size < 1 || c.table_width < 1) return RESPEC_ERR_SHAPE;
   if (x.batch > 1 && (c.table_stride < c.table_width || x.path_stride < x.path_width)) return RESPEC_ERR_SHAPE;
-  // A sequence's length and status are written by its first workgroup, while those of other layers may not have started.
-  const int64_t ints = 4ll * x.batch;
-  const __int128 path_step = x.batch > 1 ? (__int128)4 * x.path_stride : 0, table_step = x.batch > 1 ? (__int128)4 * c.table_stride : 0;
-  for (const int32_t* to : {x.kv_len_out, x.seq_status})
-    if (overlap(to, ints, x.kv_len, 1, 0, ints) || overlap(to, ints, x.acc_len, 1, 0, ints) ||
-        overlap(to, ints, x.path, x.batch, path_step, 4ll * x.path_width) ||
-        overlap(to, ints, c.page_table, x.batch, table_step, 4ll * c.table_width))
-      return RESPEC_ERR_SHAPE;
-  if (overlap(x.kv_len_out, ints, x.seq_status, 1, 0, ints)) return RESPEC_ERR_SHAPE;
   for (int64_t s : {c.page_stride, c.head_stride, c.row_stride, x.layer_stride})
     if (!stride_ok(s, es)) return RESPEC_ERR_SHAPE;
   if (c.row_stride > 1 << 24 || !aligned(c.k, 16) || !aligned(c.v, 16)) return RESPEC_ERR_SHAPE;
@@ -183,6 +178,15 @@ respec_status respec_cache_keep(const respec_cache_keep_args* args, void* stream
   a.kv_len_out = x.kv_len_out;
   a.pieces = x.n_kv_heads * x.head_dim * es / 16;
   if (!launchable(ceil_div(2 * a.pieces, kKeepThreads) * x.n_layers * x.batch, kKeepThreads)) return RESPEC_ERR_SHAPE;
+  // A sequence's length and status are written by its first workgroup, while those of other layers may not have started.
+  const int64_t ints = 4ll * x.batch;
+  const __int128 path_step = x.batch > 1 ? (__int128)4 * x.path_stride : 0, table_step = x.batch > 1 ? (__int128)4 * c.table_stride : 0;
+  for (const int32_t* to : {x.kv_len_out, x.seq_status})
+    if (overlap(to, ints, x.kv_len, 1, 0, ints) || overlap(to, ints, x.acc_len, 1, 0, ints) ||
+        overlap(to, ints, x.path, x.batch, path_step, 4ll * x.path_width) ||
+        overlap(to, ints, c.page_table, x.batch, table_step, 4ll * c.table_width))
+      return RESPEC_ERR_SHAPE;
+  if (overlap(x.kv_len_out, ints, x.seq_status, 1, 0, ints)) return RESPEC_ERR_SHAPE;
   return launch_keep(x.head_dim * es, x.n_layers, a, static_cast<hipStream_t>(stream)) == hipSuccess ? RESPEC_OK : RESPEC_ERR_HIP;
 }
 
@@ -244,6 +248,9 @@ respec_status respec_cache_copy(const respec_cache_copy_args* args, void* stream
   if (wgs > INT_MAX || !launchable(wgs, kCopyThreads) || !launchable(wgs * layers, kCopyThreads) ||
       !launchable(wgs * layers * x.pairs, kCopyThreads))
     return RESPEC_ERR_SHAPE;
+  // (a pair's status is written while its other workgroups still read the ids)
+  for (const int32_t* ids : {x.src, x.dst})
+    if (overlap(x.status, 4ll * x.pairs, ids, 1, 0, 4ll * x.pairs)) return RESPEC_ERR_SHAPE;
   return launch_copy((int)wgs, layers, x.pairs, a, static_cast<hipStream_t>(stream)) == hipSuccess ? RESPEC_OK : RESPEC_ERR_HIP;
 }
 

@@ -10,6 +10,7 @@
 #include "../../../include/respec_cache.h"
 #include "../../../include/respec_prompt.h"
 #include "../attn_route.hpp"
+#include "../overlap.hpp"
 #include "prompt.hpp"
 
 using namespace respec;
@@ -61,6 +62,15 @@ respec_status check_batch(const respec_chunk_plan* plan, const respec_chunk_batc
     return RESPEC_ERR_SHAPE;
   if (!aligned(c.k, 16) || !aligned(c.v, 16)) return RESPEC_ERR_SHAPE;
   return RESPEC_OK;
+}
+
+// Whether the statuses lie apart from what the kernels read: a sequence's is written while other workgroups still look up lengths
+// and pages.
+bool status_apart(const respec_chunk_batch& b) {
+  const respec_paged_cache& c = b.cache;
+  const int64_t ints = 4ll * b.batch;
+  return !overlap(b.seq_status, ints, b.new_off, 1, 0, ints + 4) && !overlap(b.seq_status, ints, b.kv_len, 1, 0, ints) &&
+         !overlap(b.seq_status, ints, c.page_table, b.batch, b.batch > 1 ? (__int128)4 * c.table_stride : 0, 4ll * c.table_width);
 }
 
 ChunkBatch device_batch(const respec_chunk_plan* plan, const respec_chunk_batch& b, int ces) {
@@ -232,7 +242,7 @@ respec_status attend(const respec_chunk_plan* plan, const respec_chunk_attn_args
     a.few_rows = 0;
     a.few = ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
     a.wide = geometry(a.b, 64, blocks(64), limit, 32, 32, 2, s.head_dim == 128 ? Pace{0.16, 5} : Pace{0.1, 5}, rb, held);
-    if (!launchable(a.wide.items + reports, kAttnF32Threads)) return RESPEC_ERR_SHAPE;
+    if (!launchable(a.wide.items + reports, kAttnF32Threads) || !status_apart(x.b)) return RESPEC_ERR_SHAPE;
     e = launch_chunk_attn_f32(s.head_dim, q8 != nullptr, a, status, stm);
   } else {
     // Calls of at most 64 query rows per KV head have the few-row kernel, of one or two groups of 32 (over an 8-bit cache: of one,
@@ -252,7 +262,8 @@ respec_status attend(const respec_chunk_plan* plan, const respec_chunk_attn_args
                              : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
     a.wide = wide ? geometry(a.b, 256, blocks(256), limit, 128, 256, 1, s.head_dim == 128 ? Pace{0.032, 6} : Pace{0.018, 6}, rb, held)
                   : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
-    if (!launchable((long long)a.few.items + a.wide.items + reports, wide ? kAttnWideThreads : kAttnFewThreads)) return RESPEC_ERR_SHAPE;
+    if (!launchable((long long)a.few.items + a.wide.items + reports, wide ? kAttnWideThreads : kAttnFewThreads) || !status_apart(x.b))
+      return RESPEC_ERR_SHAPE;
     if (!raise_lds_limits(s.head_dim, q8 != nullptr)) return RESPEC_ERR_HIP;
     if (q8)
       e = wide ? launch_q8_attn_wide(s.head_dim, a, mixed, status, stm) : launch_q8_attn_few(s.head_dim, a, status, stm);
@@ -317,7 +328,8 @@ respec_status respec_chunk_append(const respec_chunk_plan* plan, const respec_ch
   const int pieces = 2 * plan->s.n_kv_heads * plan->s.head_dim * plan->es / 16;  // of a token
   a.per_tok = fast_div((uint32_t)pieces);
   a.tok_per_wg = std::max(1, std::min(2048 / pieces, kAppendMaxTok));
-  if (!launchable(ceil_div(x.b.total_new, a.tok_per_wg) + (x.b.seq_status ? x.b.batch : 0), kAppendThreads)) return RESPEC_ERR_SHAPE;
+  if (!launchable(ceil_div(x.b.total_new, a.tok_per_wg) + (x.b.seq_status ? x.b.batch : 0), kAppendThreads) || !status_apart(x.b))
+    return RESPEC_ERR_SHAPE;
   return launch_chunk_append(plan->es, plan->s.head_dim, a, static_cast<hipStream_t>(stream)) == hipSuccess
              ? RESPEC_OK
              : RESPEC_ERR_HIP;
@@ -369,7 +381,7 @@ respec_status respec_chunk_append_q8(const respec_chunk_plan* plan, const respec
   const int waves = block == 128 ? 8 : kAppendQ8Waves, per_wg = waves / (int)(block / 16);
   const long long wgs = ceil_div(blocks * 2 * plan->s.n_kv_heads, per_wg), reports = b.seq_status ? b.batch : 0;
   if (wgs + reports == 0) return RESPEC_OK;
-  if (!launchable(wgs + reports, 64 * waves)) return RESPEC_ERR_SHAPE;
+  if (!launchable(wgs + reports, 64 * waves) || !status_apart(b)) return RESPEC_ERR_SHAPE;
   a.wgs = (int)wgs;
   return launch_append_q8(plan->es, plan->s.head_dim, a, static_cast<hipStream_t>(stream)) == hipSuccess ? RESPEC_OK : RESPEC_ERR_HIP;
 }

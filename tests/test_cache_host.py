@@ -386,3 +386,47 @@ def test_keep_binding_refuses_what_it_reads(lib):
     for out in (acc, lens, path[0, 1:3]):
         layers.keep_rows(torch.zeros(2, 3, dtype=i32), lens, path, acc, out)
     assert seen == [SHAPE] * 3
+
+
+# ---------------------------------------------------------------------------
+# statuses in the place of what a call reads
+# ---------------------------------------------------------------------------
+
+TO = FAKE + 0x8000
+
+
+@pytest.mark.parametrize("over", [{"new_off": 0}, {"new_off": -8}, {"new_off": 4}, {"kv_len": 0}, {"kv_len": 4}, {"kv_len": -4},
+                                  {"page_table": 0}, {"page_table": -16}, {"page_table": -36}, {"page_table": 4}])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_chunk_status_apart(p, over, dtype):  # noqa: F811
+    """(name: its distance from the statuses)"""
+    import test_prompt_host
+    _, h = _create(p, "chunk", _chunk_shape(p, dtype=dtype))
+    d = dict(new_off=FAKE + 0x1000, kv_len=FAKE + 0x2000, page_table=FAKE + 0x3000, seq_status=TO, table_stride=9)
+    d.update({name: TO + by for name, by in over.items()})
+    L = p.lib()
+    for b, append, attn, ap, at in ((_batch(p, **d), L.respec_chunk_append_q8, L.respec_chunk_attn_q8, p.Q8AppendArgs, p.Q8AttnArgs),
+                                    (test_prompt_host._batch(p, **d), L.respec_chunk_append, L.respec_chunk_attn, p.AppendArgs, p.AttnArgs)):
+        assert append(h, ctypes.byref(ap(b, FAKE, FAKE, 128, 64, 128, 64)), None) == SHAPE
+        assert attn(h, ctypes.byref(at(b, FAKE, 512, 64, FAKE, 512, 64, 0.0)), FAKE, None) == SHAPE
+    L.respec_chunk_destroy(h)
+
+
+@pytest.mark.parametrize("over", [{"new_off": 0}, {"new_off": -8}, {"new_off": 4}, {"kv_len": 0}, {"kv_len": 4}, {"kv_len": -4}])
+@pytest.mark.parametrize("tokens", [0, 5])
+def test_rotary_status_apart(lib, over, tokens):
+    _, h = _rotary(lib)
+    d = dict(tokens=tokens, positions=None, batch=2, new_off=FAKE + 0x1000, kv_len=FAKE + 0x2000, seq_status=TO)
+    for x, n, at in (("q", 8, 0x100000), ("q_out", 8, 0x200000), ("k", 2, 0x300000), ("k_out", 2, 0x400000)):
+        d.update({x: FAKE + at, x + "_token_stride": n * 64, x + "_head_stride": 64})
+    d.update({name: TO + by for name, by in over.items()})
+    assert lib.lib().respec_rotary(h, ctypes.byref(lib.RotaryArgs(**d)), None) == SHAPE
+    lib.lib().respec_rotary_destroy(h)
+
+
+@pytest.mark.parametrize("over", [{"src": 0}, {"src": 8}, {"dst": 0}, {"dst": -8}])
+def test_copy_status_apart(lib, over):
+    planes = (lib.PagePlane * 1)(lib.PagePlane(FAKE, 4096, 2, 1 << 20, 2, 2048, 16, 128, 128))
+    d = dict(pairs=3, src=FAKE + 0x1000, dst=FAKE + 0x2000, n_pages=9, n_planes=1, planes=ctypes.addressof(planes), status=TO)
+    d.update({name: TO + by for name, by in over.items()})
+    assert lib.lib().respec_cache_copy(ctypes.byref(lib.CopyArgs(**d)), None) == SHAPE

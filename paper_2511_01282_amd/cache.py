@@ -125,8 +125,8 @@ class RotaryPlan(_Plan):
             frequencies = _frequencies(max(rotary_dim, 1), base)
         if len(frequencies) != rotary_dim // 2:
             raise ValueError(f"frequencies: one for each of {rotary_dim // 2} pairs expected, got {len(frequencies)}")
-        if not amplitude > 0:
-            raise ValueError("amplitude: a positive number expected")
+        if not ctypes.c_float(amplitude).value > 0:   # (0 would mean 1)
+            raise ValueError("amplitude: a positive number expected, in float32, too")
         w = (ctypes.c_double * max(len(frequencies), 1))(*frequencies)
         super().__init__("rotary", RotaryShape(n_q_heads, n_kv_heads, head_dim, rotary_dim, layout, dtype, max_tokens, amplitude),
                          device, None, w)

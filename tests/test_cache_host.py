@@ -430,3 +430,20 @@ def test_copy_status_apart(lib, over):
     d = dict(pairs=3, src=FAKE + 0x1000, dst=FAKE + 0x2000, n_pages=9, n_planes=1, planes=ctypes.addressof(planes), status=TO)
     d.update({name: TO + by for name, by in over.items()})
     assert lib.lib().respec_cache_copy(ctypes.byref(lib.CopyArgs(**d)), None) == SHAPE
+
+
+# ---------------------------------------------------------------------------
+# rotary amplitudes as the library takes them
+# ---------------------------------------------------------------------------
+
+def test_rotary_amplitude_as_float32(lib):
+    """The library takes a float32, of which 0 means 1: a number that rounds to 0 is refused, as one that rounds to infinity."""
+    new = dict(n_q_heads=4, n_kv_heads=2, head_dim=64, dtype=1, device="cpu")
+    for bad in (1e-50, 2.0 ** -150, -1e-50, -0.0):
+        with pytest.raises(ValueError):
+            lib.RotaryPlan(**new, amplitude=bad)
+    for bad in (1e39, math.inf):
+        with pytest.raises(lib.VerifyError):
+            lib.RotaryPlan(**new, amplitude=bad)
+    for good in (2.0 ** -149, 1.0, 3e38):
+        assert lib.RotaryPlan(**new, amplitude=good).shape.amplitude == torch.tensor(good, dtype=torch.float32).item()

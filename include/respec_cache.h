@@ -52,7 +52,9 @@ typedef struct {
  * a turn at every position; cosines, sines and products are float32, rounded once.
  * Positions are given one per token, or as a chunk batch's: token i of sequence b
  * stands at kv_len[b] + i.  A token at a negative position, one of no sequence and those of a
- * sequence with a non-zero status keep what their output rows held. */
+ * sequence with a non-zero status keep what their output rows held.
+ * An output shares no byte with an input, the other output or itself (RESPEC_ERR_SHAPE), but may be
+ * its input with the same strides; tensors may lie between each other's rows. */
 typedef struct {
   int32_t tokens;              /* rows of the tensors, 0 <= tokens <= max_tokens                */
   const int32_t* positions;    /* [tokens] int32, or NULL: new_off and kv_len                   */
@@ -61,7 +63,7 @@ typedef struct {
   const int32_t* kv_len;       /* [batch] int32                                                 */
   const void* q;               /* [tokens][Hq][D], or NULL (with q_out): no queries              */
   int64_t q_token_stride, q_head_stride;
-  void* q_out;                 /* as q; may be q itself with q's strides                         */
+  void* q_out;                 /* as q                                                          */
   int64_t q_out_token_stride, q_out_head_stride;
   const void* k;               /* [tokens][Hkv][D], or NULL (with k_out)                         */
   int64_t k_token_stride, k_head_stride;

@@ -150,7 +150,7 @@ class RotaryPlan(_Plan):
 
     def rotate(self, q, k, q_out, k_out, *, positions=None, new_off=None, kv_len=None, status=None, stream=None) -> None:
         """Enqueue respec_rotary: ``q`` [T][Hq][D] into ``q_out`` and ``k`` [T][Hkv][D] into ``k_out`` (each pair, or neither
-        of it, given; an output may be its input), at ``positions`` [T] (negative: left alone), or at a chunk batch's,
+        of it, given; an output may be its input, and overlaps nothing else), at ``positions`` [T] (negative: left alone), or at a chunk batch's,
         ``kv_len[b]`` + i for token ``new_off[b]`` + i."""
         s, i32 = self.shape, torch.int32
         tq, qs = self._side(q, q_out, "q", s.n_q_heads)

@@ -29,6 +29,25 @@ bool stride_ok(int64_t s, int es) { return s >= 0 && s < kMaxStride && s * es % 
 // A dispatch counts its threads in 32 bits (and its workgroups of the second and third dimension in 16).
 bool launchable(long long workgroups, int threads) { return workgroups >= 0 && workgroups < (1ll << 32) / threads; }
 
+// Whether rotary outputs share bytes with nothing that another thread reads or writes: an output may be its input.
+bool outputs_apart(const respec_rotary_plan* plan, const respec_rotary_args& x) {
+  const int es = plan->es;
+  const int64_t t = x.tokens, row = (int64_t)plan->s.head_dim * es;
+  const int hq = plan->s.n_q_heads, hkv = plan->s.n_kv_heads;
+  auto rows = [&](const void* p, int64_t token, int h, int64_t head) { return row_set(p, t, token * es, h, head * es, row); };
+  const RowSet in[2] = {rows(x.q, x.q_token_stride, hq, x.q_head_stride), rows(x.k, x.k_token_stride, hkv, x.k_head_stride)};
+  const RowSet out[2] = {rows(x.q_out, x.q_out_token_stride, hq, x.q_out_head_stride), rows(x.k_out, x.k_out_token_stride, hkv, x.k_out_head_stride)};
+  for (int i = 0; i < 2; ++i) {
+    if (!out[i].at) continue;
+    if (overlap_within(t, (i ? x.k_out_token_stride : x.q_out_token_stride) * es, row) ||
+        overlap_within(i ? hkv : hq, (i ? x.k_out_head_stride : x.q_out_head_stride) * es, row))
+      return false;
+    for (int j = 0; j < 2; ++j)
+      if (in[j].at && !(i == j && same_rows(out[i], in[j])) && overlap(out[i], in[j])) return false;
+  }
+  return !(out[0].at && out[1].at && overlap(out[0], out[1]));
+}
+
 constexpr double kTurn = 6.283185307179586;  // 2 pi, rounded down
 // 2^64 times the fraction of a turn that w radians are, to 2^-63 of w and half a unit: under 2^-62, so that 2^31 positions further the
 // angle is within 2^-31 of a turn.
@@ -129,6 +148,7 @@ respec_status respec_rotary(const respec_rotary_plan* plan, const respec_rotary_
   a.status_wgs = reports;
   const long long wgs = reports + ceil_div(a.tokens, a.tok_per_wg), per_token = a.tok_per_wg > 1 ? 1 : ceil_div(slots, kRotaryThreads);
   if (!launchable(wgs * per_token, kRotaryThreads)) return RESPEC_ERR_SHAPE;
+  if (rows && !outputs_apart(plan, x)) return RESPEC_ERR_SHAPE;
   // (a status is written while workgroups of tokens still read offsets and lengths)
   if (reports > 0 && (overlap(x.seq_status, 4ll * x.batch, x.new_off, 1, 0, 4ll * x.batch + 4) ||
                       overlap(x.seq_status, 4ll * x.batch, x.kv_len, 1, 0, 4ll * x.batch)))

@@ -447,3 +447,44 @@ def test_rotary_amplitude_as_float32(lib):
             lib.RotaryPlan(**new, amplitude=bad)
     for good in (2.0 ** -149, 1.0, 3e38):
         assert lib.RotaryPlan(**new, amplitude=good).shape.amplitude == torch.tensor(good, dtype=torch.float32).item()
+
+
+# ---------------------------------------------------------------------------
+# rotary outputs in the place of what other threads read
+# ---------------------------------------------------------------------------
+
+Q, K, ROW = FAKE + 0x100000, FAKE + 0x300000, 64   # (elements of a row; a bf16 row is 128 bytes)
+
+
+@pytest.mark.parametrize("over", [
+    {"q_out": Q + 128}, {"q_out": Q - 128}, {"q_out": Q + 16}, {"q_out": Q + 1024}, {"q_out": Q - 1024}, {"q_out": Q + 4 * 1024},
+    {"q_out": Q, "q_out_token_stride": 9 * ROW}, {"q_out": Q, "q_out_token_stride": ROW, "q_out_head_stride": 5 * ROW},
+    {"k_out": K + 128}, {"k_out": Q}, {"k_out": Q + 5 * 1024 - 16}, {"q_out": K}, {"q_out": K - 128 * 39}, {"k_out": FAKE + 0x200000},
+    {"k_out": FAKE + 0x200000 + 128 * 39}, {"q_out_token_stride": 0}, {"q_out_head_stride": ROW - 8}, {"k_out_token_stride": 8},
+    {"q_token_stride": 0, "q_out": Q}, {"q_token_stride": 20 * ROW, "q_out": Q + 128 * 7, "q_out_token_stride": 20 * ROW},
+    {"q_token_stride": 20 * ROW, "k_out": Q + 128 * 27, "k_out_token_stride": 20 * ROW},
+    {"q_token_stride": 20 * ROW, "q_out": Q + 1024 - 112, "q_out_token_stride": 24 * ROW}])
+@pytest.mark.parametrize("given", ["positions", "batch"])
+def test_rotary_outputs_apart(lib, over, given):
+    """Five tokens of 8 and 2 heads of 128 bytes: shifted by a token, a head, a piece; the same place laid out differently; the
+    other side's rows; rows of one output in each other's place."""
+    _, h = _rotary(lib)
+    d = dict(tokens=5, positions=FAKE if given == "positions" else None, batch=1, new_off=FAKE, kv_len=FAKE + 64)
+    for x, n, at in (("q", 8, Q), ("q_out", 8, FAKE + 0x200000), ("k", 2, K), ("k_out", 2, FAKE + 0x400000)):
+        d.update({x: at, x + "_token_stride": n * ROW, x + "_head_stride": ROW})
+    assert lib.lib().respec_rotary(h, ctypes.byref(lib.RotaryArgs(**dict(d, **over))), None) == SHAPE
+    lib.lib().respec_rotary_destroy(h)
+
+
+def test_rotary_binding_refuses_overlapping_outputs(lib):
+    plan = lib.RotaryPlan(n_q_heads=4, n_kv_heads=2, head_dim=64, dtype=1, device="cpu")
+    plan._call = lambda fn, name, args, stream: seen.append(fn(plan._h, *args, None))
+    wide, pos, seen = torch.zeros(6, 9, 64, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32), []
+    q = wide[:4, :4]
+    with pytest.raises(ValueError):   # q's own place, the tokens and heads exchanged
+        plan.rotate(q, None, q.transpose(0, 1), None, positions=pos)
+    for out in (wide[1:5, :4], wide[2:6, :4], wide[:4, 1:5], wide[:4, 3:7], wide[1:5, 2:6]):
+        plan.rotate(q, None, out, None, positions=pos)
+    plan.rotate(q, wide[:4, 4:6], wide[:4, 5:9], wide[:4, 4:6], positions=pos)
+    plan.rotate(q, None, torch.zeros(1, 4, 64, dtype=torch.bfloat16).expand(4, 4, 64), None, positions=pos)
+    assert seen == [SHAPE] * 7

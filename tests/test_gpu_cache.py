@@ -112,6 +112,32 @@ def test_rotary_of_a_batch(lib, dtype, half):
     _close(same.cpu(), want, tol)
 
 
+def test_rotary_between_rows(lib):
+    """Inputs and outputs that lie between each other's rows are no overlap: slices of one array, by heads, by tokens, and with the
+    heads ahead of the tokens; sides in place, and one input for all tokens."""
+    t, h, hkv, d = 21, 4, 2, 64
+    w = lib[2].frequencies(d)
+    q, k = _rows(t, h, hkv, d, BF, 10)
+    pos = [5 * i for i in range(t)]
+    plan = _rotary_plan(lib, q, k, d, True, w)
+    want = [cc.rotary(x, pos, w, d, True) for x in (q, k)]
+    heads = torch.zeros(t, 2 * (h + hkv) + 1, d, dtype=BF, device="cuda")
+    tokens = torch.zeros(2 * t, h + hkv, d, dtype=BF, device="cuda")
+    ahead = torch.zeros(2 * (h + hkv), t, d, dtype=BF, device="cuda").transpose(0, 1)
+    same = torch.zeros(t, h + hkv, d, dtype=BF, device="cuda")
+    for a, b, c, e in ((heads[:, :h], heads[:, h:h + hkv], heads[:, h + hkv:2 * h + hkv], heads[:, 2 * h + hkv:-1]),
+                       (tokens[::2, :h], tokens[::2, h:], tokens[1::2, :h], tokens[1::2, h:]),
+                       (ahead[:, :2 * h:2], ahead[:, 2 * h::2], ahead[:, 1:2 * h:2], ahead[:, 2 * h + 1::2]),
+                       (same[:, :h], same[:, h:], same[:, :h], same[:, h:])):
+        a.copy_(q), b.copy_(k)
+        plan.rotate(a, b, c, e, positions=_ints(pos))
+        _close(c.cpu(), *want[0])
+        _close(e.cpu(), *want[1])
+    out = torch.zeros(t, h, d, dtype=BF, device="cuda")
+    plan.rotate(q[:1].cuda().expand(t, h, d), None, out, None, positions=_ints(pos))
+    _close(out.cpu(), *cc.rotary(q[:1].expand(t, h, d), pos, w, d, True))
+
+
 def test_rotary_of_many_sequences(lib):
     """More sequences than a wave has lanes, most of them empty; more rows than a workgroup takes."""
     rng = random.Random(3)

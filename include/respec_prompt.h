@@ -119,7 +119,9 @@ typedef struct {
   respec_chunk_batch b;
   const void* q;               /* [total_new][Hq][D]                                           */
   int64_t q_token_stride, q_head_stride;
-  void* out;                   /* [total_new][Hq][D], may be q itself with q's strides          */
+  void* out;                   /* [total_new][Hq][D], may be q itself with q's strides; else shares no
+                                  byte with q's rows, nor one of its rows with another
+                                  (RESPEC_ERR_SHAPE)                                            */
   int64_t out_token_stride, out_head_stride;
   float scale;                 /* of the scores, finite and > 0; 0 = 1 / sqrt(D)                */
 } respec_chunk_attn_args;

@@ -99,6 +99,16 @@ ChunkBatch device_batch(const respec_chunk_plan* plan, const respec_chunk_batch&
   return d;
 }
 
+// Whether attention's output rows share bytes with nothing that another workgroup reads or writes: they may be the queries' own.
+bool output_apart(const respec_chunk_plan* plan, const respec_chunk_attn_args& x) {
+  const int es = plan->es, heads = plan->s.n_q_heads;
+  const int64_t row = (int64_t)plan->s.head_dim * es, t = x.b.total_new;
+  const RowSet q = row_set(x.q, t, x.q_token_stride * es, heads, x.q_head_stride * es, row);
+  const RowSet out = row_set(x.out, t, x.out_token_stride * es, heads, x.out_head_stride * es, row);
+  return !overlap_within(t, x.out_token_stride * es, row) && !overlap_within(heads, x.out_head_stride * es, row) &&
+         (same_rows(q, out) || !overlap(q, out));
+}
+
 // An 8-bit cache's batch as one over pages of one-byte elements; its scales' checks.
 respec_chunk_batch codes_batch(const respec_q8_batch& b) {
   const respec_q8_cache& c = b.cache;
@@ -237,12 +247,13 @@ respec_status attend(const respec_chunk_plan* plan, const respec_chunk_attn_args
   hipStream_t stm = static_cast<hipStream_t>(stream);
   const bool status = a.b.status != nullptr;
   const long long reports = status ? a.b.batch : 0;  // workgroups that report a sequence's status
+  auto apart = [&] { return status_apart(x.b) && (x.b.total_new == 0 || output_apart(plan, x)); };
   hipError_t e;
   if (s.dtype == RESPEC_F32) {
     a.few_rows = 0;
     a.few = ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
     a.wide = geometry(a.b, 64, blocks(64), limit, 32, 32, 2, s.head_dim == 128 ? Pace{0.16, 5} : Pace{0.1, 5}, rb, held);
-    if (!launchable(a.wide.items + reports, kAttnF32Threads) || !status_apart(x.b)) return RESPEC_ERR_SHAPE;
+    if (!launchable(a.wide.items + reports, kAttnF32Threads) || !apart()) return RESPEC_ERR_SHAPE;
     e = launch_chunk_attn_f32(s.head_dim, q8 != nullptr, a, status, stm);
   } else {
     // Calls of at most 64 query rows per KV head have the few-row kernel, of one or two groups of 32 (over an 8-bit cache: of one,
@@ -262,7 +273,7 @@ respec_status attend(const respec_chunk_plan* plan, const respec_chunk_attn_args
                              : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
     a.wide = wide ? geometry(a.b, 256, blocks(256), limit, 128, 256, 1, s.head_dim == 128 ? Pace{0.032, 6} : Pace{0.018, 6}, rb, held)
                   : ChunkGeom{1, 1, INT_MAX, 0, fast_div(INT_MAX)};
-    if (!launchable((long long)a.few.items + a.wide.items + reports, wide ? kAttnWideThreads : kAttnFewThreads) || !status_apart(x.b))
+    if (!launchable((long long)a.few.items + a.wide.items + reports, wide ? kAttnWideThreads : kAttnFewThreads) || !apart())
       return RESPEC_ERR_SHAPE;
     if (!raise_lds_limits(s.head_dim, q8 != nullptr)) return RESPEC_ERR_HIP;
     if (q8)

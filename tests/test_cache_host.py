@@ -488,3 +488,22 @@ def test_rotary_binding_refuses_overlapping_outputs(lib):
     plan.rotate(q, wide[:4, 4:6], wide[:4, 5:9], wide[:4, 4:6], positions=pos)
     plan.rotate(q, None, torch.zeros(1, 4, 64, dtype=torch.bfloat16).expand(4, 4, 64), None, positions=pos)
     assert seen == [SHAPE] * 7
+
+
+@pytest.mark.parametrize("over", [
+    {"out": Q + 128}, {"out": Q - 128}, {"out": Q + 16}, {"out": Q + 1024}, {"out": Q + 9 * 1024}, {"out": Q - 9 * 1024},
+    {"out": Q, "out_token_stride": 9 * ROW}, {"out_token_stride": 0}, {"out_head_stride": 0}, {"out_token_stride": ROW - 8},
+    {"q_token_stride": 20 * ROW, "out": Q + 128 * 7, "out_token_stride": 20 * ROW}])
+def test_attention_output_apart(p, over):  # noqa: F811
+    """Ten tokens of 8 heads of 128 bytes (256 in float32, whose strides are as many elements)."""
+    import test_prompt_host
+    d = dict(q=Q, q_token_stride=8 * ROW, q_head_stride=ROW, out=FAKE + 0x200000, out_token_stride=8 * ROW, out_head_stride=ROW, scale=0.0)
+    d.update(over)
+    for dtype in (0, 1):
+        _, h = _create(p, "chunk", _chunk_shape(p, dtype=dtype))
+        for rows in (10, 100):   # (few query rows, and many)
+            kw = dict(total_new=rows, max_new_in_batch=rows)
+            for f, a in ((p.lib().respec_chunk_attn_q8, p.Q8AttnArgs(b=_batch(p, **kw), **d)),
+                         (p.lib().respec_chunk_attn, p.AttnArgs(b=test_prompt_host._batch(p, **kw), **d))):
+                assert f(h, ctypes.byref(a), FAKE, None) == SHAPE
+        p.lib().respec_chunk_destroy(h)

@@ -144,17 +144,19 @@ typedef struct {
  * a <= 448 2^k:  the scale is 2^k or, where rows of the sequence stand in the block already
  * (from its first row to kv_len - 1), the larger of that and the scale that they have; these
  * rows' values are rounded again if their scale grows.  A new value x becomes x 2^-k
- * rounded to nearest even; a NaN or an infinity becomes a NaN.  (A value within 2^-5 of 2^128 of
- * its size may round to 2^128, which attention takes for an infinity.)  Rows of the block behind the new
+ * rounded to nearest even; a NaN or an infinity becomes a NaN.  (A number within 2^-5 of 2^128 of
+ * its size may round to 2^128, which attention takes for an infinity in a key.)  Rows of the block behind the new
  * ones keep their bytes.
  * A block belongs to one sequence while it is written: what the rows of a block hold that two
  * sequences of the call write is unspecified (share whole blocks, copy a partly filled page
  * first). */
 respec_status respec_chunk_append_q8(const respec_chunk_plan* plan, const respec_q8_append_args* args, void* stream);
 
-/* respec_chunk_attn over an 8-bit cache, of the same plan and workspace.  The cache's values are
- * exact in the products: what is rounded is what respec_chunk_attn rounds.  Sums are float32 of weights up to
- * 2^8, divided in the end: of more than 2^119 / rows (2^89 for the longest caches) values may become infinities. */
+/* respec_chunk_attn over an 8-bit cache, of the same plan and workspace.  The cache's values go into the products as they
+ * are: what is rounded is what respec_chunk_attn rounds.  (bf16 plans take them in bf16, whose least step is 2^-133: values under
+ * blocks of exponent bytes 0 to 2 are rounded to it.  A key of 2^128 or more in size counts as an infinity.)  The mean of values of
+ * any size is as accurate as another, also where their sum is no float32: such rows are computed twice, as those
+ * with a NaN are. */
 respec_status respec_chunk_attn_q8(const respec_chunk_plan* plan, const respec_q8_attn_args* args, void* workspace,
                                    void* stream);
 

@@ -149,7 +149,8 @@ respec_status respec_chunk_append(const respec_chunk_plan* plan, const respec_ch
  * token does not see have no part in its output, whatever they hold.
  * Scores and sums are float32.  bf16 rounds p to bf16 before its product with V
  * (0.0019 to 0.0022 of the output's norm in all, where rounding the output alone
- * is 0.0017); float32 rounds nothing further.
+ * is 0.0017); float32 rounds nothing further.  Sums are divided in the end, and of values above 2^119 / rows
+ * (float32: 2^128 / rows) they may be infinities.
  * workspace: respec_chunk_workspace_bytes(plan) bytes, 256-byte aligned. */
 respec_status respec_chunk_attn(const respec_chunk_plan* plan, const respec_chunk_attn_args* args, void* workspace,
                                 void* stream);

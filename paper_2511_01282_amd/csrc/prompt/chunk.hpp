@@ -93,8 +93,7 @@ struct Item {
   int split, g, rb, b;
   ChunkSeq seq;
 };
-__device__ __forceinline__ Item find_item(const ChunkBatch& c, const ChunkGeom& ge, int least, int most, int x) {
-  const int lane = (int)(threadIdx.x & 63);
+__device__ __forceinline__ Item find_item(const ChunkBatch& c, const ChunkGeom& ge, int least, int most, int x, int lane) {
   int y = (int)div_by((uint32_t)x, c.kv_heads);
   Item it{0, x - y * c.n_kv_heads, 0, 0, ChunkSeq{0, 0, 0, 0}};
   for (int b0 = 0; b0 < c.batch; b0 += 64) {

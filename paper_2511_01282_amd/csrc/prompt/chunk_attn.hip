@@ -19,32 +19,33 @@ namespace {
 // product of 2048 operations, are busy 45% of the cycles; causal blocks are unequal work over one round of workgroups, and
 // 40% of the LDS cycles are conflicts (see fetch).  One token of 4 heads over 512 rows, 6.9 us.
 // Q8: the cache holds e4m3 values with a scale per block of rows; four of them at a time become what a piece is otherwise.
-template <int D, bool Q8>
-__global__ __launch_bounds__(kAttnF32Threads) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
+template <int D>
+struct F32Shape {
+  static constexpr int TK = 32;
+  static constexpr int KP = D * 4 + 16;  // bytes between K rows
+  static constexpr int VP = TK + 4;      // floats between V columns
+};
+
+// One pass over item x.  (Q8) V is taken in units of 2^UNIT (see kUnit in q8.hpp); in units of more than 1, the rows that the pass before
+// found large (`again`: 16 bits of each wave) are stored alone.  Returns whether this one found any.
+template <int D, bool Q8, int UNIT>
+__device__ __forceinline__ bool f32_rows_pass(const ChunkAttnArgs& a, int x, int lane, int wave,
+                                              unsigned char (&k_lds)[2][F32Shape<D>::TK * F32Shape<D>::KP],
+                                              float (&v_lds)[2][D * F32Shape<D>::VP], uint32_t (&again)[4]) {
   constexpr int KC = D / 16;           // 64-byte K-chunks of a head row
   constexpr int DB = D / 16;
-  constexpr int TK = 32;
-  constexpr int KP = D * 4 + 16;       // bytes between K rows
-  constexpr int VP = TK + 4;           // floats between V columns
+  constexpr int TK = F32Shape<D>::TK, KP = F32Shape<D>::KP, VP = F32Shape<D>::VP;
   constexpr int NP = TK * D / 4 / 256;  // 16-byte pieces of a tile per thread
-  __shared__ __align__(16) unsigned char k_lds[2][TK * KP];
-  __shared__ __align__(16) float v_lds[2][D * VP];
-
-  if ((int)blockIdx.x >= a.wide.items) {
-    report_status<256>(a.b, (int)blockIdx.x - a.wide.items, true);
-    return;
-  }
   const ChunkGeom& ge = a.wide;
-  const Item it = find_item(a.b, ge, 1, INT32_MAX, blockIdx.x);
+  const Item it = find_item(a.b, ge, 1, INT32_MAX, x, lane);
   const ChunkSeq& sq = it.seq;
-  if (sq.n == 0) return;
+  if (sq.n == 0) return false;
   const int rows = sq.n * a.b.group, row0 = it.rb * ge.rows_per_wg;
   const int limit = block_limit(a, ge, sq, it.rb);
   const int lo = it.split * ge.split_rows;
-  if (lo >= limit) return;
+  if (lo >= limit) return false;
   const bool whole = limit <= ge.split_rows;  // the block's only split
   const int hi = whole ? limit : min(limit, lo + ge.split_rows);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c16 = lane & 15, g4 = lane >> 4;
   const int row = row0 + wave * 16 + c16, rowc = min(row, rows - 1);
   const int i = (int)div_by((uint32_t)rowc, a.group), hh = rowc - i * a.b.group;
@@ -63,7 +64,7 @@ __global__ __launch_bounds__(kAttnF32Threads) void chunk_attn_f32_kernel(ChunkAt
   // A thread brings every eighth 16-byte piece of one row: one address per tile for all of them.  The transposed stores of a
   // wave are of 32 rows of two columns that lie 4 VP = 144 words apart, 16 of the 64 banks, so 16 banks are met twice.  The
   // row's page id is read another tile ahead.
-  const int my_row = (int)threadIdx.x % TK, my_piece = (int)threadIdx.x / TK;
+  const int my_row = lane % TK, my_piece = wave * (64 / TK) + lane / TK;
   u32x4 kp[NP], vp[NP];
   uint32_t k_byte = 127, v_byte = 127;  // (exponents of the row's scales)
   int32_t id = 0;
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(kAttnF32Threads) void chunk_attn_f32_kernel(ChunkAt
 #pragma unroll
       for (int x = 0; x < NP; ++x) {
         kp[x] = q8_floats(kp[x].x, k_byte);
-        vp[x] = q8_floats(vp[x].x, v_byte);
+        vp[x] = q8_floats(vp[x].x, v_byte - UNIT);
       }
     }
 #pragma unroll
@@ -208,21 +209,54 @@ __global__ __launch_bounds__(kAttnF32Threads) void chunk_attn_f32_kernel(ChunkAt
   }
   l += xchg<4>(l);
   l += xchg<5>(l);
-  if (row >= rows) return;
-  if (whole) {
+  const bool mine = row < rows && (UNIT == 0 || (again[wave] >> c16 & 1));
+  float size = 0.f, to_o = 1.f;
+  if constexpr (Q8 && UNIT == 0) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d) add_sizes(size, o[d]);
+  }
+  if constexpr (UNIT != 0) {
+    if (whole) to_o = __builtin_amdgcn_ldexpf(1.f, UNIT);
+    else move_unit(UNIT, m, l, to_o);
+  }
+  if (mine && whole) {
     char* to = a.out + t * a.o_tok + head * a.o_head;
     const float inv = 1.f / l;
 #pragma unroll
-    for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(to + (d * 16 + g4 * 4) * 4) = o[d] * inv;
-  } else {
+    for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(to + (d * 16 + g4 * 4) * 4) = o[d] * inv * to_o;
+  } else if (mine) {
     const int64_t hq = (int64_t)a.b.n_kv_heads * a.b.group;
     const int64_t pr = ((int64_t)it.split * a.b.total_new + t) * hq + head;
 #pragma unroll
-    for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(a.part_o + pr * D + d * 16 + g4 * 4) = o[d];
+    for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(a.part_o + pr * D + d * 16 + g4 * 4) = o[d] * to_o;
     if (g4 == 0) {
       a.part_m[pr] = m;
       a.part_l[pr] = l;
     }
+  }
+  if constexpr (!Q8 || UNIT != 0) return false;
+  uint64_t large = __ballot(mine && !(size < kLarge));
+  large |= large >> 32;
+  if (lane == 0) again[wave] = (uint32_t)(large | large >> 16) & 0xFFFFu;
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(again[0] | again[1] | again[2] | again[3]) != 0;
+}
+
+template <int D, bool Q8>
+__global__ __launch_bounds__(kAttnF32Threads) void chunk_attn_f32_kernel(ChunkAttnArgs a) {
+  using G = F32Shape<D>;
+  __shared__ __align__(16) unsigned char k_lds[2][G::TK * G::KP];
+  __shared__ __align__(16) float v_lds[2][D * G::VP];
+  __shared__ uint32_t again[4];
+  if ((int)blockIdx.x >= a.wide.items) {
+    report_status<256>(a.b, (int)blockIdx.x - a.wide.items, true);
+    return;
+  }
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (!f32_rows_pass<D, Q8, 0>(a, (int)blockIdx.x, (int)threadIdx.x & 63, wave, k_lds, v_lds, again)) return;
+  if constexpr (Q8) {
+    const Again g = again_from((int)blockIdx.x, wave);
+    f32_rows_pass<D, Q8, kUnit>(g.a, g.x, lane_id(), g.wave, k_lds, v_lds, again);
   }
 }
 

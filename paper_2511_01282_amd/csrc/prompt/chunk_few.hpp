@@ -39,7 +39,7 @@ __device__ __forceinline__ void few_rows_item(const ChunkAttnArgs& a, int x, uns
   using Feed = RowFeed<D, kFewTile / 2>;
   constexpr int KS = D / 16, DB = D / 32, NR = Feed::NR, S = G::S;
   const ChunkGeom& ge = a.few;
-  const Item it = find_item(a.b, ge, 1, a.few_rows, x);
+  const Item it = find_item(a.b, ge, 1, a.few_rows, x, (int)(threadIdx.x & 63));
   const ChunkSeq& sq = it.seq;
   if (sq.n == 0) return;
   const int rows = sq.n * a.b.group;

@@ -8,7 +8,7 @@
 // row (by the DMA's source addresses) so that fragment reads touch every bank once.
 #pragma once
 
-#include "chunk.hpp"
+#include "q8.hpp"
 
 namespace respec {
 
@@ -304,12 +304,16 @@ __device__ __forceinline__ void add_not_finite(Rows<D> (&rows)[G], const unsigne
       }
 }
 
-// Unnormalised partial (a split's) or normalised output of a lane's row.
+// Unnormalised partial (a split's) or normalised output of a lane's row; `unit`: its values are in units of 2^unit.
 template <int D>
 __device__ __forceinline__ void store_rows(Rows<D>& r, const ChunkAttnArgs& a, bool whole, int split, int64_t t, int64_t head,
-                                           bool live, int lane) {
+                                           bool live, int lane, int unit = 0) {
   const int hi = lane >> 5;
-  const float l = r.l + xchg<5>(r.l);
+  float l = r.l + xchg<5>(r.l), to_o = 1.f;
+  if (unit) {  // (uniform)
+    if (whole) to_o = __builtin_amdgcn_ldexpf(1.f, unit);
+    else move_unit(unit, r.m, l, to_o);
+  }
   if (!live) return;
   if (whole) {
     char* to = a.out + t * a.o_tok + head * a.o_head;
@@ -321,7 +325,7 @@ __device__ __forceinline__ void store_rows(Rows<D>& r, const ChunkAttnArgs& a, b
         u32x2 x;
 #pragma unroll
         for (int w = 0; w < 2; ++w)
-          x[w] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{r.o[db][4 * q + 2 * w] * inv, r.o[db][4 * q + 2 * w + 1] * inv}, bf16x2));
+          x[w] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{r.o[db][4 * q + 2 * w] * inv * to_o, r.o[db][4 * q + 2 * w + 1] * inv * to_o}, bf16x2));
         *reinterpret_cast<u32x2*>(to + (32 * db + 8 * q + 4 * hi) * 2) = x;
       }
   } else {
@@ -331,7 +335,7 @@ __device__ __forceinline__ void store_rows(Rows<D>& r, const ChunkAttnArgs& a, b
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         *reinterpret_cast<f32x4*>(a.part_o + pr * D + 32 * db + 8 * q + 4 * hi) =
-            f32x4{r.o[db][4 * q], r.o[db][4 * q + 1], r.o[db][4 * q + 2], r.o[db][4 * q + 3]};
+            f32x4{r.o[db][4 * q], r.o[db][4 * q + 1], r.o[db][4 * q + 2], r.o[db][4 * q + 3]} * to_o;
     if (hi == 0) {
       a.part_m[pr] = r.m;
       a.part_l[pr] = l;

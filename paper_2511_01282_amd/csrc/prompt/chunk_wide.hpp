@@ -34,36 +34,38 @@ struct WideShape {
   static constexpr int kSlot = 2 * kHalf;
   static constexpr int kPageIds = 384;             // page ids of a wave's window
   static constexpr int kIds = S * kSlot;
-  static constexpr int kLds = kIds + (Q8 ? 0 : kWideWaves * kPageIds * 4);
+  static constexpr int kLds = kIds + (Q8 ? kWideWaves * 4 : kWideWaves * kPageIds * 4);  // (Q8: a word of each wave)
   static_assert(kLds <= 163840 - 1024, "LDS of a CU, less report_status()'s");
 };
 
 // Q8: the cache holds e4m3 values with a scale per block.  A wave brings its rows of a pass, 16 that share a page and a
-// scale, through registers, and they become bf16, which holds them exactly, on the way into LDS.  So each value is converted
+// scale, through registers, and they become bf16 (see q8.hpp) on the way into LDS.  So each value is converted
 // once for all 256 rows, and what follows is the same.  At 64 columns both are on their way during a whole pass (K written in its
 // middle: 1% more).  At 128 K is on its way during the first half of a pass and V during the
 // second, for want of registers: both during all of it spilled 76, and 512 tokens over 16384 rows, 32 heads on 8 of 128, took 561 us.
 // Like this 148 to 158 with the card's temperature, the merge's 10 among them; 8192 tokens, 32 heads, 540 to 562 us, as over the bf16 cache.
 // V's writes meet banks twice, 17% of the LDS cycles.  Waves at a higher priority in their products: 160 instead of 155 us
 // (512 tokens).  Values left as they are in LDS after the first passes, which is wrong, 138 of 152: what the conversion costs.
-template <int D, bool Q8>
-__device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, unsigned char* smem) {
+//
+// V is taken in units of 2^UNIT (see kUnit in q8_tile.hpp); in units of more than 1, the rows that the pass before found large are
+// stored alone.  Returns whether this one found any (Q8).
+template <int D, bool Q8, int UNIT>
+__device__ __forceinline__ bool wide_rows_pass(const ChunkAttnArgs& a, int x, int lane, int wave, unsigned char* smem) {
   using G = WideShape<D, Q8>;
   using Feed = RowFeed<D, G::kRows>;
   constexpr int KS = D / 16, DB = D / 32, S = G::S, kPass = G::kPass, kRows = G::kRows, NR = Feed::NR;
   const ChunkGeom& ge = a.wide;
-  const Item it = find_item(a.b, ge, a.few_rows + 1, INT32_MAX, x);
+  const Item it = find_item(a.b, ge, a.few_rows + 1, INT32_MAX, x, lane);
   const ChunkSeq& sq = it.seq;
-  if (sq.n == 0) return;
+  if (sq.n == 0) return false;
   const int rows = sq.n * a.b.group, row0 = it.rb * ge.rows_per_wg;
   const int limit = block_limit(a, ge, sq, it.rb);
   const int lo = it.split * ge.split_rows;
-  if (lo >= limit) return;
+  if (lo >= limit) return false;
   const bool whole = limit <= ge.split_rows;  // the block's only split
   const int hi_row = whole ? limit : min(limit, lo + ge.split_rows);
   const int np = (hi_row - lo + kWideTile * kPass - 1) / (kWideTile * kPass);  // passes
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r32 = lane & 31, hi = lane >> 5;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char*)smem;
 
@@ -131,7 +133,7 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
     if constexpr (kBoth) k8.template to_lds<true>(smem + into, w_row, q8_scale(q8_scales() & 0xFF), q8_k);
     const int valid = hi_row - (lo + coming * kWideTile + w_row);  // rows that some token sees
     if (valid < kRows) v8.clear_from(valid, lane);
-    v8.template to_lds<false>(smem + into + G::kHalf, w_row, q8_scale(q8_scales() >> 16), q8_v);
+    v8.template to_lds<false>(smem + into + G::kHalf, w_row, q8_scale<UNIT>(q8_scales() >> 16), q8_v);
   };
   auto request = [&]() __attribute__((always_inline)) {
     const int u = unit++, t = kPass * u + 1 + w_tile, t0 = lo + t * kWideTile + w_row;
@@ -262,7 +264,35 @@ __device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, un
   }
   // the requests past the last pass land before the workgroup's LDS is released
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  store_rows<D>(r[0], a, whole, it.split, tok, head, wrow + r32 < rows, lane);
+  if constexpr (!Q8) {
+    store_rows<D>(r[0], a, whole, it.split, tok, head, wrow + r32 < rows, lane);
+    return false;
+  } else {
+    uint32_t* again = reinterpret_cast<uint32_t*>(smem + G::kIds);  // the waves' rows, a bit each
+    const bool mine = wrow + r32 < rows && (UNIT == 0 || (again[wave] >> r32 & 1));
+    float size = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) add_sizes(size, r[0].o[db]);
+    store_rows<D>(r[0], a, whole, it.split, tok, head, mine, lane, UNIT);
+    if constexpr (UNIT != 0) return false;
+    const uint64_t large = __ballot(mine && !(size < kLarge));
+    if (lane == 0) again[wave] = (uint32_t)large | (uint32_t)(large >> 32);
+    __syncthreads();
+    uint32_t any = 0;
+#pragma unroll
+    for (int w = 0; w < kWideWaves; ++w) any |= again[w];
+    return __builtin_amdgcn_readfirstlane(any) != 0;
+  }
+}
+
+template <int D, bool Q8>
+__device__ __forceinline__ void wide_rows_item(const ChunkAttnArgs& a, int x, unsigned char* smem) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (!wide_rows_pass<D, Q8, 0>(a, x, (int)threadIdx.x & 63, wave, smem)) return;
+  if constexpr (Q8) {
+    const Again g = again_from(x, wave);
+    wide_rows_pass<D, Q8, kUnit>(g.a, g.x, lane_id(), g.wave, smem);
+  }
 }
 
 }  // namespace respec

@@ -12,7 +12,7 @@ __global__ __launch_bounds__(kAttnFewThreads, GR <= 2 ? 2 : 1) void q8_attn_few_
     report_status<kAttnFewThreads>(a.b, (int)blockIdx.x - a.few.items, true);
     return;
   }
-  q8_few_rows_item<D, GR>(a, (int)blockIdx.x, smem);
+  q8_few_rows_item<D, GR>(a, (int)blockIdx.x, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), smem);
 }
 
 // MIXED: as chunk_attn_wide_kernel's.
@@ -27,7 +27,9 @@ __global__ __launch_bounds__(kAttnWideThreads, 1) void q8_attn_wide_kernel(Chunk
   x -= a.wide.items;
   if constexpr (MIXED) {
     if (x < a.few.items) {
-      if (threadIdx.x < 256) q8_few_rows_item<D, 2>(a, x, smem);
+      if (threadIdx.x >= 256) return;
+      const Again g = again_from(x, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+      q8_few_rows_item<D, 2>(g.a, g.x, g.wave, smem);
       return;
     }
     x -= a.few.items;

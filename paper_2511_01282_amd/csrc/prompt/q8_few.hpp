@@ -1,7 +1,7 @@
 // Causal attention of a few query rows over an 8-bit paged cache: decoding steps and short chunks.
 //
 // As chunk_few.hpp's: four waves own all the query rows and every fourth tile of 32 cache rows each, with rings of their own
-// in LDS, filled by DMA as the codes lie in memory.  The codes become bf16, exactly, on the way from LDS into the products'
+// in LDS, filled by DMA as the codes lie in memory.  The codes become bf16 (see q8.hpp) on the way from LDS into the products'
 // operands.  The cache's bytes bound it, if the matrix and vector work on them hides behind their arrival:
 //
 // * Groups of 16 query rows: a conversion costs the same for any number of rows, products and softmax less the fewer
@@ -32,7 +32,8 @@ struct Q8FewShape {
   static constexpr int kSlot = 2 * kHalf;
   static constexpr int kWave = S * kSlot;
   static constexpr int kMl = 4 * kWave;
-  static constexpr int kLds = kMl + 4 * 64 * 8;
+  static constexpr int kAgain = kMl + 4 * 64 * 8;  // 64 bits of each wave
+  static constexpr int kLds = kAgain + 4 * 8;
   static_assert(D * 64 <= kWave, "the waves hand their O over through their rings");
   static_assert(kLds <= 163840 / 2 - 1024, "two workgroups to a CU");
 };
@@ -44,43 +45,49 @@ __device__ __forceinline__ void wait_tiles(int n) {
   else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
-// Item x, by four waves (256 threads); GR groups of 16 query rows.
-template <int D, int GR>
-__device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, unsigned char* smem) {
+// One pass over item x, by four waves (256 threads); GR groups of 16 query rows.  V is taken in units of 2^UNIT (see kUnit); in units of
+// more than 1, the rows that the pass before found large are stored alone.  Returns whether this one found any.
+template <int D, int GR, int UNIT>
+__device__ __forceinline__ bool q8_few_rows_pass(const ChunkAttnArgs& a, int x, int lane, int wave, unsigned char* smem) {
   using G = Q8FewShape<D>;
   constexpr int KS = D / 32, CB = D / 16, S = G::S;
   constexpr int NR = D / 64, RPI = 1024 / D, CPR = D / 16;  // requests of 16 rows, rows of a request, chunks of a row
   static_assert(S == 2, "wait_tiles()");
   const ChunkGeom& ge = a.few;
-  const Item it = find_item(a.b, ge, 1, a.few_rows, x);
+  const Item it = find_item(a.b, ge, 1, a.few_rows, x, lane);
   const ChunkSeq& sq = it.seq;
-  if (sq.n == 0) return;
+  if (sq.n == 0) return false;
   const int rows = sq.n * a.b.group;
   const int limit = block_limit(a, ge, sq, 0);
   const int lo = it.split * ge.split_rows;
-  if (lo >= limit) return;
+  if (lo >= limit) return false;
   const bool whole = limit <= ge.split_rows;
   const int hi_row = whole ? limit : min(limit, lo + ge.split_rows);
   const int nt = (hi_row - lo + kQ8Tile - 1) / kQ8Tile;
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, g4 = lane >> 4;
   const uint32_t lds0 =
       (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char*)smem + (uint32_t)(wave * G::kWave);
   const unsigned char* ring = smem + wave * G::kWave;
   const int my_nt = nt > wave ? (nt - wave + 3) / 4 : 0;
 
-  int64_t tok[GR], head[GR];
+  // (a row's token, its head: worked out again for the output, not kept in registers)
+  struct Place {
+    int i;
+    int64_t tok, head;
+  };
+  auto place = [&](int g, int of) __attribute__((always_inline)) {
+    const int row = min(g * 16 + of, rows - 1), i = (int)div_by((uint32_t)row, a.group);
+    return Place{i, (int64_t)sq.t0 + i, (int64_t)it.g * a.b.group + (row - i * a.b.group)};
+  };
   int end[GR];
   u32x4 qf[GR][KS];
   Rows16<D> r[GR];
 #pragma unroll
   for (int g = 0; g < GR; ++g) {
-    const int row = min(g * 16 + r16, rows - 1), i = (int)div_by((uint32_t)row, a.group);
-    tok[g] = sq.t0 + i;
-    head[g] = (int64_t)it.g * a.b.group + (row - i * a.b.group);
-    end[g] = min(sq.L + i + 1, hi_row);
-    const char* q = a.q + tok[g] * a.q_tok + head[g] * a.q_head;
+    const Place at = place(g, r16);
+    end[g] = min(sq.L + at.i + 1, hi_row);
+    const char* q = a.q + at.tok * a.q_tok + at.head * a.q_head;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[g][ks] = ld16(q + (2 * (4 * (ks / 2) + g4) + ks % 2) * 16);  // (as read_k8 orders them)
     r[g].init();
@@ -137,7 +144,7 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
     const unsigned char* t = ring + (j % S) * G::kSlot;
     const int key0 = lo + (j * 4 + wave) * kQ8Tile;
     const uint32_t word = (uint32_t)__builtin_amdgcn_readlane((int)(j & 64 ? scales[1] : scales[0]), j & 63);
-    const float v0 = q8_scale((word >> 16) & 0xFF), v1 = q8_scale(word >> 24);
+    const float v0 = q8_scale<UNIT>((word >> 16) & 0xFF), v1 = q8_scale<UNIT>(word >> 24);
     u32x4 vf[CB], p[GR];
     f32x4 s[GR][2];
 #pragma unroll
@@ -183,8 +190,14 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
 
   // ---- O = sum_w 2^(m_w - M) O_w, l likewise: every wave writes its own, and joins a quarter of the columns ----
   float2* ml = reinterpret_cast<float2*>(smem + G::kMl);
+  uint64_t* again = reinterpret_cast<uint64_t*>(smem + G::kAgain);
+  const uint64_t live = UNIT ? again[0] | again[1] | again[2] | again[3] : ~0ull;
+  uint64_t large = 0;
+  int of = r16;
+  asm volatile("" : "+v"(of));
 #pragma unroll
   for (int g = 0; g < GR; ++g) {
+    const Place at = place(g, of);
     if (g > 0) __syncthreads();
     f32x4* to = reinterpret_cast<f32x4*>(smem + wave * G::kWave) + lane;
 #pragma unroll
@@ -201,31 +214,54 @@ __device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, 
     }
     l += xchg<4>(l);
     l += xchg<5>(l);
-    const bool mine = g * 16 + r16 < rows;
-    const int64_t pr = ((int64_t)it.split * a.b.total_new + tok[g]) * ((int64_t)a.b.n_kv_heads * a.b.group) + head[g];
+    const bool mine = g * 16 + r16 < rows && (live >> (g * 16 + r16) & 1);
+    const int64_t pr = ((int64_t)it.split * a.b.total_new + at.tok) * ((int64_t)a.b.n_kv_heads * a.b.group) + at.head;
     const float inv = 1.f / l;
+    float to_o = 1.f;
+    if constexpr (UNIT != 0) {
+      if (whole) to_o = __builtin_amdgcn_ldexpf(1.f, UNIT);
+      else move_unit(UNIT, M, l, to_o);
+    }
+    float size = 0.f;
 #pragma unroll
     for (int c = 0; c < CB / 4; ++c) {
       const int cb = wave * (CB / 4) + c, col = 16 * cb + 4 * g4;
       f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w_ = 0; w_ < 4; ++w_) v += (reinterpret_cast<const f32x4*>(smem + w_ * G::kWave) + lane)[cb * 64] * w[w_];
+      add_sizes(size, v);
       if (!mine) continue;
       if (whole) {
         u32x2 y;
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * e] * inv, v[2 * e + 1] * inv}, bf16x2));
-        *reinterpret_cast<u32x2*>(a.out + tok[g] * a.o_tok + head[g] * a.o_head + col * 2) = y;
+          y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * e] * inv * to_o, v[2 * e + 1] * inv * to_o}, bf16x2));
+        *reinterpret_cast<u32x2*>(a.out + at.tok * a.o_tok + at.head * a.o_head + col * 2) = y;
       } else {
-        *reinterpret_cast<f32x4*>(a.part_o + pr * D + col) = v;
+        *reinterpret_cast<f32x4*>(a.part_o + pr * D + col) = v * to_o;
       }
     }
     if (!whole && mine && wave == 0 && g4 == 0) {
       a.part_m[pr] = M;
       a.part_l[pr] = l;
     }
+    uint64_t of = __ballot(mine && !(size < kLarge));
+    of |= of >> 32;
+    large |= ((of | of >> 16) & 0xFFFF) << (16 * g);
   }
+  if constexpr (UNIT != 0) return false;
+  // (every wave knows of its columns: all of them together)
+  if (lane == 0) again[wave] = large;
+  __syncthreads();
+  return uniform_u64(again[0] | again[1] | again[2] | again[3]) != 0;
+}
+
+// Item x, by four waves (256 threads), `wave` this one; GR groups of 16 query rows.
+template <int D, int GR>
+__device__ __forceinline__ void q8_few_rows_item(const ChunkAttnArgs& a, int x, int wave, unsigned char* smem) {
+  if (!q8_few_rows_pass<D, GR, 0>(a, x, (int)threadIdx.x & 63, wave, smem)) return;
+  const Again g = again_from(x, wave);
+  q8_few_rows_pass<D, GR, kUnit>(g.a, g.x, lane_id(), g.wave, smem);
 }
 
 }  // namespace respec

@@ -3,7 +3,7 @@
 // Sixteen rows from a multiple of 16 lie in one page and share a scale (scale blocks are multiples of 16 rows, pages of
 // blocks), so a wave's rows come 16 at a time from one address, whole also where the sequence ends inside them: keys
 // behind the end are masked in the scores, and their values, which a reused page may well hold NaNs in, count as zeros.
-// bf16 holds e4m3 values times a power of two exactly.
+// bf16 holds e4m3 values times a power of two (all but the very least and largest, see q8.hpp).
 #pragma once
 
 #include "chunk_tile.hpp"
@@ -12,6 +12,8 @@
 namespace respec {
 
 __device__ __forceinline__ float q8_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+template <int UNIT>
+__device__ __forceinline__ float q8_scale(uint32_t byte) { return q8_scale((uint32_t)max((int)byte - UNIT, 0)); }
 
 // Places and scales of 16 rows each, a lane for each: rows r0 .. r0 + 15 of the sequence (r0 a multiple of 16, from the
 // sequence's end on its last 16 instead).

@@ -437,6 +437,68 @@ def test_scales_of_any_size(lib, dtype, byte):
         _close(_attend(lib, x), want, tol)
 
 
+def _with_scales(x, v_bytes):
+    """The batch with V's exponent bytes of v_bytes(sequence, row) for every block that holds a row of a sequence."""
+    c = x.c
+    x.after = [t.clone() for t in x.after]
+    for b, (n, l) in enumerate(c.sizes):
+        k, v = c.rows[b][0], torch.empty_like(c.rows[b][1])
+        for r in range(0, n + l, x.block):
+            x.after[3][int(c.table[b, r // c.page]), :, r % c.page // x.block] = v_bytes(b, r)
+        for r in range(n + l):
+            at, within = int(c.table[b, r // c.page]), r % c.page
+            v[r] = cc.values(x.after[1][at, :, within], x.after[3][at, :, within // x.block, None])
+        c.rows[b] = (k, v)
+    return x
+
+
+@pytest.mark.parametrize("kind", ["all", "late", "one", "many"])
+@pytest.mark.parametrize("dtype,sizes,kv_heads,group,head_dim,page,block", [
+    (BF, [(1, 300), (1, 90), (1, 2)], 2, 4, 128, 32, 16),
+    (BF, [(1, 3000)], 1, 7, 64, 16, 16),
+    (BF, [(4, 2500), (3, 40)], 1, 8, 128, 64, 64),
+    (BF, [(8, 0), (8, 100)], 2, 4, 64, 32, 32),
+    (BF, [(9, 1500)], 1, 7, 128, 48, 16),
+    (BF, [(60, 30), (50, 0)], 2, 1, 64, 16, 16),
+    (BF, [(200, 0)], 1, 4, 128, 128, 128),
+    (BF, [(150, 2000)], 2, 2, 64, 32, 16),
+    (BF, [(90, 2200), (3, 60), (1, 1400), (8, 0)], 1, 4, 128, 16, 16),
+    (BF, [(300, 100), (20, 9), (1, 700)], 1, 1, 64, 64, 32),
+    (F32, [(1, 900)], 2, 2, 64, 16, 16),
+    (F32, [(70, 40), (2, 300)], 1, 3, 128, 32, 32)])
+def test_values_as_large_as_the_scales_allow_q8(lib, kind, dtype, sizes, kv_heads, group, head_dim, page, block):
+    """Values of up to 448 2^119, whose sums are infinite in float32 and whose means are not: in every block, in those from
+    the middle of each sequence on (the tokens before see values of 2^-60, beside them in one group of query rows), in one block,
+    and of all kinds."""
+    x = cc.q8(sizes, dtype=dtype, heads=kv_heads * group, kv_heads=kv_heads, head_dim=head_dim, page=page, block=block, seed=14)
+    gen = random.Random(3)
+    longest = [n + l for n, l in sizes]
+    x = _with_scales(x, {"all": lambda b, r: 246, "late": lambda b, r: 60 if 2 * r < longest[b] else 246,
+                         "one": lambda b, r: 245 if r == longest[b] // 3 // block * block else 127,
+                         "many": lambda b, r: gen.choice([1, 60, 127, 200, 216, 230, 239, 246])}[kind])
+    want, tol = pc.attention(x.c)
+    assert float(want.abs().max()) < 2.0 ** 128 * (1 - 2.0 ** -8)
+    _close(_attend(lib, x), want, tol)
+
+
+@pytest.mark.parametrize("dtype,head_dim", [(BF, 64), (BF, 128), (F32, 64)])
+@pytest.mark.parametrize("sizes", [[(1, 300)], [(200, 40)], [(9, 200), (100, 300)]])
+def test_values_behind_float32_q8(lib, dtype, head_dim, sizes):
+    """A row with values of 2^128 and more, which float32 does not hold, among ordinary ones: its share of the mean is finite."""
+    x = cc.q8(sizes, dtype=dtype, heads=4, kv_heads=2, head_dim=head_dim, page=32, seed=15, q_std=0.5)
+    x.after = [t.clone() for t in x.after]
+    for b, (n, l) in enumerate(sizes):
+        r0 = (n + l) // 3 // 16 * 16
+        at, within = int(x.c.table[b, r0 // 32]), r0 % 32
+        x.after[1][at, :, within:within + 16] &= 0x80
+        x.after[1][at, :, within + 3] |= torch.randint(0x70, 0x7E, (2, head_dim), generator=torch.Generator().manual_seed(b), dtype=U8)
+    x = _with_scales(x, lambda b, r: 248 if r == sum(sizes[b]) // 3 // 16 * 16 else 127)
+    assert max(float(v.abs().max()) for _, v in x.c.rows) >= 2.0 ** 128
+    want, tol = pc.attention(x.c)
+    assert float(want.abs().max()) < 2.0 ** 128 * (1 - 2.0 ** -8)
+    _close(_attend(lib, x), want, tol)
+
+
 @pytest.mark.parametrize("longest", [0, 70])
 def test_many_sequences_q8(lib, longest):
     sizes = [((b * 7) % 4, (b * 13) % 50) for b in range(150)]

@@ -373,6 +373,46 @@ def test_attention_q8_over_more_tiles_than_a_window(lib, sizes, block):
 
 
 @pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("kind", ["16 rows", "32 rows", "64 rows", "mixed", "long"])
+def test_windows_that_move_on_q8(lib, kind, head_dim):
+    """Every form of the kernels over so many rows in one split that a wave's window of 64 tiles (of long chunks, 64 units) of
+    8192 rows moves on, of few query rows more than once: 256 KV heads and as many tokens as leave the workspace no split, or two at 64 columns,
+    whose sequences are as much longer.  A few heads are checked."""
+    h, page, block, more = 256, 64, 16, 128 // head_dim
+    per = {"16 rows": 16, "32 rows": 32, "64 rows": 64}.get(kind)
+    sizes = ([(per, 20_000 * more)] + [(per, 7 * i) for i in range(1024 // per - 1)] if per else
+             {"mixed": [(600, 9000 * more), (20, 20_000 * more), (1, 17_500 * more), (403, 100)],
+              "long": [(1024, 9000 * more)]}[kind])
+    gen = torch.Generator(device="cuda").manual_seed(head_dim)
+    pages = [-(-(n + l) // page) for n, l in sizes]
+    ids = torch.randperm(sum(pages), generator=gen, device="cuda").tolist()
+    k, v = (torch.randint(0, 256, (len(ids), h, page, head_dim), dtype=U8, generator=gen, device="cuda") & 0xBF for _ in range(2))
+    ks, vs = (torch.randint(124, 130, (len(ids), h, page // block), dtype=U8, generator=gen, device="cuda") for _ in range(2))
+    table, at = torch.full((len(sizes), max(pages)), -1, dtype=I32), 0
+    for b, n in enumerate(pages):
+        table[b, :n] = torch.tensor(ids[at:at + n])
+        at += n
+    total = sum(n for n, _ in sizes)
+    q = torch.randn(total, h, head_dim, generator=gen, device="cuda").to(BF)
+    off = torch.tensor([0] + [n for n, _ in sizes]).cumsum(0).int()
+    lens = torch.tensor([l for _, l in sizes], dtype=I32)
+    longest = dict(max_new_in_batch=max(n for n, _ in sizes), max_kv_len_in_batch=max(l for _, l in sizes))
+    plan = lib[0].ChunkPlan(n_q_heads=h, n_kv_heads=h, head_dim=head_dim, dtype=lib[1].BF16, max_batch=len(sizes), max_new=total,
+                            max_kv_len=longest["max_kv_len_in_batch"], device="cuda:0")
+    out = torch.empty_like(q)
+    plan.attend_q8(q, k.view(cc.E4M3), v.view(cc.E4M3), ks.view(cc.E8M0), vs.view(cc.E8M0), table.cuda(), off.cuda(), lens.cuda(), out, **longest)
+    torch.cuda.synchronize()
+    for head in (0, 255):
+        rows = []
+        for (n, l), t in zip(sizes, table):
+            used = t[:-(-(n + l) // page)].long().cuda()
+            rows.append(tuple(cc.values(x[used, head].cpu(), s[used, head].cpu().repeat_interleave(block, 1)[..., None]).reshape(-1, 1, head_dim)[:n + l]
+                              for x, s in ((k, ks), (v, vs))))
+        one = pc.Chunk(BF, 1, 1, head_dim, page, sizes, q[:, head:head + 1].cpu(), None, None, None, None, table, off, lens, rows)
+        _close(out[:, head:head + 1].cpu(), *pc.attention(one))
+
+
+@pytest.mark.parametrize("head_dim", [64, 128])
 @pytest.mark.parametrize("step", [32, 128])
 def test_numbers_of_splits_q8(lib, head_dim, step):
     for n in (2, 3, 4, 5, 16, 17, 64):
@@ -643,6 +683,62 @@ def test_captured_decoding_step_replays(lib):
         assert all(torch.equal(a.view(U8), b.view(U8)) for a, b in zip(cache[:4], e_cache[:4])), k
 
 
+def test_captured_sequences_that_grow(lib):
+    """A step captured once whose lengths grow by its tokens, on the device, replayed until every sequence has gone into new blocks
+    and pages; every replay against the eager calls, bit for bit, and the last one against the definition over the cache's values."""
+    news, start, page, longest = [3, 1, 0, 6], [10, 31, 7, 0], 16, 120
+    c = pc.make([(n, longest - n) for n in news], heads=4, kv_heads=2, head_dim=64, page=page, seed=13)
+    x = cc.Q8(c, 16, [torch.full((len(c.k_pages), 2, page, 64), cc.NAN_CODE, dtype=U8)] * 2 + [torch.zeros(len(c.k_pages), 2, 1, dtype=U8)] * 2, None)
+    rotary = lib[2].RotaryPlan(n_q_heads=4, n_kv_heads=2, head_dim=64, dtype=lib[1].BF16, device="cuda:0")
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    qk, counts = [t.cuda() for t in (c.q, c.k_new, c.v_new)], _ints(news)
+
+    def side():
+        cache, plan = _cache(x, x.before), _plan(lib, c, max_kv_len=longest)
+        for t in cache[:2]:   # (rows in front: a value of every row)
+            t.view(U8).fill_(0x38)
+        cache[2].view(U8).fill_(120), cache[3].view(U8).fill_(125)
+        cache[6].copy_(torch.tensor(start, dtype=I32))
+        turned, out = [torch.zeros_like(t) for t in qk[:2]], torch.zeros_like(qk[0])
+
+        def step():
+            rotary.rotate(qk[0], qk[1], turned[0], turned[1], new_off=cache[5], kv_len=cache[6])
+            plan.append_q8(turned[1], qk[2], *cache, max_new_in_batch=6)
+            plan.attend_q8(turned[0], *cache, out, max_new_in_batch=6, max_kv_len_in_batch=longest)
+            cache[6].add_(counts)
+        return cache, turned, out, step
+
+    cache, turned, out, step = side()
+    e_cache, e_turned, e_out, e_step = side()
+    apart = torch.cuda.Stream()
+    with torch.cuda.stream(apart):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for a, b in zip(cache, e_cache):
+        a.view(U8).copy_(b.view(U8))
+    for k in range(17):
+        for t in qk:
+            t.normal_(generator=gen)
+        lens = cache[6].tolist()
+        graph.replay()
+        torch.cuda.synchronize()
+        e_step()
+        torch.cuda.synchronize()
+        assert torch.equal(out, e_out) and all(torch.equal(a.view(U8), b.view(U8)) for a, b in zip(cache, e_cache)), k
+        if k % 4 == 0:
+            state = [t.view(U8).cpu() for t in cache[:4]]
+            c.sizes, c.q, c.rows = [(n, l) for n, l in zip(news, lens)], turned[0].cpu(), []
+            for (n, l), pages in zip(c.sizes, c.table.tolist()):
+                at = [(pages[r // page], r % page) for r in range(n + l)]
+                c.rows.append(tuple(torch.stack([cc.values(state[w][p, :, i], state[2 + w][p, :, 0, None]) for p, i in at]) if at else None
+                                    for w in (0, 1)))
+            _close(out.cpu(), *pc.attention(c))
+    assert cache[6].tolist() == [l + 17 * n for l, n in zip(start, news)]
+
+
 # ---------------------------------------------------------------------------
 # rows kept
 # ---------------------------------------------------------------------------
@@ -805,6 +901,81 @@ def test_verification_then_kept_rows(lib):
     rows = L + 3
     torch.testing.assert_close(k[:, :, :rows].cpu(), torch.from_numpy(np.ascontiguousarray(want.k_cache[:, :, :rows])), rtol=0, atol=0)
     torch.testing.assert_close(v[:, :, :rows].cpu(), torch.from_numpy(np.ascontiguousarray(want.v_cache[:, :, :rows])), rtol=0, atol=0)
+
+
+def test_steps_over_kept_rows(lib):
+    """Verification steps of two sequences over one cache: each step's accepted rows are kept, and the next step reads them with the
+    lengths that the call before left on the device.  Every output is that of a step over caches built afresh, bit for bit; a second
+    layer's rows move along."""
+    import decode_loop
+    from paper_2511_01282_amd import binding, runner
+    m = decode_loop.make_model(n_heads=4, head_dim=64, hidden=256)
+    s, cap = m.shape, 96
+    prompt = [int(t) for t in decode_loop.prompt()]
+    texts, heads, d = [prompt[:20], prompt[3:44]], s.n_kv_heads, s.head_dim
+    tables = [torch.from_numpy(t).view(-1, heads, d) for t in (m.E_k, m.E_v)]
+    caches = [torch.full((2, 2, heads, cap, d), math.nan, device="cuda") for _ in tables]
+
+    def put(to, table, b, first, tokens, factor=1.0):
+        to[b, :, first:first + len(tokens)] = table[tokens].transpose(0, 1).to(to.device) * factor
+
+    for b, text in enumerate(texts):
+        for t, table in zip(caches, tables):
+            put(t[0], table, b, 0, text[:-1])
+            put(t[1], table, b, 0, text[:-1], 2.0)
+    lens, pages, layers = _ints([len(t) - 1 for t in texts]), _ints([[0], [1]]), lib[2].CacheLayers(*caches)
+    accepted = set()
+    for step in range(5):
+        trees = []
+        for b, text in enumerate(texts):
+            right, at = [], list(text)
+            for _ in range(3):
+                right.append(int(runner.run(decode_loop.workload(m, at, [-1], [at[-1]], [0]), device="cuda:0")["argmax"][0]))
+                at.append(right[-1])
+            wrong = [(t + 1) % s.vocab for t in right]
+            if (step + b) % 3 == 2:   # no node but the root is right
+                trees.append(([text[-1], wrong[0]], [-1, 0]))
+            else:                     # two or three are, behind wrong ones
+                n = 6 + 2 * (step % 2)
+                trees.append(([text[-1], wrong[0], wrong[1], right[0], wrong[1], right[1], wrong[2], right[2]][:n], [-1, 0, 1, 0, 3, 3, 5, 5][:n]))
+        loads = [decode_loop.workload(m, text, parents, tokens, [0] * len(tokens)) for text, (tokens, parents) in zip(texts, trees)]
+        ins = [runner.upload(w, "cuda:0") for w in loads]
+        both = {n: torch.cat([i[n] for i in ins]) for n in ("hidden", "parent", "token", "src")}
+        sizes = [len(t) for t, _ in trees]
+        both.update(lm_head=ins[0]["lm_head"], node_off=_ints([0, sizes[0], sum(sizes)]))
+        fresh = [torch.zeros(2, heads, cap, d, device="cuda") for _ in tables]
+        for b, (text, (tokens, _)) in enumerate(zip(texts, trees)):
+            for t, f, table in zip(caches, fresh, tables):
+                put(f, table, b, 0, text[:-1] + tokens)
+                put(t[0], table, b, len(text) - 1, tokens)
+                put(t[1], table, b, len(text) - 1, tokens, 2.0)
+        kw = dict(runner.step_kwargs(loads[0]), batch=2, total_nodes=sum(sizes), max_nodes_in_batch=max(sizes),
+                  max_kv_len_in_batch=max(len(t) - 1 for t in texts), kv_capacity=cap)
+        plan = runner.make_plan(loads[0], "cuda:0", max_batch=2, max_nodes=8, max_kv_len=cap)
+        outs = []
+        for (k, v), length in (((caches[0][0], caches[1][0]), lens), (fresh, _ints([len(t) - 1 for t in texts]))):
+            out = binding.alloc_outputs(total_nodes=sum(sizes), batch=2, hidden=s.hidden, vocab=s.vocab, topk_out=s.topk_out, max_depth=s.max_depth,
+                                        device="cuda:0", attn_out=True)
+            for t in out.values():   # (a strict step leaves some outputs alone)
+                if t is not None:
+                    t.zero_()
+            plan.step(dict(both, k_cache=k, v_cache=v, kv_len=length), out, **kw)
+            outs.append(out)
+        for name, t in outs[0].items():
+            assert t is None or torch.equal(t, outs[1][name]), (step, name)
+        new, st = _ints([-1, -1]), _ints([-1, -1])
+        layers.keep_rows(pages, lens, outs[0]["path"], outs[0]["acc_len"], new, status=st)
+        for b, (tokens, _) in enumerate(trees):
+            acc = int(outs[0]["acc_len"][b])
+            path = outs[0]["path"][b, :acc + 1].tolist()
+            accepted.add(acc)
+            texts[b] = texts[b] + [tokens[i] for i in path[1:]] + [int(outs[0]["bonus"][b])]
+            for t, table in zip(caches, tables):
+                rows = table[texts[b][:-1]].transpose(0, 1)
+                assert torch.equal(t[0, b, :, :rows.shape[1]].cpu(), rows) and torch.equal(t[1, b, :, :rows.shape[1]].cpu(), rows * 2)
+        assert st.tolist() == [0, 0] and new.tolist() == [len(t) - 1 for t in texts]
+        lens = new
+    assert accepted >= {0, 2, 3}
 
 
 # ---------------------------------------------------------------------------

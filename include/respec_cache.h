@@ -167,6 +167,8 @@ respec_status respec_chunk_attn_q8(const respec_chunk_plan* plan, const respec_q
  * ids, ascending, the root's 0 first), and kv_len_out[b] = kv_len[b] + acc_len[b] + 1.
  * acc_len[b] = -1 (a step that failed for the sequence): nothing moves, kv_len_out[b] = kv_len[b].
  * A sequence with a non-zero status: nothing moves, kv_len_out[b] = kv_len[b].
+ * A page with rows that move, or that rows move to, belongs to one sequence (copy a shared, partly filled page first), and rows
+ * of layers, pages and heads to one place each (RESPEC_ERR_SHAPE for a stride of less than a row).
  * kv_len_out and seq_status share no byte with kv_len, acc_len, the paths, the page table's rows or each other
  * (RESPEC_ERR_SHAPE): they are written while other workgroups may still read. */
 typedef struct {

@@ -198,6 +198,10 @@ respec_status respec_cache_keep(const respec_cache_keep_args* args, void* stream
   a.kv_len_out = x.kv_len_out;
   a.pieces = x.n_kv_heads * x.head_dim * es / 16;
   if (!launchable(ceil_div(2 * a.pieces, kKeepThreads) * x.n_layers * x.batch, kKeepThreads)) return RESPEC_ERR_SHAPE;
+  const int64_t row = (int64_t)x.head_dim * es;
+  if (overlap_within(x.n_layers, a.layer_stride, row) || overlap_within(c.n_pages, c.page_stride * es, row) ||
+      overlap_within(x.n_kv_heads, c.head_stride * es, row) || overlap_within(c.page_size, c.row_stride * es, row))
+    return RESPEC_ERR_SHAPE;  // (rows in one place would be moved more than once)
   // A sequence's length and status are written by its first workgroup, while those of other layers may not have started.
   const int64_t ints = 4ll * x.batch;
   const __int128 path_step = x.batch > 1 ? (__int128)4 * x.path_stride : 0, table_step = x.batch > 1 ? (__int128)4 * c.table_stride : 0;

@@ -388,6 +388,25 @@ def test_keep_binding_refuses_what_it_reads(lib):
     assert seen == [SHAPE] * 3
 
 
+@pytest.mark.parametrize("over", [{"layer_stride": 0}, {"layer_stride": 56}, {"page_stride": 0}, {"head_stride": 0}, {"head_stride": 8}, {"row_stride": 0},
+                                  {"row_stride": 56}])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_keep_moves_no_row_twice(lib, p, over, dtype):  # noqa: F811
+    """Layers, pages, heads or rows in one place: every one of them would be moved there, the later ones what was moved already."""
+    a = _keep_args(lib, p, dtype=dtype, **over)
+    assert lib.lib().respec_cache_keep(ctypes.byref(a), None) == SHAPE
+
+
+def test_keep_binding_refuses_expanded_layers(lib):
+    i32 = torch.int32
+    k = torch.zeros(1, 5, 2, 16, 64, dtype=torch.bfloat16).expand(3, 5, 2, 16, 64)
+    layers = lib.CacheLayers(k, k)
+    layers._call = lambda fn, name, args, stream: seen.append(fn(args, None))
+    seen, path = [], torch.zeros(2, 6, dtype=i32)
+    layers.keep_rows(torch.zeros(2, 3, dtype=i32), torch.zeros(2, dtype=i32), path, torch.zeros(2, dtype=i32))
+    assert seen == [SHAPE]
+
+
 # ---------------------------------------------------------------------------
 # statuses in the place of what a call reads
 # ---------------------------------------------------------------------------

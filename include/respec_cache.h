@@ -3,7 +3,8 @@
  * Beside respec_prompt.h's append and attention over a cache of the model's type:
  *
  *   respec_rotary            rotary positions of queries and keys, of new tokens and of
- *                            the nodes of a draft tree
+ *                            the nodes of a draft tree (a verification step takes a node's
+ *                            query from its hidden state as it is: for it, of the keys)
  *   respec_chunk_append_q8   K/V rows of new tokens into a paged cache of 8-bit values
  *   respec_chunk_attn_q8     causal attention of new tokens over that cache
  *   respec_cache_keep        the accepted path of every verified draft tree moves to the

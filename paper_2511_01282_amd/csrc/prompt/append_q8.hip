@@ -9,7 +9,8 @@
 // Earlier rows are read only where their scale grows.
 //
 // 8057 tokens of 32 heads of 128, bf16, blocks of 32 rows (198 MB): 41 to 43 us, 4.6 to 4.8 TB/s, as a large copy.  96 sequences of one
-// token each, 8 heads: 4.8 to 5.4 us, which is a launch and three dependent reads (lengths, page id, scale).
+// token each, 8 heads: 4.5 to 5.4 us, which is a launch and three dependent reads (lengths, page id, scale).  Every wave walks over the
+// batch for its block: 1024 sequences 21 us, 4096 175, 16384 2241 (calls).
 #include "q8.hpp"
 
 namespace respec {

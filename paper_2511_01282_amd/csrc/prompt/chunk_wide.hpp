@@ -43,7 +43,7 @@ struct WideShape {
 // once for all 256 rows, and what follows is the same.  At 64 columns both are on their way during a whole pass (K written in its
 // middle: 1% more).  At 128 K is on its way during the first half of a pass and V during the
 // second, for want of registers: both during all of it spilled 76, and 512 tokens over 16384 rows, 32 heads on 8 of 128, took 561 us.
-// Like this 148 to 158 with the card's temperature, the merge's 10 among them; 8192 tokens, 32 heads, 540 to 562 us, as over the bf16 cache.
+// Like this 144 to 158 with the card's temperature, the merge's 10 among them; 8192 tokens, 32 heads, 514 to 562 us, as over the bf16 cache.
 // V's writes meet banks twice, 17% of the LDS cycles.  Waves at a higher priority in their products: 160 instead of 155 us
 // (512 tokens).  Values left as they are in LDS after the first passes, which is wrong, 138 of 152: what the conversion costs.
 //

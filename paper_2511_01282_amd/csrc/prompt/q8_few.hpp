@@ -15,8 +15,9 @@
 // * Sequences' lines of tiles dealt evenly over the workgroups: 62 us.  The longest splits first: 61, and 64 tokens over 200-3000 rows 38
 //   instead of 33.
 //
-// The 32 tokens: 268 MB in 53 to 56 us (4.8 to 5.1 TB/s; batches of equal lengths 5.2 to 5.4), and 5 for the merge.  One token
-// over 32767 rows, 28 heads on 4: 33.6 MB in 10.1 to 11.5 us.
+// The 32 tokens: 268 MB in 52 to 58 us (4.6 to 5.1 TB/s; batches of equal lengths 5.2 to 5.4), and 5 for the merge.  One token
+// over 32767 rows, 28 heads on 4: 33.6 MB in 9.8 to 12.3 us.  Two groups: 24 sequences of 4 to 8 tokens over 2000-16000 rows, 32 heads on 8
+// of 128, 339 MB in 86 us; four groups, 9 to 16 tokens, 341 MB in 145: one workgroup to a CU.
 #pragma once
 
 #include "q8_tile.hpp"

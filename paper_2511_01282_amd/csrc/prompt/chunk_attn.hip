@@ -27,7 +27,7 @@ struct F32Shape {
 };
 
 // One pass over item x.  (Q8) V is taken in units of 2^UNIT (see kUnit in q8.hpp); in units of more than 1, the rows that the pass before
-// found large (`again`: 16 bits of each wave) are stored alone.  Returns whether this one found any.
+// found large, and did not store (`again`: 16 bits of each wave), are stored alone.  Returns whether this one found any.
 template <int D, bool Q8, int UNIT>
 __device__ __forceinline__ bool f32_rows_pass(const ChunkAttnArgs& a, int x, int lane, int wave,
                                               unsigned char (&k_lds)[2][F32Shape<D>::TK * F32Shape<D>::KP],
@@ -209,12 +209,18 @@ __device__ __forceinline__ bool f32_rows_pass(const ChunkAttnArgs& a, int x, int
   }
   l += xchg<4>(l);
   l += xchg<5>(l);
-  const bool mine = row < rows && (UNIT == 0 || (again[wave] >> c16 & 1));
-  float size = 0.f, to_o = 1.f;
+  bool mine = row < rows;
   if constexpr (Q8 && UNIT == 0) {
+    float size = 0.f;
 #pragma unroll
     for (int d = 0; d < DB; ++d) add_sizes(size, o[d]);
+    uint64_t large = __ballot(mine && !(size < kLarge));
+    large |= large >> 32;
+    if (lane == 0) again[wave] = (uint32_t)(large | large >> 16) & 0xFFFFu;
+    wave_lds_sync();
   }
+  if constexpr (Q8) mine = mine && (again[wave] >> c16 & 1) == (UNIT != 0);  // (queries may lie in the output's place: a row is stored once)
+  float to_o = 1.f;
   if constexpr (UNIT != 0) {
     if (whole) to_o = __builtin_amdgcn_ldexpf(1.f, UNIT);
     else move_unit(UNIT, m, l, to_o);
@@ -235,9 +241,6 @@ __device__ __forceinline__ bool f32_rows_pass(const ChunkAttnArgs& a, int x, int
     }
   }
   if constexpr (!Q8 || UNIT != 0) return false;
-  uint64_t large = __ballot(mine && !(size < kLarge));
-  large |= large >> 32;
-  if (lane == 0) again[wave] = (uint32_t)(large | large >> 16) & 0xFFFFu;
   __syncthreads();
   return __builtin_amdgcn_readfirstlane(again[0] | again[1] | again[2] | again[3]) != 0;
 }

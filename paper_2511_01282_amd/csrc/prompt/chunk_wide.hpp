@@ -47,8 +47,8 @@ struct WideShape {
 // V's writes meet banks twice, 17% of the LDS cycles.  Waves at a higher priority in their products: 160 instead of 155 us
 // (512 tokens).  Values left as they are in LDS after the first passes, which is wrong, 138 of 152: what the conversion costs.
 //
-// V is taken in units of 2^UNIT (see kUnit in q8_tile.hpp); in units of more than 1, the rows that the pass before found large are
-// stored alone.  Returns whether this one found any (Q8).
+// V is taken in units of 2^UNIT (see kUnit in q8.hpp); in units of more than 1, the rows that the pass before found large, and did not
+// store, are stored alone.  Returns whether this one found any (Q8).
 template <int D, bool Q8, int UNIT>
 __device__ __forceinline__ bool wide_rows_pass(const ChunkAttnArgs& a, int x, int lane, int wave, unsigned char* smem) {
   using G = WideShape<D, Q8>;
@@ -269,14 +269,18 @@ __device__ __forceinline__ bool wide_rows_pass(const ChunkAttnArgs& a, int x, in
     return false;
   } else {
     uint32_t* again = reinterpret_cast<uint32_t*>(smem + G::kIds);  // the waves' rows, a bit each
-    const bool mine = wrow + r32 < rows && (UNIT == 0 || (again[wave] >> r32 & 1));
-    float size = 0.f;
+    const bool row_here = wrow + r32 < rows;
+    if constexpr (UNIT == 0) {
+      float size = 0.f;
 #pragma unroll
-    for (int db = 0; db < DB; ++db) add_sizes(size, r[0].o[db]);
-    store_rows<D>(r[0], a, whole, it.split, tok, head, mine, lane, UNIT);
+      for (int db = 0; db < DB; ++db) add_sizes(size, r[0].o[db]);
+      const uint64_t large = __ballot(row_here && !(size < kLarge));
+      if (lane == 0) again[wave] = (uint32_t)large | (uint32_t)(large >> 32);
+      wave_lds_sync();
+    }
+    // (queries may lie in the output's place: a row is stored once)
+    store_rows<D>(r[0], a, whole, it.split, tok, head, row_here && (again[wave] >> r32 & 1) == (UNIT != 0), lane, UNIT);
     if constexpr (UNIT != 0) return false;
-    const uint64_t large = __ballot(mine && !(size < kLarge));
-    if (lane == 0) again[wave] = (uint32_t)large | (uint32_t)(large >> 32);
     __syncthreads();
     uint32_t any = 0;
 #pragma unroll

@@ -47,7 +47,7 @@ __device__ __forceinline__ void wait_tiles(int n) {
 }
 
 // One pass over item x, by four waves (256 threads); GR groups of 16 query rows.  V is taken in units of 2^UNIT (see kUnit); in units of
-// more than 1, the rows that the pass before found large are stored alone.  Returns whether this one found any.
+// more than 1, the rows that the pass before found large, and did not store, are stored alone.  Returns whether this one found any.
 template <int D, int GR, int UNIT>
 __device__ __forceinline__ bool q8_few_rows_pass(const ChunkAttnArgs& a, int x, int lane, int wave, unsigned char* smem) {
   using G = Q8FewShape<D>;
@@ -191,70 +191,85 @@ __device__ __forceinline__ bool q8_few_rows_pass(const ChunkAttnArgs& a, int x, 
 
   // ---- O = sum_w 2^(m_w - M) O_w, l likewise: every wave writes its own, and joins a quarter of the columns ----
   float2* ml = reinterpret_cast<float2*>(smem + G::kMl);
-  uint64_t* again = reinterpret_cast<uint64_t*>(smem + G::kAgain);
-  const uint64_t live = UNIT ? again[0] | again[1] | again[2] | again[3] : ~0ull;
-  uint64_t large = 0;
-  int of = r16;
-  asm volatile("" : "+v"(of));
+  f32x4 v[GR][CB / 4];
+  float M[GR], l[GR];
+  uint64_t large = 0;  // rows of large sums in this wave's columns, a bit each
 #pragma unroll
   for (int g = 0; g < GR; ++g) {
-    const Place at = place(g, of);
     if (g > 0) __syncthreads();
     f32x4* to = reinterpret_cast<f32x4*>(smem + wave * G::kWave) + lane;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) to[cb * 64] = r[g].o[cb];
     ml[wave * 64 + lane] = make_float2(r[g].m, r[g].l);
     __syncthreads();
-    float M = kNoRef, w[4], l = 0.f;
+    float w[4];
+    M[g] = kNoRef;
+    l[g] = 0.f;
 #pragma unroll
-    for (int w_ = 0; w_ < 4; ++w_) M = fmaxf(M, ml[w_ * 64 + lane].x);
+    for (int w_ = 0; w_ < 4; ++w_) M[g] = fmaxf(M[g], ml[w_ * 64 + lane].x);
 #pragma unroll
     for (int w_ = 0; w_ < 4; ++w_) {
-      w[w_] = __builtin_amdgcn_exp2f(ml[w_ * 64 + lane].x - M);
-      l += w[w_] * ml[w_ * 64 + lane].y;
+      w[w_] = __builtin_amdgcn_exp2f(ml[w_ * 64 + lane].x - M[g]);
+      l[g] += w[w_] * ml[w_ * 64 + lane].y;
     }
-    l += xchg<4>(l);
-    l += xchg<5>(l);
-    const bool mine = g * 16 + r16 < rows && (live >> (g * 16 + r16) & 1);
-    const int64_t pr = ((int64_t)it.split * a.b.total_new + at.tok) * ((int64_t)a.b.n_kv_heads * a.b.group) + at.head;
-    const float inv = 1.f / l;
-    float to_o = 1.f;
-    if constexpr (UNIT != 0) {
-      if (whole) to_o = __builtin_amdgcn_ldexpf(1.f, UNIT);
-      else move_unit(UNIT, M, l, to_o);
-    }
+    l[g] += xchg<4>(l[g]);
+    l[g] += xchg<5>(l[g]);
     float size = 0.f;
 #pragma unroll
     for (int c = 0; c < CB / 4; ++c) {
-      const int cb = wave * (CB / 4) + c, col = 16 * cb + 4 * g4;
-      f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+      v[g][c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w_ = 0; w_ < 4; ++w_) v += (reinterpret_cast<const f32x4*>(smem + w_ * G::kWave) + lane)[cb * 64] * w[w_];
-      add_sizes(size, v);
-      if (!mine) continue;
+      for (int w_ = 0; w_ < 4; ++w_)
+        v[g][c] += (reinterpret_cast<const f32x4*>(smem + w_ * G::kWave) + lane)[(wave * (CB / 4) + c) * 64] * w[w_];
+      add_sizes(size, v[g][c]);
+    }
+    if constexpr (UNIT == 0) {
+      uint64_t of = __ballot(!(size < kLarge));
+      of |= of >> 32;
+      large |= ((of | of >> 16) & 0xFFFF) << (16 * g);
+    }
+  }
+  // each wave knows of its columns: all of them together
+  uint64_t* again = reinterpret_cast<uint64_t*>(smem + G::kAgain);
+  if constexpr (UNIT == 0) {
+    if (lane == 0) again[wave] = large;
+    __syncthreads();
+  }
+  large = uniform_u64(again[0] | again[1] | again[2] | again[3]);
+  int of = r16;
+  asm volatile("" : "+v"(of));
+#pragma unroll
+  for (int g = 0; g < GR; ++g) {
+    const Place at = place(g, of);
+    // (queries may lie in the output's place: a row is stored once)
+    if (g * 16 + r16 >= rows || (large >> (g * 16 + r16) & 1) != (UNIT != 0)) continue;
+    const int64_t pr = ((int64_t)it.split * a.b.total_new + at.tok) * ((int64_t)a.b.n_kv_heads * a.b.group) + at.head;
+    const float inv = 1.f / l[g];
+    float to_o = 1.f;
+    if constexpr (UNIT != 0) {
+      if (whole) to_o = __builtin_amdgcn_ldexpf(1.f, UNIT);
+      else move_unit(UNIT, M[g], l[g], to_o);
+    }
+#pragma unroll
+    for (int c = 0; c < CB / 4; ++c) {
+      const int col = 16 * (wave * (CB / 4) + c) + 4 * g4;
+      const f32x4 x = v[g][c];
       if (whole) {
         u32x2 y;
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * e] * inv * to_o, v[2 * e + 1] * inv * to_o}, bf16x2));
+          y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * e] * inv * to_o, x[2 * e + 1] * inv * to_o}, bf16x2));
         *reinterpret_cast<u32x2*>(a.out + at.tok * a.o_tok + at.head * a.o_head + col * 2) = y;
       } else {
-        *reinterpret_cast<f32x4*>(a.part_o + pr * D + col) = v * to_o;
+        *reinterpret_cast<f32x4*>(a.part_o + pr * D + col) = x * to_o;
       }
     }
-    if (!whole && mine && wave == 0 && g4 == 0) {
-      a.part_m[pr] = M;
-      a.part_l[pr] = l;
+    if (!whole && wave == 0 && g4 == 0) {
+      a.part_m[pr] = M[g];
+      a.part_l[pr] = l[g];
     }
-    uint64_t of = __ballot(mine && !(size < kLarge));
-    of |= of >> 32;
-    large |= ((of | of >> 16) & 0xFFFF) << (16 * g);
   }
-  if constexpr (UNIT != 0) return false;
-  // (every wave knows of its columns: all of them together)
-  if (lane == 0) again[wave] = large;
-  __syncthreads();
-  return uniform_u64(again[0] | again[1] | again[2] | again[3]) != 0;
+  return UNIT == 0 && large != 0;
 }
 
 // Item x, by four waves (256 threads), `wave` this one; GR groups of 16 query rows.

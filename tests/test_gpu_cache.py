@@ -521,6 +521,22 @@ def test_values_as_large_as_the_scales_allow_q8(lib, kind, dtype, sizes, kv_head
     _close(_attend(lib, x), want, tol)
 
 
+@pytest.mark.parametrize("dtype,sizes,kv_heads,group,head_dim", [
+    (BF, [(1, 300), (1, 40)], 2, 4, 128), (BF, [(8, 100), (3, 20)], 1, 4, 128), (BF, [(9, 60), (8, 90)], 1, 7, 128), (BF, [(3, 100)], 2, 4, 64),
+    (BF, [(30, 80)], 2, 2, 64), (BF, [(200, 0)], 1, 4, 128), (BF, [(150, 60), (4, 90)], 2, 2, 64), (F32, [(20, 30)], 1, 2, 64), (BF, [(1, 3000)], 1, 4, 64)])
+def test_large_values_in_place_q8(lib, dtype, sizes, kv_heads, group, head_dim):
+    """An output in the queries' place, where some columns of some rows have sums that leave float32: what is computed twice has its
+    queries twice."""
+    x = cc.q8(sizes, dtype=dtype, heads=kv_heads * group, kv_heads=kv_heads, head_dim=head_dim, page=32, seed=16)
+    x.after = [t.clone() for t in x.after]
+    x.after[1][..., 5:] &= 0x80   # (one wave's columns alone are large)
+    longest = [n + l for n, l in sizes]
+    x = _with_scales(x, lambda b, r: 127 if 2 * r < longest[b] else 246)
+    q = x.c.q.cuda()
+    _plan(lib, x.c).attend_q8(q, *_cache(x, x.after), q, max_new_in_batch=x.c.max_new, max_kv_len_in_batch=x.c.max_kv)
+    _close(q.cpu(), *pc.attention(x.c))
+
+
 @pytest.mark.parametrize("dtype,head_dim", [(BF, 64), (BF, 128), (F32, 64)])
 @pytest.mark.parametrize("sizes", [[(1, 300)], [(200, 40)], [(9, 200), (100, 300)]])
 def test_values_behind_float32_q8(lib, dtype, head_dim, sizes):

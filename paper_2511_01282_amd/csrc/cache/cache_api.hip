@@ -39,8 +39,8 @@ bool outputs_apart(const respec_rotary_plan* plan, const respec_rotary_args& x) 
   const RowSet out[2] = {rows(x.q_out, x.q_out_token_stride, hq, x.q_out_head_stride), rows(x.k_out, x.k_out_token_stride, hkv, x.k_out_head_stride)};
   for (int i = 0; i < 2; ++i) {
     if (!out[i].at) continue;
-    if (overlap_within(t, (i ? x.k_out_token_stride : x.q_out_token_stride) * es, row) ||
-        overlap_within(i ? hkv : hq, (i ? x.k_out_head_stride : x.q_out_head_stride) * es, row))
+    if (i == 0 ? overlap_within(t, x.q_out_token_stride * es, hq, x.q_out_head_stride * es, row)
+               : overlap_within(t, x.k_out_token_stride * es, hkv, x.k_out_head_stride * es, row))
       return false;
     for (int j = 0; j < 2; ++j)
       if (in[j].at && !(i == j && same_rows(out[i], in[j])) && overlap(out[i], in[j])) return false;

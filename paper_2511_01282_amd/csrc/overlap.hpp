@@ -91,5 +91,18 @@ inline bool overlap(const RowSet& a, const RowSet& b) {
 }
 // Whether two places of a tensor are sure to share a byte: neighbours in one dimension.
 inline bool overlap_within(int64_t n, int64_t step, int64_t row) { return n > 1 && step < row; }
+// Whether two places of a two-dimensional tensor share a byte.
+inline bool overlap_within(int64_t n0, int64_t step0, int64_t n1, int64_t step1, int64_t row) {
+  if (overlap_within(n0, step0, row) || overlap_within(n1, step1, row)) return true;
+  const RowSet s = row_set(nullptr, n0, step0, n1, step1, row);
+  if (s.outer.n == 1 || s.inner.n == 1 || s.outer.step >= s.inner_size || s.size == kMost) return false;
+  // places i and j further in the one dimension and the other: the two i next to j's distance
+  const Comb a = s.outer.n < s.inner.n ? s.outer : s.inner, b = s.outer.n < s.inner.n ? s.inner : s.outer;
+  for (int64_t j = 1; j < a.n; ++j) {
+    const int64_t x = j * a.step, i = x / b.step;
+    if ((i > 0 && i < b.n && x - i * b.step < row) || (i + 1 < b.n && (i + 1) * b.step - x < row)) return true;
+  }
+  return false;
+}
 
 }  // namespace respec

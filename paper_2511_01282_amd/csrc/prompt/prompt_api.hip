@@ -105,8 +105,7 @@ bool output_apart(const respec_chunk_plan* plan, const respec_chunk_attn_args& x
   const int64_t row = (int64_t)plan->s.head_dim * es, t = x.b.total_new;
   const RowSet q = row_set(x.q, t, x.q_token_stride * es, heads, x.q_head_stride * es, row);
   const RowSet out = row_set(x.out, t, x.out_token_stride * es, heads, x.out_head_stride * es, row);
-  return !overlap_within(t, x.out_token_stride * es, row) && !overlap_within(heads, x.out_head_stride * es, row) &&
-         (same_rows(q, out) || !overlap(q, out));
+  return !overlap_within(t, x.out_token_stride * es, heads, x.out_head_stride * es, row) && (same_rows(q, out) || !overlap(q, out));
 }
 
 // An 8-bit cache's batch as one over pages of one-byte elements; its scales' checks.

@@ -479,7 +479,8 @@ Q, K, ROW = FAKE + 0x100000, FAKE + 0x300000, 64   # (elements of a row; a bf16 
     {"q_out": Q + 128}, {"q_out": Q - 128}, {"q_out": Q + 16}, {"q_out": Q + 1024}, {"q_out": Q - 1024}, {"q_out": Q + 4 * 1024},
     {"q_out": Q, "q_out_token_stride": 9 * ROW}, {"q_out": Q, "q_out_token_stride": ROW, "q_out_head_stride": 5 * ROW},
     {"k_out": K + 128}, {"k_out": Q}, {"k_out": Q + 5 * 1024 - 16}, {"q_out": K}, {"q_out": K - 128 * 39}, {"k_out": FAKE + 0x200000},
-    {"k_out": FAKE + 0x200000 + 128 * 39}, {"q_out_token_stride": 0}, {"q_out_head_stride": ROW - 8}, {"k_out_token_stride": 8},
+    {"k_out": FAKE + 0x200000 + 128 * 39}, {"q_out_token_stride": 0}, {"q_out_token_stride": ROW}, {"q_out_token_stride": 7 * ROW + 8}, {"q_out_token_stride": 3 * ROW, "q_out_head_stride": 2 * ROW},
+    {"q_out_head_stride": ROW - 8}, {"k_out_token_stride": 8},
     {"q_token_stride": 0, "q_out": Q}, {"q_token_stride": 20 * ROW, "q_out": Q + 128 * 7, "q_out_token_stride": 20 * ROW},
     {"q_token_stride": 20 * ROW, "k_out": Q + 128 * 27, "k_out_token_stride": 20 * ROW},
     {"q_token_stride": 20 * ROW, "q_out": Q + 1024 - 112, "q_out_token_stride": 24 * ROW}])
@@ -511,7 +512,7 @@ def test_rotary_binding_refuses_overlapping_outputs(lib):
 
 @pytest.mark.parametrize("over", [
     {"out": Q + 128}, {"out": Q - 128}, {"out": Q + 16}, {"out": Q + 1024}, {"out": Q + 9 * 1024}, {"out": Q - 9 * 1024},
-    {"out": Q, "out_token_stride": 9 * ROW}, {"out_token_stride": 0}, {"out_head_stride": 0}, {"out_token_stride": ROW - 8},
+    {"out": Q, "out_token_stride": 9 * ROW}, {"out_token_stride": 0}, {"out_token_stride": 4 * ROW}, {"out_head_stride": 0}, {"out_token_stride": ROW - 8},
     {"q_token_stride": 20 * ROW, "out": Q + 128 * 7, "out_token_stride": 20 * ROW}])
 def test_attention_output_apart(p, over):  # noqa: F811
     """Ten tokens of 8 heads of 128 bytes (256 in float32, whose strides are as many elements)."""

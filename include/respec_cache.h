@@ -50,7 +50,7 @@ typedef struct {
 /* Row t of q and k (one head's D columns) at position p: with w_i = frequency[i],
  *   y_a = amplitude (x_a cos(p w_i) - x_b sin(p w_i)),  y_b = amplitude (x_b cos(p w_i) + x_a sin(p w_i))
  * for pair i = (a, b); columns from rotary_dim on are copied.  Angles are within 2^-31 of
- * a turn at every position; cosines, sines and products are float32, rounded once.
+ * a turn at every position; cosines, sines and products are float32, the result is rounded once.
  * Positions are given one per token, or as a chunk batch's: token i of sequence b
  * stands at kv_len[b] + i.  A token at a negative position, one of no sequence and those of a
  * sequence with a non-zero status keep what their output rows held.
